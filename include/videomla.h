@@ -341,6 +341,188 @@ int mla_dense_attention_forward(const mla_config* cfg, const void* q, const void
 int mla_decompress_window(const mla_cache* cache, const void* w_uk, const void* w_uv, void* k,
                           void* v, void* stream);
 
+/* --------------------------------------------------------------------------
+ * Rotary positions, and a latent cache in pages that many streams share.
+ *
+ * The ring above holds one window of fixed length per batch element. A server
+ * of many streams keeps their latents in one pool of pages instead: streams of
+ * different lengths, streams that start as a branch of another one and share
+ * its pages, and streams that end and give their pages back. All metadata (the
+ * page table, the lengths, the pages' reference counts) lies in device memory
+ * and is read and written by kernels, so none of these calls waits for the
+ * GPU, and all of them can be captured in a CUDA graph.
+ * ------------------------------------------------------------------------ */
+
+/* Value types of mla_rope_apply. */
+#define MLA_DTYPE_BF16 0
+#define MLA_DTYPE_FP16 1
+#define MLA_DTYPE_FP32 2
+
+/* Which two channels of the rotated part make pair i of m: 2i and 2i + 1, or
+ * i and i + m. */
+#define MLA_ROPE_INTERLEAVED 0
+#define MLA_ROPE_HALF 1
+
+/* Frequencies of mla_rope_scaled_table_fill. */
+#define MLA_ROPE_SCALE_NONE 0
+#define MLA_ROPE_SCALE_LINEAR 1
+#define MLA_ROPE_SCALE_NTK 2
+#define MLA_ROPE_SCALE_YARN 3
+
+/*
+ * A rotation of 2*(pairs_t + pairs_h + pairs_w) channels of a head.
+ *  table      fp32 [table_len][pairs][2] = (cos, sin) of every position, device
+ *             memory, 8-byte aligned; from mla_rope_table_fill or
+ *             mla_rope_scaled_table_fill
+ *  axes       coordinates per token: 3 = (t, h, w), the first pairs_t pairs turn
+ *             with t, then pairs_h with h and pairs_w with w; 1 = every pair turns
+ *             with the one coordinate (pairs_h = pairs_w = 0)
+ *  offset     first rotated channel of the head
+ *  layout     MLA_ROPE_INTERLEAVED or MLA_ROPE_HALF
+ */
+typedef struct mla_rope {
+  const void* table;
+  int table_len;
+  int pairs_t, pairs_h, pairs_w;
+  int axes;
+  int offset;
+  int layout;
+} mla_rope;
+
+/*
+ * Fill host_table (fp32 [table_len][rot_dim/2][2]) for one coordinate, with the
+ * frequencies f_i = theta^(-2i/rot_dim) scaled for contexts longer than the
+ * native_len positions that a model was trained with:
+ *  NONE    f_i
+ *  LINEAR  f_i / factor (position interpolation)
+ *  NTK     f_i with theta * factor^(rot_dim / (rot_dim - 2)): the lowest
+ *          frequency is divided by factor, the highest is kept
+ *  YARN    f_i / factor * (1 - k_i) + f_i * k_i with k_i =
+ *          clamp((r_i - beta_slow) / (beta_fast - beta_slow), 0, 1), where r_i =
+ *          native_len * f_i / (2 pi) is how often the pair turns within the native
+ *          context; cos and sin are multiplied by 0.1 ln(factor) + 1
+ * Computed in double and rounded once. MLA_ERR_ARG for a null pointer, rot_dim
+ * not even or < 2 (NTK: < 4), table_len < 1, theta <= 0, an unknown scaling,
+ * factor < 1, and for YARN native_len < 1 or beta_fast <= beta_slow.
+ */
+int mla_rope_scaled_table_fill(int rot_dim, int table_len, double theta, int scaling,
+                               double factor, int native_len, double beta_fast,
+                               double beta_slow, float* host_table);
+
+/*
+ * Rotate part of every head (Sec. 3.2; App. D.3), forward or, with inverse
+ * != 0, by the opposite angles: the inverse rotation and also its gradient
+ * (dx from dy), for a table without YaRN's factor the exact inverse.
+ *     (a, b) -> (a cos - b sin, a sin + b cos)   for every pair (a, b)
+ *  x, y    [tokens][heads][head_dim] of `dtype`, channels contiguous, the given
+ *          strides in elements between tokens and heads (any values; rows must
+ *          not overlap in y). y may be x (same strides): then only the rotated
+ *          channels are touched. Otherwise y must not overlap x, and the other
+ *          channels are copied.
+ *  pos     int32 [tokens][axes], device memory; each coordinate in [0, table_len)
+ *          (device-checked: another one is recorded as MLA_ERR_RANGE and counts
+ *          as 0)
+ * Computed in fp32 and rounded once. tokens = 0 is MLA_OK and launches nothing.
+ * x and y need the alignment of their type only; with rows that start on 16-byte
+ * boundaries the kernel moves 16 bytes at a time.
+ */
+int mla_rope_apply(const mla_rope* rope, const void* x, const int* pos, void* y, int dtype,
+                   long long tokens, int heads, int head_dim, long long x_token_stride,
+                   long long x_head_stride, long long y_token_stride, long long y_head_stride,
+                   int inverse, void* stream);
+
+/*
+ * A latent cache in pages. Caller-owned device buffers:
+ *  c      bf16 [layers][pages][page_tokens][d_c]   latents c^KV
+ *  kr     bf16 [layers][pages][page_tokens][d_r]   rotated positional keys
+ *  table  int32 [seqs][max_pages]  page of each page_tokens consecutive tokens of a
+ *         stream, -1 where it has none
+ *  lens   int32 [seqs]             tokens a stream holds
+ *  refs   int32 [pages]            streams that use a page; 0 = free
+ *  plan   scratch of mla_pages_plan_bytes() bytes for the page operations, which
+ *         run one after another on one stream
+ * Token a of stream s lies in row a % page_tokens of page table[s][a / page_tokens],
+ * the same page in every layer. A pool starts with table = -1, lens = 0, refs = 0.
+ * Rows past a stream's length and free pages are never used, whatever they hold.
+ * Sizes: page_tokens >= 8; d_c and d_r multiples of 8; at most 65,536 streams;
+ * pages * page_tokens and max_pages * page_tokens below 2^31 - 2^16; all buffers
+ * start on 16-byte boundaries.
+ */
+typedef struct mla_paged_cache {
+  void* c;
+  void* kr;
+  int* table;
+  int* lens;
+  int* refs;
+  void* plan;
+  int layers, pages, page_tokens, seqs, max_pages, d_c, d_r;
+} mla_paged_cache;
+
+/* Check the sizes of a paged cache without launching anything. */
+int mla_paged_check(const mla_paged_cache* cache);
+
+/* Bytes of `plan` (0 for bad sizes). */
+unsigned long long mla_pages_plan_bytes(const mla_paged_cache* cache);
+
+/*
+ * Give streams new lengths: new_lens int32 [seqs], -1 = leave the stream alone.
+ *  - A shorter length gives the pages past it back (0 frees the stream).
+ *  - A longer one adds pages. If the last page is partly filled and other streams
+ *    use it too, the stream first gets a copy of its own (its held rows, all
+ *    layers), so what is appended next is seen by no other stream.
+ * Pages given back by the call are free for the same call. Pages are handed out
+ * stream after stream, lowest free page first, within a stream the copy first; a
+ * shared page that all its streams copy in one call is free afterwards.
+ * If the pool runs out, the streams whose pages still fit (counted in order) grow
+ * and the others keep their length; that, and a length above max_pages * page_tokens
+ * (the stream is left alone), is recorded as MLA_ERR_RANGE in the device status.
+ */
+int mla_pages_resize(mla_paged_cache* cache, const int* new_lens, void* stream);
+
+/*
+ * Branch streams: for each of the n pairs, stream dst[i] becomes a copy of stream
+ * src[i] that shares all its pages (src, dst: int32 [n], device memory). dst must
+ * be empty (length 0) and no stream may be named as dst twice or as both; an index
+ * outside the cache or a dst that is not empty is recorded as MLA_ERR_RANGE and
+ * skipped. n = 0 is MLA_OK.
+ */
+int mla_pages_fork(mla_paged_cache* cache, const int* src, const int* dst, int n, void* stream);
+
+/*
+ * Copy whole pages, all layers: page src[i] to page dst[i] (int32 [n], device
+ * memory). No page may be a dst twice, or a dst and a src. A page outside the pool
+ * is recorded as MLA_ERR_RANGE and skipped. Metadata is not touched.
+ */
+int mla_pages_copy(mla_paged_cache* cache, const int* src, const int* dst, int n, void* stream);
+
+/*
+ * Pack the pool: with n pages in use, the pages in use among 0..n-1 stay, and the
+ * k-th page in use past them moves to the k-th free one of them (all layers).
+ * new_table [seqs][max_pages] and new_refs [pages] receive the metadata afterwards;
+ * they may be the cache's own buffers, or others that replace them once nothing
+ * reads the old ones any more. The moved pages' old rows keep their contents. Table
+ * entries that name a page not in use become -1 (MLA_ERR_RANGE if not -1 before).
+ */
+int mla_pages_compact(mla_paged_cache* cache, int* new_table, int* new_refs, void* stream);
+
+/*
+ * Write new tokens into the streams' pages (App. D.4): the tokens q_start[s] ..
+ * q_start[s+1]-1 are stream s's newest, that is its places lens[s] - n .. lens[s]-1
+ * with n = q_start[s+1] - q_start[s] (mla_pages_resize first).
+ *     c row <- c_new[i];   kr row <- RoPE(kr_new[i], pos[i])
+ *  layer    which layer of the pool
+ *  c_new    bf16 [total][d_c], kr_new bf16 [total][d_r] unrotated
+ *  q_start  int32 [seqs + 1], device memory, ascending from 0 to total
+ *  pos      int32 [total][rope->axes]
+ *  rope     rotates all d_r channels (offset 0, 2 * pairs = d_r)
+ * A token whose place has no page, a q_start that is not ascending within 0..total
+ * and a coordinate outside the table are recorded as MLA_ERR_RANGE (the token is
+ * skipped; the coordinate counts as 0). total = 0 is MLA_OK.
+ */
+int mla_paged_append(mla_paged_cache* cache, int layer, const void* c_new, const void* kr_new,
+                     int total, const int* q_start, const int* pos, const mla_rope* rope,
+                     void* stream);
+
 /*
  * Self-test of the bounded device waits that guard every mbarrier wait in the
  * tensor-core kernels (a device wait never hangs: after its limit it records

@@ -32,6 +32,8 @@ std::mutex g_mu;
 
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 
+}  // namespace
+
 // Device address of the status word on the current device, looked up once per
 // device (the address stays valid until the device's primary context is torn
 // down, e.g. by cudaDeviceReset, which the library does not survive). On
@@ -85,6 +87,8 @@ int check_resident(std::initializer_list<const void*> ptrs) {
   }
   return MLA_OK;
 }
+
+namespace {
 
 PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   std::lock_guard<std::mutex> lk(g_mu);

@@ -1,6 +1,8 @@
 // Host-side interface between the C ABI (api.cu) and the kernel files.
 #pragma once
 
+#include <initializer_list>
+
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -137,6 +139,35 @@ struct DecompressArgs {
   cudaStream_t stream;
 };
 
+// Rotary positions of part of a head, a tensor in, a tensor out.
+struct RopeArgs {
+  const void* x;        // [tokens][heads][head_dim], strides in elements
+  const int* pos;       // int32 [tokens][axes]
+  void* y;
+  const float2* table;  // [table_len][pairs]
+  long long tokens, x_tok, x_head, y_tok, y_head;
+  int heads, head_dim, table_len, pairs, pairs_t, pairs_h, axes, offset, layout, dtype, inverse;
+  int* status;
+  cudaStream_t stream;
+};
+
+// New tokens into their streams' pages.
+struct PagedAppendArgs {
+  const void* c_new;    // bf16 [total][d_c]
+  const void* kr_new;   // bf16 [total][d_r] unrotated
+  const int* q_start;   // int32 [seqs + 1]
+  const int* pos;       // int32 [total][axes]
+  void* c;              // bf16 [pages][page_tokens][d_c] of the layer
+  void* kr;             // bf16 [pages][page_tokens][d_r]
+  const int* table;     // int32 [seqs][max_pages]
+  const int* lens;      // int32 [seqs]
+  const float2* rope;   // [rope_len][d_r / 2]
+  int total, seqs, pages, page_tokens, max_pages, d_c, d_r;
+  int rope_len, pairs_t, pairs_h, axes, layout;
+  int* status;
+  cudaStream_t stream;
+};
+
 // Each launcher returns MLA_OK, MLA_ERR_UNSUPPORTED or MLA_ERR_CUDA.
 int launch_attention_tc(const AttnArgs& a);
 int launch_attention_simt(const AttnArgs& a);
@@ -148,6 +179,17 @@ int launch_output_projection(const OutProjArgs& a);
 int launch_dense_attention_tc(const DenseArgs& a);
 int launch_window_assemble(const WindowArgs& a);
 int launch_decompress(const DecompressArgs& a);
+int launch_paged_append(const PagedAppendArgs& a);
+int launch_pages_resize(const mla_paged_cache& c, const int* new_lens, int* status,
+                        cudaStream_t stream);
+int launch_pages_fork(const mla_paged_cache& c, const int* src, const int* dst, int n,
+                      int* status, cudaStream_t stream);
+int launch_pages_copy(const mla_paged_cache& c, const int* src, const int* dst, int n,
+                      int* status, cudaStream_t stream);
+int launch_pages_compact(const mla_paged_cache& c, int* new_table, int* new_refs, int* status,
+                         cudaStream_t stream);
+unsigned long long pages_plan_ints(const mla_paged_cache& c);
+int launch_rope_apply(const RopeArgs& a);
 int launch_wait_selftest(unsigned long long limit_ns, int* status, cudaStream_t stream);
 // Device address of the fixed no-allocation scratch on the current device.
 int query_scratch_address(void** out);
@@ -164,5 +206,38 @@ bool encode_map_2d_bf16(CUtensorMap* map, const void* base, unsigned long long d
                         unsigned b1, CUtensorMapSwizzle swizzle);
 
 void set_last_cuda_error(cudaError_t e);
+
+// Argument checks shared by the entry points: MLA_OK if every non-null pointer
+// is device memory of the current device, and the status word's address there
+// (null with the CUDA error recorded); check_rope is a rotation's own rules.
+int check_resident(std::initializer_list<const void*> ptrs);
+int* device_status_ptr();
+int check_rope(const mla_rope* r);
+inline bool aligned_to(const void* p, unsigned n) {
+  return (reinterpret_cast<unsigned long long>(p) & (n - 1)) == 0;
+}
+
+// cudaLaunchKernelEx with programmatic stream serialization (see grid_dep_sync).
+template <typename... P, typename... A>
+int launch_pdl(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream,
+               A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+  if (e != cudaSuccess) {
+    set_last_cuda_error(e);
+    (void)cudaGetLastError();
+    return MLA_ERR_CUDA;
+  }
+  return MLA_OK;
+}
 
 }  // namespace vmla

@@ -1,0 +1,118 @@
+// New tokens of ragged streams into their pages (App. D.4), with the positional
+// key rotated on the way (Sec. 3.2).
+//
+// One warp per token: it finds the token's stream in q_start with a 32-way
+// search, then moves the row of d_c + d_r values in 16-byte pieces. Bound by
+// latency for a decoding step and by memory for chunks.
+#include "internal.h"
+#include "ptx_sm103.cuh"
+
+namespace vmla {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct AppendK {
+  const uint4* c_new;
+  const __nv_bfloat16* kr_new;
+  const int* q_start;
+  const int* pos;
+  uint4* c;
+  __nv_bfloat16* kr;
+  const int* table;
+  const int* lens;
+  const float2* rope;
+  int total, seqs, pages, page_tokens, max_pages, d_c, d_r;
+  int rope_len, pairs_t, pairs_h, axes;
+  int* status;
+};
+
+// The last stream whose first token is not past t: every lane gets the answer.
+__device__ __forceinline__ int stream_of(const int* q_start, int seqs, int t, int lane) {
+  int lo = 0, n = seqs;
+  while (n > 1) {
+    const int step = (n + 31) / 32;
+    const int at = lane * step;
+    const bool le = at < n && __ldg(q_start + lo + at) <= t;
+    const unsigned m = __ballot_sync(0xffffffffu, le);
+    const int k = m ? 31 - __clz(m) : 0;
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return lo;
+}
+
+template <bool HALF>
+__global__ void __launch_bounds__(kThreads) paged_append_kernel(const AppendK p) {
+  grid_dep_sync();
+  const int lane = threadIdx.x & 31;
+  const int warps = gridDim.x * (kThreads / 32);
+  for (int t = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < p.total; t += warps) {
+    const int s = stream_of(p.q_start, p.seqs, t, lane);
+    const int q0 = __ldg(p.q_start + s), q1 = __ldg(p.q_start + s + 1);
+    const int len = __ldg(p.lens + s);
+    const long long a = static_cast<long long>(len) - (q1 - q0) + (t - q0);
+    const long long j = a / p.page_tokens;
+    int page = -1;
+    if (t >= q0 && t < q1 && q1 <= p.total && a >= 0 && j < p.max_pages)
+      page = __ldg(p.table + static_cast<size_t>(s) * p.max_pages + j);
+    if (page < 0 || page >= p.pages) {
+      if (lane == 0) record_status(p.status, MLA_ERR_RANGE);
+      continue;
+    }
+    const size_t row = static_cast<size_t>(page) * p.page_tokens + (a - j * p.page_tokens);
+    const int c16 = p.d_c / 8;
+    for (int i = lane; i < c16; i += 32)
+      p.c[row * c16 + i] = __ldg(p.c_new + static_cast<size_t>(t) * c16 + i);
+    const int m = p.d_r / 2;
+    const __nv_bfloat16* x = p.kr_new + static_cast<size_t>(t) * p.d_r;
+    __nv_bfloat16* y = p.kr + row * p.d_r;
+    for (int i = lane; i < m; i += 32) {
+      const int axis = p.axes == 1 || i < p.pairs_t ? 0 : (i < p.pairs_t + p.pairs_h ? 1 : 2);
+      int co = __ldg(p.pos + static_cast<size_t>(t) * p.axes + axis);
+      if (co < 0 || co >= p.rope_len) {
+        record_status(p.status, MLA_ERR_RANGE);
+        co = 0;
+      }
+      const float2 cs = __ldg(p.rope + static_cast<size_t>(co) * m + i);
+      const int ia = HALF ? i : 2 * i, ib = HALF ? i + m : 2 * i + 1;
+      const float u = __bfloat162float(x[ia]), v = __bfloat162float(x[ib]);
+      y[ia] = __float2bfloat16_rn(u * cs.x - v * cs.y);
+      y[ib] = __float2bfloat16_rn(u * cs.y + v * cs.x);
+    }
+  }
+}
+
+}  // namespace
+
+int launch_paged_append(const PagedAppendArgs& a) {
+  AppendK k;
+  k.c_new = static_cast<const uint4*>(a.c_new);
+  k.kr_new = static_cast<const __nv_bfloat16*>(a.kr_new);
+  k.q_start = a.q_start;
+  k.pos = a.pos;
+  k.c = static_cast<uint4*>(a.c);
+  k.kr = static_cast<__nv_bfloat16*>(a.kr);
+  k.table = a.table;
+  k.lens = a.lens;
+  k.rope = a.rope;
+  k.total = a.total;
+  k.seqs = a.seqs;
+  k.pages = a.pages;
+  k.page_tokens = a.page_tokens;
+  k.max_pages = a.max_pages;
+  k.d_c = a.d_c;
+  k.d_r = a.d_r;
+  k.rope_len = a.rope_len;
+  k.pairs_t = a.pairs_t;
+  k.pairs_h = a.pairs_h;
+  k.axes = a.axes;
+  k.status = a.status;
+  const int want = (a.total - 1) / (kThreads / 32) + 1;
+  const int blocks = want < 152 * 8 ? want : 152 * 8;
+  return launch_pdl(a.layout == MLA_ROPE_HALF ? paged_append_kernel<true>
+                                              : paged_append_kernel<false>,
+                    dim3(blocks), kThreads, 0, a.stream, k);
+}
+
+}  // namespace vmla

@@ -28,12 +28,23 @@ MLA_FLAG_NO_RMSNORM = 1
 MLA_FLAG_SIMT = 2
 MLA_FLAG_ROTATE_AT_USE = 4
 
+MLA_ROPE_INTERLEAVED = 0
+MLA_ROPE_HALF = 1
+MLA_ROPE_SCALE_NONE = 0
+MLA_ROPE_SCALE_LINEAR = 1
+MLA_ROPE_SCALE_NTK = 2
+MLA_ROPE_SCALE_YARN = 3
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}  # MLA_DTYPE_*
+
 # Every symbol include/videomla.h declares.
 EXPORTS = ("mla_rope_table_bytes", "mla_rope_table_fill", "mla_config_check",
            "mla_cache_reset", "mla_cache_append", "mla_attention_forward",
            "mla_absorb_weights", "mla_query_workspace_bytes", "mla_query_prologue",
            "mla_query_prologue_noalloc", "mla_output_projection", "mla_dense_attention_forward",
            "mla_window_workspace_bytes", "mla_attention_window_forward", "mla_decompress_window",
+           "mla_rope_scaled_table_fill", "mla_rope_apply", "mla_paged_check",
+           "mla_pages_plan_bytes", "mla_pages_resize", "mla_pages_fork", "mla_pages_copy",
+           "mla_pages_compact", "mla_paged_append",
            "mla_selftest_bounded_wait", "mla_status_string", "mla_last_cuda_error", "mla_device_status",
            "mla_debug_rescale_count", "mla_version")
 
@@ -56,6 +67,24 @@ class mla_cache(ctypes.Structure):
     _fields_ = [
         ("c", ctypes.c_void_p), ("kr", ctypes.c_void_p), ("rope_table", ctypes.c_void_p),
         ("frames_written", ctypes.c_longlong), ("cfg", mla_config),
+    ]
+
+
+class mla_rope(ctypes.Structure):
+    _fields_ = [
+        ("table", ctypes.c_void_p), ("table_len", ctypes.c_int),
+        ("pairs_t", ctypes.c_int), ("pairs_h", ctypes.c_int), ("pairs_w", ctypes.c_int),
+        ("axes", ctypes.c_int), ("offset", ctypes.c_int), ("layout", ctypes.c_int),
+    ]
+
+
+class mla_paged_cache(ctypes.Structure):
+    _fields_ = [
+        ("c", ctypes.c_void_p), ("kr", ctypes.c_void_p), ("table", ctypes.c_void_p),
+        ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p), ("plan", ctypes.c_void_p),
+        ("layers", ctypes.c_int), ("pages", ctypes.c_int), ("page_tokens", ctypes.c_int),
+        ("seqs", ctypes.c_int), ("max_pages", ctypes.c_int), ("d_c", ctypes.c_int),
+        ("d_r", ctypes.c_int),
     ]
 
 
@@ -107,6 +136,21 @@ def load():
     lib.mla_window_workspace_bytes.restype = ctypes.c_ulonglong
     lib.mla_attention_window_forward.argtypes = [P(mla_cache), VP, VP, VP, I, VP, VP,
                                                  ctypes.c_ulonglong, VP, VP]
+    D = ctypes.c_double
+    lib.mla_rope_scaled_table_fill.argtypes = [I, I, D, I, D, I, D, D, P(ctypes.c_float)]
+    lib.mla_rope_apply.argtypes = [P(mla_rope), VP, VP, VP, I, LL, I, I, LL, LL, LL, LL, I, VP]
+    lib.mla_paged_check.argtypes = [P(mla_paged_cache)]
+    lib.mla_pages_plan_bytes.argtypes = [P(mla_paged_cache)]
+    lib.mla_pages_plan_bytes.restype = ctypes.c_ulonglong
+    lib.mla_pages_resize.argtypes = [P(mla_paged_cache), VP, VP]
+    lib.mla_pages_fork.argtypes = [P(mla_paged_cache), VP, VP, I, VP]
+    lib.mla_pages_copy.argtypes = [P(mla_paged_cache), VP, VP, I, VP]
+    lib.mla_pages_compact.argtypes = [P(mla_paged_cache), VP, VP, VP]
+    lib.mla_paged_append.argtypes = [P(mla_paged_cache), I, VP, VP, I, VP, VP, P(mla_rope), VP]
+    for name in ("mla_rope_scaled_table_fill", "mla_rope_apply", "mla_paged_check",
+                 "mla_pages_resize", "mla_pages_fork", "mla_pages_copy", "mla_pages_compact",
+                 "mla_paged_append"):
+        getattr(lib, name).restype = I
     for name in ("mla_rope_table_fill", "mla_config_check", "mla_cache_reset", "mla_cache_append",
                  "mla_attention_forward", "mla_last_cuda_error", "mla_device_status",
                  "mla_version", "mla_absorb_weights", "mla_query_prologue",
@@ -365,6 +409,155 @@ def mla_dense_attention_forward(cfg, q, k, v, n_valid, o, stream=None):
                _dev(k, bf, (B, H, slots, dh), "k"), _dev(v, bf, (B, H, slots, dh), "v"),
                int(slots), int(n_valid), int(Nq), _dev(o, bf, (B, Nq, H, dh), "o"),
                _stream_ptr(stream)))
+
+
+def mla_rope_scaled_table_fill(rot_dim, table_len, theta=10000.0, scaling=MLA_ROPE_SCALE_NONE,
+                               factor=1.0, native_len=0, beta_fast=32.0, beta_slow=1.0):
+    """cos/sin of one coordinate, frequencies scaled for a long context, as a
+    float32 NumPy array [table_len, rot_dim/2, 2]."""
+    if rot_dim < 2 or table_len < 1:
+        raise MlaError("mla_rope_scaled_table_fill", MLA_ERR_ARG, load())
+    out = np.empty((table_len, rot_dim // 2, 2), dtype=np.float32)
+    _check("mla_rope_scaled_table_fill",
+           load().mla_rope_scaled_table_fill(
+               int(rot_dim), int(table_len), float(theta), int(scaling), float(factor),
+               int(native_len), float(beta_fast), float(beta_slow),
+               out.ctypes.data_as(ctypes.POINTER(ctypes.c_float))))
+    return out
+
+
+class Rope:
+    """A rotation: its table (float32 CUDA tensor [len, pairs, 2]) + the C struct.
+
+    pairs = (t, h, w) complex pairs per coordinate. (m, 0, 0) turns all pairs
+    with one coordinate, pos [tokens, 1], unless axes=3 says that tokens carry
+    three; offset is the first rotated channel of a head, half the layout that
+    pairs channel i with i + m instead of 2i with 2i + 1.
+    """
+
+    def __init__(self, table, pairs, offset=0, half=False, axes=None):
+        pairs = tuple(int(v) for v in pairs)
+        if len(pairs) != 3:
+            raise ValueError("pairs must be (t, h, w)")
+        self.table = table
+        self.pairs = pairs
+        self.axes = (3 if pairs[1] or pairs[2] else 1) if axes is None else int(axes)
+        _dev(table, torch.float32, (table.shape[0], sum(pairs), 2), "table")
+        self.struct = mla_rope(table=table.data_ptr(), table_len=table.shape[0],
+                               pairs_t=pairs[0], pairs_h=pairs[1], pairs_w=pairs[2],
+                               axes=self.axes, offset=int(offset),
+                               layout=MLA_ROPE_HALF if half else MLA_ROPE_INTERLEAVED)
+        self.ref = ctypes.byref(self.struct)
+
+
+def mla_rope_apply(rope, x, pos, y, inverse=False, stream=None):
+    """Rotate part of every head of x [tokens, heads, head_dim] into y (which
+    may be x); bf16, fp16 or fp32, channels contiguous, other strides free."""
+    for t, name in ((x, "x"), (y, "y")):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a CUDA tensor")
+        if t.dim() != 3 or t.shape[2] < 1 or (t.shape[2] > 1 and t.stride(2) != 1):
+            raise ValueError(f"{name} must be [tokens, heads, head_dim] with contiguous channels")
+    if x.dtype not in _DTYPES or y.dtype != x.dtype:
+        raise TypeError(f"x and y must both be bfloat16, float16 or float32, got {x.dtype}, {y.dtype}")
+    if x.shape != y.shape:
+        raise ValueError(f"y must have shape {tuple(x.shape)}, got {tuple(y.shape)}")
+    tokens, heads, dim = x.shape
+    _check("mla_rope_apply",
+           load().mla_rope_apply(
+               rope.ref, x.data_ptr(), _dev(pos, torch.int32, (tokens, rope.axes), "pos"),
+               y.data_ptr(), _DTYPES[x.dtype], tokens, heads, dim, x.stride(0), x.stride(1),
+               y.stride(0), y.stride(1), int(bool(inverse)), _stream_ptr(stream)))
+
+
+class PagedCache:
+    """A latent cache in pages over the caller's CUDA tensors + the C struct.
+
+    c bf16 [layers, pages, page_tokens, d_c]; kr bf16 [..., d_r]; table int32
+    [seqs, max_pages]; lens int32 [seqs]; refs int32 [pages]. PagedCache.empty()
+    allocates them for a pool without streams.
+    """
+
+    def __init__(self, c, kr, table, lens, refs):
+        if c.dim() != 4 or kr.dim() != 4 or table.dim() != 2:
+            raise ValueError("c and kr must be [layers, pages, page_tokens, width], table "
+                             "[seqs, max_pages]")
+        layers, pages, tokens, d_c = c.shape
+        seqs, max_pages = table.shape
+        bf, i32 = torch.bfloat16, torch.int32
+        self.c, self.kr, self.table, self.lens, self.refs = c, kr, table, lens, refs
+        self.struct = mla_paged_cache(
+            c=_dev(c, bf, c.shape, "c"),
+            kr=_dev(kr, bf, (layers, pages, tokens, kr.shape[3]), "kr"),
+            table=_dev(table, i32, table.shape, "table"), lens=_dev(lens, i32, (seqs,), "lens"),
+            refs=_dev(refs, i32, (pages,), "refs"), layers=layers, pages=pages,
+            page_tokens=tokens, seqs=seqs, max_pages=max_pages, d_c=d_c, d_r=kr.shape[3])
+        self.ref = ctypes.byref(self.struct)
+        nbytes = load().mla_pages_plan_bytes(self.ref)
+        if nbytes == 0:
+            raise MlaError("mla_pages_plan_bytes", MLA_ERR_ARG, load())
+        self.plan = torch.empty(nbytes // 4, dtype=i32, device=c.device)
+        self.struct.plan = self.plan.data_ptr()
+
+    @classmethod
+    def empty(cls, layers, pages, page_tokens, seqs, max_pages, d_c, d_r, device="cuda"):
+        bf, i32 = torch.bfloat16, torch.int32
+        return cls(torch.zeros(layers, pages, page_tokens, d_c, dtype=bf, device=device),
+                   torch.zeros(layers, pages, page_tokens, d_r, dtype=bf, device=device),
+                   torch.full((seqs, max_pages), -1, dtype=i32, device=device),
+                   torch.zeros(seqs, dtype=i32, device=device),
+                   torch.zeros(pages, dtype=i32, device=device))
+
+
+def mla_pages_resize(cache, new_lens, stream=None):
+    """Give streams new lengths (int32 [seqs], -1: leave it): pages are given
+    back or added, a shared last page that grows is copied first."""
+    _check("mla_pages_resize",
+           load().mla_pages_resize(cache.ref,
+                                   _dev(new_lens, torch.int32, (cache.struct.seqs,), "new_lens"),
+                                   _stream_ptr(stream)))
+
+
+def _pairs_of(src, dst):
+    n = src.shape[0] if isinstance(src, torch.Tensor) and src.dim() == 1 else 0
+    return _dev(src, torch.int32, (n,), "src"), _dev(dst, torch.int32, (n,), "dst"), n
+
+
+def mla_pages_fork(cache, src, dst, stream=None):
+    """Branch stream src[i] as the empty stream dst[i]; all pages are shared."""
+    _check("mla_pages_fork",
+           load().mla_pages_fork(cache.ref, *_pairs_of(src, dst), _stream_ptr(stream)))
+
+
+def mla_pages_copy(cache, src, dst, stream=None):
+    """Copy page src[i] to page dst[i] in every layer."""
+    _check("mla_pages_copy",
+           load().mla_pages_copy(cache.ref, *_pairs_of(src, dst), _stream_ptr(stream)))
+
+
+def mla_pages_compact(cache, new_table, new_refs, stream=None):
+    """Pack the pool's pages in use to its front; the metadata afterwards goes
+    to new_table and new_refs (the cache's own, or buffers that replace them)."""
+    i32 = torch.int32
+    _check("mla_pages_compact",
+           load().mla_pages_compact(cache.ref,
+                                    _dev(new_table, i32, cache.table.shape, "new_table"),
+                                    _dev(new_refs, i32, cache.refs.shape, "new_refs"),
+                                    _stream_ptr(stream)))
+
+
+def mla_paged_append(cache, layer, c_new, kr_new, q_start, pos, rope, stream=None):
+    """Write new tokens, the streams' newest, into their pages of one layer:
+    c_new [total, d_c] as is, kr_new [total, d_r] rotated at pos."""
+    st = cache.struct
+    bf, i32 = torch.bfloat16, torch.int32
+    total = c_new.shape[0] if isinstance(c_new, torch.Tensor) and c_new.dim() == 2 else 0
+    _check("mla_paged_append",
+           load().mla_paged_append(
+               cache.ref, int(layer), _dev(c_new, bf, (total, st.d_c), "c_new"),
+               _dev(kr_new, bf, (total, st.d_r), "kr_new"), total,
+               _dev(q_start, i32, (st.seqs + 1,), "q_start"),
+               _dev(pos, i32, (total, rope.axes), "pos"), rope.ref, _stream_ptr(stream)))
 
 
 def mla_selftest_bounded_wait(limit_ns, stream=None):
