@@ -523,6 +523,38 @@ int mla_paged_append(mla_paged_cache* cache, int layer, const void* c_new, const
                      int total, const int* q_start, const int* pos, const mla_rope* rope,
                      void* stream);
 
+/* Bytes of caller-owned device workspace mla_paged_attention needs (0 for bad
+ * sizes, or a d_c and d_r without a kernel). */
+unsigned long long mla_paged_workspace_bytes(const mla_paged_cache* cache);
+
+/*
+ * Absorbed-form attention (Eq. score; App. E) of the streams' newest tokens over
+ * the pages of one layer, the new tokens' own latents included (mla_paged_append
+ * first):
+ *     s_hj = (q_c,h . c_j + q_r,h . k_j) / sqrt(head_dim),  o_h = sum_j softmax_j(s_hj) c_j
+ *  q_c     bf16 [total][heads][d_c]  absorbed content queries
+ *  q_r     bf16 [total][heads][d_r]  positional queries, rotated (mla_rope_apply)
+ *  q_start int32 [seqs + 1], device memory: tokens q_start[s] .. q_start[s+1]-1 are
+ *          stream s's newest n, its places a = lens[s] - n .. lens[s] - 1 (n = 0: the
+ *          stream has none)
+ *  causal_block  keys that the token at place a sees: 0 = all lens[s]; b >= 1 = those
+ *          before the end of its block of b tokens, min(lens[s], (a / b + 1) * b): 1 is
+ *          token by token, a chunk's length is bidirectional inside a chunk (App. D.4)
+ *  o       bf16 [total][heads][d_c]; a row that sees no key (a < 0, lens[s] = 0) is 0
+ * Rows past a stream's length and free pages may hold anything, NaN included. A NaN or
+ * infinity in a key that a mask hides from some of the new tokens may reach those too.
+ * q_start not ascending within 0..total, a length past max_pages * page_tokens and a
+ * table entry that names no page are recorded as MLA_ERR_RANGE: the stream's rows are
+ * not written, or the page counts as zeros. total = 0 is MLA_OK.
+ * The workspace (16-byte aligned) is scratch of the call; calls that overlap on the
+ * GPU need one each. MLA_ERR_UNSUPPORTED unless d_c is 64, 128, 192, 256 or 512 and
+ * d_r 32 or 64. total * heads is at most 2^30.
+ */
+int mla_paged_attention(const mla_paged_cache* cache, int layer, const void* q_c,
+                        const void* q_r, int total, int heads, const int* q_start,
+                        int head_dim, int causal_block, void* workspace,
+                        unsigned long long workspace_bytes, void* o, void* stream);
+
 /*
  * Self-test of the bounded device waits that guard every mbarrier wait in the
  * tensor-core kernels (a device wait never hangs: after its limit it records

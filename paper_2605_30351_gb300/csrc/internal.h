@@ -168,6 +168,23 @@ struct PagedAppendArgs {
   cudaStream_t stream;
 };
 
+// Attention of ragged streams' newest tokens over their pages.
+struct PagedAttnArgs {
+  const void* q_c;      // bf16 [total][heads][d_c]
+  const void* q_r;      // bf16 [total][heads][d_r] rotated
+  const int* q_start;   // int32 [seqs + 1]
+  const void* c;        // bf16 [pages][page_tokens][d_c] of the layer
+  const void* kr;       // bf16 [pages][page_tokens][d_r]
+  const int* table;     // int32 [seqs][max_pages]
+  const int* lens;      // int32 [seqs]
+  void* workspace;
+  void* o;              // bf16 [total][heads][d_c]
+  int total, heads, seqs, pages, page_tokens, max_pages, d_c, d_r, causal_block;
+  float scale_log2;     // log2(e) / sqrt(head_dim)
+  int* status;
+  cudaStream_t stream;
+};
+
 // Each launcher returns MLA_OK, MLA_ERR_UNSUPPORTED or MLA_ERR_CUDA.
 int launch_attention_tc(const AttnArgs& a);
 int launch_attention_simt(const AttnArgs& a);
@@ -180,6 +197,8 @@ int launch_dense_attention_tc(const DenseArgs& a);
 int launch_window_assemble(const WindowArgs& a);
 int launch_decompress(const DecompressArgs& a);
 int launch_paged_append(const PagedAppendArgs& a);
+int launch_paged_attention(const PagedAttnArgs& a);
+unsigned long long paged_attention_workspace(int d_c, int d_r);  // 0: no kernel
 int launch_pages_resize(const mla_paged_cache& c, const int* new_lens, int* status,
                         cudaStream_t stream);
 int launch_pages_fork(const mla_paged_cache& c, const int* src, const int* dst, int n,

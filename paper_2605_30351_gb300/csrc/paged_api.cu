@@ -136,4 +136,55 @@ int mla_paged_append(mla_paged_cache* cache, int layer, const void* c_new, const
   return launch_paged_append(a);
 }
 
+unsigned long long mla_paged_workspace_bytes(const mla_paged_cache* cache) {
+  return check_sizes(cache) == MLA_OK ? paged_attention_workspace(cache->d_c, cache->d_r) : 0;
+}
+
+int mla_paged_attention(const mla_paged_cache* cache, int layer, const void* q_c, const void* q_r,
+                        int total, int heads, const int* q_start, int head_dim, int causal_block,
+                        void* workspace, unsigned long long workspace_bytes, void* o,
+                        void* stream) {
+  int rc = check_sizes(cache);
+  if (rc != MLA_OK) return rc;
+  if (layer < 0 || layer >= cache->layers || total < 0 || heads < 1 || head_dim < 1 ||
+      causal_block < 0 || static_cast<long long>(total) * heads > (1ll << 30))
+    return MLA_ERR_ARG;
+  const unsigned long long need = paged_attention_workspace(cache->d_c, cache->d_r);
+  if (need == 0) return MLA_ERR_UNSUPPORTED;
+  if (total == 0) return check_cache(cache, false);
+  if (!q_c || !q_r || !q_start || !workspace || !o || !aligned_to(q_c, 16) ||
+      !aligned_to(q_r, 16) || !aligned_to(q_start, 4) || !aligned_to(workspace, 16) ||
+      !aligned_to(o, 16) || workspace_bytes < need)
+    return MLA_ERR_ARG;
+  rc = check_cache(cache, false);
+  if (rc == MLA_OK) rc = check_resident({q_c, q_r, q_start, workspace, o});
+  if (rc != MLA_OK) return rc;
+  const size_t rows = static_cast<size_t>(cache->pages) * cache->page_tokens * layer;
+  PagedAttnArgs a;
+  a.q_c = q_c;
+  a.q_r = q_r;
+  a.q_start = q_start;
+  a.c = static_cast<char*>(cache->c) + rows * cache->d_c * 2;
+  a.kr = static_cast<char*>(cache->kr) + rows * cache->d_r * 2;
+  a.table = cache->table;
+  a.lens = cache->lens;
+  a.workspace = workspace;
+  a.o = o;
+  a.total = total;
+  a.heads = heads;
+  a.seqs = cache->seqs;
+  a.pages = cache->pages;
+  a.page_tokens = cache->page_tokens;
+  a.max_pages = cache->max_pages;
+  a.d_c = cache->d_c;
+  a.d_r = cache->d_r;
+  a.causal_block = causal_block;
+  a.scale_log2 =
+      static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(head_dim)));
+  a.status = device_status_ptr();
+  a.stream = static_cast<cudaStream_t>(stream);
+  if (!a.status) return MLA_ERR_CUDA;
+  return launch_paged_attention(a);
+}
+
 }  // extern "C"

@@ -5,6 +5,7 @@
 // search, then moves the row of d_c + d_r values in 16-byte pieces. Bound by
 // latency for a decoding step and by memory for chunks.
 #include "internal.h"
+#include "paged_common.cuh"
 #include "ptx_sm103.cuh"
 
 namespace vmla {
@@ -27,24 +28,10 @@ struct AppendK {
   int* status;
 };
 
-// The last stream whose first token is not past t: every lane gets the answer.
-__device__ __forceinline__ int stream_of(const int* q_start, int seqs, int t, int lane) {
-  int lo = 0, n = seqs;
-  while (n > 1) {
-    const int step = (n + 31) / 32;
-    const int at = lane * step;
-    const bool le = at < n && __ldg(q_start + lo + at) <= t;
-    const unsigned m = __ballot_sync(0xffffffffu, le);
-    const int k = m ? 31 - __clz(m) : 0;
-    lo += k * step;
-    n = min(step, n - k * step);
-  }
-  return lo;
-}
-
 template <bool HALF>
 __global__ void __launch_bounds__(kThreads) paged_append_kernel(const AppendK p) {
   grid_dep_sync();
+  if (blockIdx.x == 0) check_q_start(p.q_start, p.seqs, p.total, p.status);
   const int lane = threadIdx.x & 31;
   const int warps = gridDim.x * (kThreads / 32);
   for (int t = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < p.total; t += warps) {

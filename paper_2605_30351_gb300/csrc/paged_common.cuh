@@ -1,0 +1,45 @@
+// Device helpers of the paged-cache kernels.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include "ptx_sm103.cuh"
+
+namespace vmla {
+
+// The last stream whose first token is not past t: every lane gets the answer.
+__device__ __forceinline__ int stream_of(const int* q_start, int seqs, int t, int lane) {
+  int lo = 0, n = seqs;
+  while (n > 1) {
+    const int step = (n + 31) / 32;
+    const int at = lane * step;
+    const bool le = at < n && __ldg(q_start + lo + at) <= t;
+    const unsigned m = __ballot_sync(0xffffffffu, le);
+    const int k = m ? 31 - __clz(m) : 0;
+    lo += k * step;
+    n = min(step, n - k * step);
+  }
+  return lo;
+}
+
+// Record a q_start that does not ascend from 0 to total; one block calls it.
+__device__ __forceinline__ void check_q_start(const int* q_start, int seqs, int total,
+                                              int* status) {
+  for (int s = threadIdx.x; s <= seqs; s += blockDim.x) {
+    const int v = __ldg(q_start + s);
+    const int next = s < seqs ? __ldg(q_start + s + 1) : total;
+    if (v > next || (s == 0 && v != 0) || (s == seqs && v != total))
+      record_status(status, MLA_ERR_RANGE);
+  }
+}
+
+// Keys that the token at place a (it may be negative) of a stream of `held`
+// tokens sees.
+__device__ __forceinline__ int visible_keys(int a, int held, int block) {
+  if (a < 0) return 0;
+  if (block == 0) return held;
+  const long long end = (static_cast<long long>(a) / block + 1) * block;
+  return end < held ? static_cast<int>(end) : held;
+}
+
+}  // namespace vmla

@@ -44,7 +44,8 @@ EXPORTS = ("mla_rope_table_bytes", "mla_rope_table_fill", "mla_config_check",
            "mla_window_workspace_bytes", "mla_attention_window_forward", "mla_decompress_window",
            "mla_rope_scaled_table_fill", "mla_rope_apply", "mla_paged_check",
            "mla_pages_plan_bytes", "mla_pages_resize", "mla_pages_fork", "mla_pages_copy",
-           "mla_pages_compact", "mla_paged_append",
+           "mla_pages_compact", "mla_paged_append", "mla_paged_workspace_bytes",
+           "mla_paged_attention",
            "mla_selftest_bounded_wait", "mla_status_string", "mla_last_cuda_error", "mla_device_status",
            "mla_debug_rescale_count", "mla_version")
 
@@ -147,7 +148,11 @@ def load():
     lib.mla_pages_copy.argtypes = [P(mla_paged_cache), VP, VP, I, VP]
     lib.mla_pages_compact.argtypes = [P(mla_paged_cache), VP, VP, VP]
     lib.mla_paged_append.argtypes = [P(mla_paged_cache), I, VP, VP, I, VP, VP, P(mla_rope), VP]
-    for name in ("mla_rope_scaled_table_fill", "mla_rope_apply", "mla_paged_check",
+    lib.mla_paged_workspace_bytes.argtypes = [P(mla_paged_cache)]
+    lib.mla_paged_workspace_bytes.restype = ctypes.c_ulonglong
+    lib.mla_paged_attention.argtypes = [P(mla_paged_cache), I, VP, VP, I, I, VP, I, I, VP,
+                                        ctypes.c_ulonglong, VP, VP]
+    for name in ("mla_paged_attention", "mla_rope_scaled_table_fill", "mla_rope_apply", "mla_paged_check",
                  "mla_pages_resize", "mla_pages_fork", "mla_pages_copy", "mla_pages_compact",
                  "mla_paged_append"):
         getattr(lib, name).restype = I
@@ -558,6 +563,31 @@ def mla_paged_append(cache, layer, c_new, kr_new, q_start, pos, rope, stream=Non
                _dev(kr_new, bf, (total, st.d_r), "kr_new"), total,
                _dev(q_start, i32, (st.seqs + 1,), "q_start"),
                _dev(pos, i32, (total, rope.axes), "pos"), rope.ref, _stream_ptr(stream)))
+
+
+def mla_paged_workspace_bytes(cache):
+    return int(load().mla_paged_workspace_bytes(cache.ref))
+
+
+def mla_paged_attention(cache, layer, q_c, q_r, q_start, head_dim, causal_block, workspace, o,
+                        stream=None):
+    """Attention of the streams' newest tokens (q_c [total, heads, d_c], q_r
+    [total, heads, d_r] rotated; rows of stream s from q_start[s]) over the
+    pages of one layer. causal_block 0: every held token is seen; b: those
+    before the end of the token's own block of b."""
+    st = cache.struct
+    bf = torch.bfloat16
+    if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    total, heads = q_c.shape[:2]
+    _check("mla_paged_attention",
+           load().mla_paged_attention(
+               cache.ref, int(layer), _dev(q_c, bf, (total, heads, st.d_c), "q_c"),
+               _dev(q_r, bf, (total, heads, st.d_r), "q_r"), total, heads,
+               _dev(q_start, torch.int32, (st.seqs + 1,), "q_start"), int(head_dim),
+               int(causal_block), workspace.data_ptr(),
+               workspace.numel() * workspace.element_size(),
+               _dev(o, bf, (total, heads, st.d_c), "o"), _stream_ptr(stream)))
 
 
 def mla_selftest_bounded_wait(limit_ns, stream=None):
