@@ -1,6 +1,33 @@
-// Attention of ragged streams' newest tokens over a paged latent cache (Eq.
-// score; App. E): one block per (token, head) row, keys in tiles of 128 with a
-// running maximum and sum (fp32).
+// Attention of ragged streams' newest tokens over a paged latent cache, on the
+// sm_103a tensor cores (Eq. score; App. E).
+//
+// Every (token, head) row of a stream scores the same latents, so a stream's
+// rows stack along M and a key tile is read once per 128 of them:
+//     S = [q_c | q_r] . [c | k]^T      K = d_c + d_r
+//     P = exp2(S * log2(e)/sqrt(d_h) - m)   running maximum and sum in fp32;
+//                                      P is rounded to bf16 (the type of c, as
+//                                      the MMA takes both operands of one type)
+//     O += P . c                       N = d_c, c read again from the same tile
+//
+// Work is split evenly whatever the streams look like: all (row tile, key block)
+// pairs of the call form one sequence, and each CTA (or pair of CTAs) takes an
+// equal share of consecutive pairs. A chunk of thousands of tokens, one token of
+// one long stream and hundreds of ragged streams run on the same grid of one CTA
+// per SM. A row tile that lies in one share is finished there; one that several
+// shares cut writes unnormalised fp32 partial rows with their maximum and sum to
+// the workspace, and paged_join_kernel adds them up in order. The shares depend
+// on q_start and lens only, which every CTA reads for itself: no plan kernel, no
+// host round trip, and the same result from call to call.
+//
+//   warp 0     finds the pages of a key block and copies them by TMA into a ring
+//              of stages (one box per page and 64 columns)
+//   warp 1     clears rows of a stage that hold no token of the stream (they may
+//              hold NaN, and 0 * NaN would reach O), issues the score MMAs
+//   warp 6     issues O += P V
+//   warps 2-5  load Q, then the softmax: thread i owns row i
+// Pairs (CL = 2): two consecutive row tiles walk the same key blocks; each CTA
+// fetches half of the boxes and multicasts them to both. At d_c = 512 the two
+// CTAs of a pair share one row tile instead and hold 256 columns of O each.
 #include <cmath>
 
 #include "internal.h"
@@ -10,108 +37,925 @@
 namespace vmla {
 namespace {
 
-constexpr int kThreads = 128;
-constexpr int kMaxDC = 512, kMaxDR = 64;
+constexpr int kBM = 128;       // rows per tile = TMEM lanes
+constexpr int kThreads = 224;  // 7 warps
+constexpr float kRescaleLog2 = 8.0f;
+constexpr int kMaxCtas = 152;  // the workspace holds two partial tiles for each
+constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = 16;  // row groups of a joined tile
 
-__device__ __forceinline__ float block_reduce(float v, float* red, bool is_max) {
+template <int DC, int DR>
+struct PagedShape {
+  static constexpr int BN = DC > 256 ? 64 : 128;   // keys per block
+  static constexpr int DV = DC > 256 ? 256 : DC;   // output columns per CTA
+  static constexpr int DK = DC + DR;
+  static constexpr int kSplit = DC / DV;           // CTAs that share a row tile
+  static constexpr int kTileBytes = BN * DK * 2;   // one stage
+  static constexpr int kCBox = BN * 128;           // [BN keys x 64 columns] of c
+  static constexpr int kKrOff = DC * BN * 2;       // the d_r columns of a stage
+  static constexpr int kBoxes = DC / 64 + 1;       // boxes per page
+  // TMEM columns: S, P (bf16, two a column), O, and Q as far as it fits
+  static constexpr int kTmemS = 0;
+  static constexpr int kTmemP = BN;
+  static constexpr int kTmemO = BN + BN / 2;
+  static constexpr int kTmemQ = kTmemO + DV;
+  static constexpr int kBarBytes = 512;
+  static constexpr int kSmemCap = 232448;
+  static constexpr bool kQinTmem = kTmemQ + DK / 2 <= 512;
+  static constexpr bool kQSmemFits = 1024 + kBarBytes + kBM * DK * 2 + 2 * kTileBytes <= kSmemCap;
+  static constexpr int kQcTmem =
+      kQinTmem ? DC : (kQSmemFits ? 0 : ((512 - kTmemQ) * 2 / 64) * 64);
+  static constexpr int kQcSmem = DC - kQcTmem;
+  static constexpr int kQKrOff = kQcSmem * kBM * 2;
+  static constexpr int kQBytes = kQinTmem ? 0 : kQKrOff + kBM * DR * 2;
+  static constexpr int kFit = (kSmemCap - 1024 - kBarBytes - kQBytes) / kTileBytes;
+  static constexpr int kMaxStages = BN == 128 ? 4 : 6;
+  static constexpr int kStages = kFit > kMaxStages ? kMaxStages : kFit;
+  static constexpr int kSmemBytes = 1024 + kQBytes + kTileBytes * kStages + kBarBytes;
+  static constexpr uint32_t kTmemCols = 512;
+  static constexpr uint32_t kKrSw = DR == 32 ? kSw64 : kSw128;
+  static constexpr uint32_t kKrRow = DR * 2;
+  static constexpr uint32_t kKrSbo = 8 * kKrRow;
+  static constexpr uint32_t kIdescQK = idesc_bf16_f32(kBM, BN, false, false);
+  static constexpr uint32_t kIdescPV = idesc_bf16_f32(kBM, DV, false, true);
+  // workspace of one launch: partial rows, their (maximum, sum), descriptors
+  static constexpr unsigned long long kPartBytes = 2ull * kMaxCtas * kBM * DV * 4;
+  static constexpr unsigned long long kMlBytes = 2ull * kMaxCtas * kBM * 8;
+  static constexpr unsigned long long kWorkspace = kPartBytes + kMlBytes + 2ull * kMaxCtas * 16;
+  static_assert(kTmemQ + kQcTmem / 2 <= 512 && kStages >= 2, "TMEM and stages must fit");
+  static_assert(kTileBytes % 1024 == 0 && kKrOff % 1024 == 0 && kQKrOff % 1024 == 0,
+                "swizzle-atom alignment");
+};
+
+struct PagedK {
+  const __nv_bfloat16* q_c;
+  const __nv_bfloat16* q_r;
+  const int* q_start;
+  const int* table;
+  const int* lens;
+  __nv_bfloat16* o;
+  float* part_o;
+  float2* part_ml;
+  int4* part_desc;  // first row in o, rows, 1 = ends its tile, -
+  int total, heads, seqs, pages, page_tokens, max_pages, block;
+  // Key blocks never straddle a group of `group` tokens: BN tokens (per_group
+  // whole pages) where the pages divide a block, else one page.
+  int group, blocks, per_group;
+  int box_rows;
+  float scale_log2;
+  int* status;
+};
+
+struct Stream {
+  int q0, n, len;
+};
+
+__device__ __forceinline__ Stream stream_at(const PagedK& p, int s) {
+  Stream t{__ldg(p.q_start + s), __ldg(p.q_start + s + 1), __ldg(p.lens + s)};
+  const int q1 = t.n;
+  t.n = q1 - t.q0;
+  if (t.q0 < 0 || q1 < t.q0 || q1 > p.total || t.len < 0 ||
+      t.len > static_cast<long long>(p.max_pages) * p.page_tokens)
+    t.n = 0;
+  return t;
+}
+
+// Key blocks of row tile `tile` (TR rows) of a stream: what its last row, which
+// sees most, needs; at least one, so that rows that see nothing are written.
+template <int BN, int TR>
+__device__ __forceinline__ int tile_blocks(const PagedK& p, int n, int len, int tile) {
+  const int last = min(n * p.heads, (tile + 1) * TR) - 1;
+  const int keys = visible_keys(len - n + last / p.heads, len, p.block);
+  const int whole = keys / p.group, rest = keys - whole * p.group;
+  return max(1, whole * p.blocks + (rest + BN - 1) / BN);
+}
+
+__device__ __forceinline__ long long warp_total(long long v) {
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    const float w = __shfl_xor_sync(0xffffffffu, v, d);
-    v = is_max ? fmaxf(v, w) : v + w;
-  }
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  return is_max ? fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]))
-                : (red[0] + red[1]) + (red[2] + red[3]);
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
 }
 
-__device__ __forceinline__ float dot8(uint4 v, const float* q) {
-  return bf16_lo(v.x) * q[0] + bf16_hi(v.x) * q[1] + bf16_lo(v.y) * q[2] + bf16_hi(v.y) * q[3] +
-         bf16_lo(v.z) * q[4] + bf16_hi(v.z) * q[5] + bf16_lo(v.w) * q[6] + bf16_hi(v.w) * q[7];
+// All key blocks of a stream; the whole warp calls it with its lanes' streams.
+template <int BN, int TR>
+__device__ __forceinline__ long long stream_blocks(const PagedK& p, const Stream& st) {
+  const int lane = threadIdx.x & 31;
+  const int tiles = (st.n * p.heads + TR - 1) / TR;
+  long long u = 0;
+  if (tiles <= 2)
+    for (int t = 0; t < tiles; ++t) u += tile_blocks<BN, TR>(p, st.n, st.len, t);
+  unsigned many = __ballot_sync(0xffffffffu, tiles > 2);
+  while (many) {
+    const int l = __ffs(many) - 1;
+    many &= many - 1;
+    const int n = __shfl_sync(0xffffffffu, st.n, l), len = __shfl_sync(0xffffffffu, st.len, l);
+    const int ts = __shfl_sync(0xffffffffu, tiles, l);
+    long long a = 0;
+    for (int t = lane; t < ts; t += 32) a += tile_blocks<BN, TR>(p, n, len, t);
+    a = warp_total(a);
+    if (lane == l) u = a;
+  }
+  return u;
 }
 
-__global__ void __launch_bounds__(kThreads) paged_attn_simple_kernel(const PagedAttnArgs p) {
-  grid_dep_sync();
-  __shared__ float q[kMaxDC + kMaxDR], w[kThreads], red[4];
-  __shared__ int pages[kThreads];
-  if (blockIdx.x == 0) check_q_start(p.q_start, p.seqs, p.total, p.status);
-  const __nv_bfloat16* c = static_cast<const __nv_bfloat16*>(p.c);
-  const int t = blockIdx.x / p.heads;
-  const int s = stream_of(p.q_start, p.seqs, t, threadIdx.x & 31);
-  const int q0 = p.q_start[s], q1 = p.q_start[s + 1], len = p.lens[s];
-  if (t < q0 || t >= q1 || q0 < 0 || q1 > p.total || len < 0 ||
-      len > static_cast<long long>(p.max_pages) * p.page_tokens) {
-    if (threadIdx.x == 0) record_status(p.status, MLA_ERR_RANGE);
-    return;
+struct Share {
+  int s, tile, off;  // first stream, row tile and key block
+  int pad;
+  long long count;   // key blocks
+};
+
+// Share `id` of `groups`: every thread of the block calls it. scratch: 8 long
+// longs, out: in shared memory.
+template <int BN, int TR>
+__device__ __forceinline__ void find_share(const PagedK& p, int id, int groups,
+                                           long long* scratch, Share* out) {
+  constexpr int kWarps = kThreads / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int per = (p.seqs + kThreads - 1) / kThreads;
+  long long mine = 0;
+  for (int k = 0; k < per; ++k) {
+    const int s = threadIdx.x * per + k;
+    Stream st{0, 0, 0};
+    if (s < p.seqs) st = stream_at(p, s);
+    mine += stream_blocks<BN, TR>(p, st);
   }
-  const int keys = visible_keys(len - (q1 - q0) + (t - q0), len, p.causal_block);
-  const size_t row = blockIdx.x;
-  for (int i = threadIdx.x; i < p.d_c; i += kThreads)
-    q[i] = __bfloat162float(static_cast<const __nv_bfloat16*>(p.q_c)[row * p.d_c + i]);
-  for (int i = threadIdx.x; i < p.d_r; i += kThreads)
-    q[p.d_c + i] = __bfloat162float(static_cast<const __nv_bfloat16*>(p.q_r)[row * p.d_r + i]);
-  float m = -INFINITY, l = 0.f, o[kMaxDC / kThreads] = {};
-  for (int k0 = 0; k0 < keys; k0 += kThreads) {
-    __syncthreads();
-    const int k = k0 + threadIdx.x;
-    int page = -1;
-    if (k < keys) {
-      page = p.table[static_cast<size_t>(s) * p.max_pages + k / p.page_tokens];
-      if (page < 0 || page >= p.pages) {
-        record_status(p.status, MLA_ERR_RANGE);
-        page = -1;
+  long long x = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, x, d);
+    if (lane >= d) x += y;
+  }
+  if (lane == 31) scratch[warp] = x;
+  if (threadIdx.x == 0) out->count = 0;
+  __syncthreads();
+  long long total = 0, base = x - mine;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) base += scratch[w];
+    total += scratch[w];
+  }
+  const long long active = min(static_cast<long long>(groups), total);
+  if (id < active) {
+    const long long u0 = total * id / active, u1 = total * (id + 1) / active;
+    const unsigned owner = __ballot_sync(0xffffffffu, base <= u0 && u0 < base + mine);
+    if (owner) {  // this warp walks the streams of that lane
+      const int l = __ffs(owner) - 1;
+      long long rem = u0 - __shfl_sync(0xffffffffu, base, l);
+      int s = (warp * 32 + l) * per;
+      Stream st{0, 0, 0};
+      for (; s < p.seqs; ++s) {
+        st = stream_at(p, s);
+        const Stream one = lane == 0 ? st : Stream{0, 0, 0};
+        const long long u =
+            __shfl_sync(0xffffffffu, stream_blocks<BN, TR>(p, one), 0);
+        if (rem < u) break;
+        rem -= u;
+      }
+      const int tiles = (st.n * p.heads + TR - 1) / TR;
+      for (int t0 = 0; t0 < tiles; t0 += 32) {
+        const int v = t0 + lane < tiles ? tile_blocks<BN, TR>(p, st.n, st.len, t0 + lane) : 0;
+        long long y = v;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const long long z = __shfl_up_sync(0xffffffffu, y, d);
+          if (lane >= d) y += z;
+        }
+        const long long sum = __shfl_sync(0xffffffffu, y, 31);
+        if (rem < sum) {
+          if (rem < y && rem >= y - v) {
+            out->s = s;
+            out->tile = t0 + lane;
+            out->off = static_cast<int>(rem - (y - v));
+            out->count = u1 - u0;
+          }
+          break;
+        }
+        rem -= sum;
       }
     }
-    pages[threadIdx.x] = page;
-    float sc = 0.f;
-    if (page >= 0) {
-      const size_t r = static_cast<size_t>(page) * p.page_tokens + k % p.page_tokens;
-      const uint4* cr = static_cast<const uint4*>(p.c) + r * (p.d_c / 8);
-      const uint4* kr = static_cast<const uint4*>(p.kr) + r * (p.d_r / 8);
-      for (int i = 0; i < p.d_c / 8; ++i) sc += dot8(__ldg(cr + i), q + 8 * i);
-      for (int i = 0; i < p.d_r / 8; ++i) sc += dot8(__ldg(kr + i), q + p.d_c + 8 * i);
+  }
+  __syncthreads();
+}
+
+// Walks a share segment by segment: a segment is a run of key blocks of one row
+// tile. Every role of the CTA walks it for itself.
+struct Segment {
+  Stream st;
+  int s, tile;
+  int kb0, kb1;        // key blocks [kb0, kb1)
+  bool starts, ends;   // the tile's first, last block is in it
+};
+
+template <int BN, int TR>
+struct Walk {
+  const PagedK& p;
+  Stream st;
+  int s, tile, off;
+  long long left;
+  __device__ Walk(const PagedK& k, const Share& sh)
+      : p(k), s(sh.s), tile(sh.tile), off(sh.off), left(sh.count) {
+    if (left > 0) st = stream_at(p, s);
+  }
+  __device__ bool next(Segment& g) {
+    if (left <= 0) return false;
+    while (tile * TR >= st.n * p.heads) {  // the next stream with new tokens
+      if (++s >= p.seqs) return false;
+      st = stream_at(p, s);
+      tile = 0;
     }
-    sc = k < keys ? sc * p.scale_log2 : -INFINITY;
-    const float m_new = fmaxf(m, block_reduce(sc, red, true));
-    const float base = m_new == -INFINITY ? 0.f : m_new;
-    const float e = exp2f(sc - base), alpha = exp2f(m - base);
-    w[threadIdx.x] = e;
-    l = l * alpha + block_reduce(e, red, false);
-    m = m_new;
-    const int n = min(kThreads, keys - k0);
-#pragma unroll
-    for (int i = 0; i < kMaxDC / kThreads; ++i) {
-      const int col = threadIdx.x + i * kThreads;
-      if (col >= p.d_c) break;
-      float acc = o[i] * alpha;
-      for (int j = 0; j < n; ++j)
-        if (pages[j] >= 0)
-          acc += w[j] * __bfloat162float(
-                            c[(static_cast<size_t>(pages[j]) * p.page_tokens +
-                               (k0 + j) % p.page_tokens) * p.d_c + col]);
-      o[i] = acc;
+    const int all = tile_blocks<BN, TR>(p, st.n, st.len, tile);
+    const int take = static_cast<int>(min(static_cast<long long>(all - off), left));
+    g.st = st;
+    g.s = s;
+    g.tile = tile;
+    g.kb0 = off;
+    g.kb1 = off + take;
+    g.starts = off == 0;
+    g.ends = g.kb1 == all;
+    left -= take;
+    off = 0;
+    ++tile;
+    return true;
+  }
+};
+
+// Place of key block kb: its first token, and the rows of its group from there.
+template <int BN>
+struct BlockPos {
+  int grp, sub;
+  __device__ BlockPos(const PagedK& p, int kb) : grp(kb / p.blocks), sub(kb % p.blocks) {}
+  __device__ int token(const PagedK& p) const { return grp * p.group + sub * BN; }
+  __device__ int rows(const PagedK& p) const { return min(BN, p.group - sub * BN); }
+  __device__ void step(const PagedK& p) {
+    if (++sub == p.blocks) {
+      sub = 0;
+      ++grp;
     }
   }
-  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);  // a NaN stays one
+};
+
+template <int DC, int DR, int CL>
+__global__ void __launch_bounds__(kThreads, 1)
+    paged_attn_kernel(const __grid_constant__ CUtensorMap tm_c,
+                      const __grid_constant__ CUtensorMap tm_kr, const PagedK p) {
+  using S = PagedShape<DC, DR>;
+  constexpr int BN = S::BN, DV = S::DV, NST = S::kStages;
+  constexpr int TR = kBM * CL / S::kSplit;  // rows of a CTA's, or a pair's, tile
+  constexpr uint16_t kPair = static_cast<uint16_t>((1u << CL) - 1u);
+  static_assert(S::kSplit == 1 || CL == S::kSplit, "split tiles take a pair");
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = align_smem_1024(smem_raw);
+  uint8_t* sQ = smem;
+  uint8_t* sKV = smem + S::kQBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sKV + NST * S::kTileBytes);
+  uint64_t* q_ready = bars;
+  uint64_t* kv_full = bars + 1;
+  uint64_t* kv_empty = kv_full + NST;
+  uint64_t* s_full = kv_empty + NST;
+  uint64_t* s_free = s_full + 1;
+  uint64_t* p_full = s_free + 1;
+  uint64_t* pv_done = p_full + 1;
+  uint64_t* mma_drain = pv_done + 1;  // [2]
+  long long* scratch = reinterpret_cast<long long*>(mma_drain + 2);  // [8]
+  Share* share = reinterpret_cast<Share*>(scratch + 8);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(share + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const WaitCtx wc{abort_flag, p.status};
+
+  if (threadIdx.x == 0) {
+    mbar_init(q_ready, kBM);
+    for (int s = 0; s < NST; ++s) {
+      mbar_init(&kv_full[s], 1);
+      mbar_init(&kv_empty[s], CL);
+    }
+    mbar_init(s_full, 1);
+    mbar_init(s_free, kBM);
+    mbar_init(p_full, kBM);
+    mbar_init(pv_done, 1);
+    mbar_init(&mma_drain[0], 1);
+    mbar_init(&mma_drain[1], 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tm_c);
+    tma_prefetch_desc(&tm_kr);
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, S::kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  // the peer's barriers must be initialised before any multicast lands
+  if constexpr (CL > 1) cluster_sync();
+  grid_dep_sync();
+  const int crank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  if (blockIdx.x == 0) {
+    check_q_start(p.q_start, p.seqs, p.total, p.status);
+    for (int s = threadIdx.x; s < p.seqs; s += kThreads) {
+      const int len = __ldg(p.lens + s);
+      if (len < 0 || len > static_cast<long long>(p.max_pages) * p.page_tokens)
+        record_status(p.status, MLA_ERR_RANGE);
+    }
+  }
+  if (threadIdx.x < 2) p.part_desc[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
+  find_share<BN, TR>(p, blockIdx.x / CL, gridDim.x / CL, scratch, share);
+  Walk<BN, TR> walk(p, *share);
+  Segment g;
+  bool ok = true;
+  int it = 0;  // key blocks so far: the phase of every per-block barrier
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ producer
+    while (ok && walk.next(g)) {
+      const int* row = p.table + static_cast<size_t>(g.s) * p.max_pages;
+      BlockPos<BN> pos(p, g.kb0);
+      for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, pos.step(p)) {
+        const int st = it % NST;
+        const int valid = min(pos.rows(p), g.st.len - pos.token(p));
+        const int boxes =
+            p.per_group == 1 ? (valid > 0) : (max(valid, 0) + p.page_tokens - 1) / p.page_tokens;
+        if (it >= NST) ok = mbar_wait(&kv_empty[st], ((it / NST) - 1) & 1, wc);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        uint8_t* kv = sKV + st * S::kTileBytes;
+        if (lane == 0) {
+          if (boxes)
+            mbar_arrive_expect_tx(&kv_full[st], boxes * p.box_rows * S::DK * 2);
+          else
+            mbar_arrive(&kv_full[st]);
+        }
+        __syncwarp();
+        for (int bx = lane; bx < boxes * S::kBoxes; bx += 32) {
+          if (CL > 1 && (bx & 1) != crank) continue;
+          const int i = bx / S::kBoxes, cb = bx - i * S::kBoxes;
+          const int page = __ldg(row + pos.grp * p.per_group + i);
+          int r = p.pages * p.page_tokens;  // past the pool: zeros
+          if (page >= 0 && page < p.pages)
+            r = page * p.page_tokens + pos.sub * BN;
+          else
+            record_status(p.status, MLA_ERR_RANGE);
+          const bool is_c = cb < DC / 64;
+          uint8_t* dst = is_c ? kv + cb * S::kCBox + i * p.box_rows * 128
+                              : kv + S::kKrOff + i * p.box_rows * static_cast<int>(S::kKrRow);
+          const CUtensorMap* map = is_c ? &tm_c : &tm_kr;
+          const int x = is_c ? cb * 64 : 0;
+          if constexpr (CL == 1)
+            tma_load_2d(dst, map, &kv_full[st], x, r);
+          else
+            tma_load_2d_mc(dst, map, &kv_full[st], x, r, kPair);
+        }
+      }
+    }
+    // every stage's last use must be released before the CTA may exit
+    for (int st = 0; st < NST && st < it && !*abort_flag; ++st)
+      mbar_wait(&kv_empty[st], (((it - st + NST - 1) / NST) - 1) & 1, wc);
+    if (*abort_flag)  // let every copy this CTA started land before exit
+      for (int u = it > NST ? it - NST : 0; u < it; ++u)
+        mbar_wait_drain(&kv_full[u % NST], (u / NST) & 1, p.status);
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---------------------------------------------------------- QK issuer
+    const uint32_t qa = smem_u32(sQ);
+    int seg = 0;
+    while (ok && walk.next(g)) {
+      ok = __all_sync(0xffffffffu, mbar_wait(q_ready, seg & 1, wc));
+      ++seg;
+      if (!ok) break;
+      BlockPos<BN> pos(p, g.kb0);
+      for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, pos.step(p)) {
+        const int st = it % NST;
+        // S's previous contents must have been read, and the keys have landed
+        if (it >= 1) ok = mbar_wait(s_free, (it - 1) & 1, wc);
+        ok = ok && mbar_wait(&kv_full[st], (it / NST) & 1, wc);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        uint8_t* kv = sKV + st * S::kTileBytes;
+        const int valid = max(0, min(pos.rows(p), g.st.len - pos.token(p)));
+        if (valid < BN) {
+          const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+          for (int cb = 0; cb < DC / 64; ++cb)
+            for (int i = valid * 8 + lane; i < BN * 8; i += 32)
+              *reinterpret_cast<uint4*>(kv + cb * S::kCBox + i * 16) = zero;
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        if (lane == 0) {
+          tc_fence_after();
+          const uint32_t ka = smem_u32(kv);
 #pragma unroll
-  for (int i = 0; i < kMaxDC / kThreads; ++i) {
-    const int col = threadIdx.x + i * kThreads;
-    if (col < p.d_c)
-      static_cast<__nv_bfloat16*>(p.o)[row * p.d_c + col] = __float2bfloat16_rn(o[i] * inv);
+          for (int cb = 0; cb < DC / 64; ++cb)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint64_t bd = sdesc(ka + cb * S::kCBox + k * 32, 16, 1024, kSw128);
+              const uint32_t acc = (cb | k) != 0 ? 1u : 0u;
+              if (cb < S::kQcTmem / 64)
+                umma_ts(tmem + S::kTmemS, tmem + S::kTmemQ + (cb * 4 + k) * 8, bd, S::kIdescQK,
+                        acc);
+              else
+                umma_ss(tmem + S::kTmemS,
+                        sdesc(qa + (cb - S::kQcTmem / 64) * 16384 + k * 32, 16, 1024, kSw128), bd,
+                        S::kIdescQK, acc);
+            }
+#pragma unroll
+          for (int k = 0; k < DR / 16; ++k) {
+            const uint64_t bd = sdesc(ka + S::kKrOff + k * 32, 16, S::kKrSbo, S::kKrSw);
+            if constexpr (S::kQinTmem)
+              umma_ts(tmem + S::kTmemS, tmem + S::kTmemQ + DC / 2 + k * 8, bd, S::kIdescQK, 1u);
+            else
+              umma_ss(tmem + S::kTmemS, sdesc(qa + S::kQKrOff + k * 32, 16, S::kKrSbo, S::kKrSw),
+                      bd, S::kIdescQK, 1u);
+          }
+          umma_commit(s_full);
+        }
+        __syncwarp();
+      }
+    }
+    if (!ok && lane == 0) {  // wait for every MMA issued before TMEM is freed
+      umma_commit(&mma_drain[0]);
+      mbar_wait_drain(&mma_drain[0], 0, p.status);
+    }
+    __syncwarp();
+  } else if (warp == 6) {
+    // ---------------------------------------------------------- PV issuer
+    if (lane == 0) {
+      const int vpart = S::kSplit > 1 ? crank : 0;
+      while (ok && walk.next(g)) {
+        for (int kb = g.kb0; kb < g.kb1; ++kb, ++it) {
+          ok = mbar_wait(p_full, it & 1, wc);
+          if (!ok) break;
+          tc_fence_after();
+          const int st = it % NST;
+          const uint32_t va = smem_u32(sKV) + st * S::kTileBytes + vpart * (DV / 64) * S::kCBox;
+#pragma unroll
+          for (int s = 0; s < BN / 16; ++s)
+            umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + s * 8,
+                    sdesc(va + s * 2048, S::kCBox, 1024, kSw128), S::kIdescPV,
+                    (kb > g.kb0 || s > 0) ? 1u : 0u);
+          if constexpr (CL == 1)
+            umma_commit(&kv_empty[st]);
+          else
+            umma_commit_mc(&kv_empty[st], kPair);
+          umma_commit(pv_done);
+        }
+      }
+      if (!ok) {
+        umma_commit(&mma_drain[1]);
+        mbar_wait_drain(&mma_drain[1], 0, p.status);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------ softmax (warps 2..5)
+    const int quarter = warp & 3;  // TMEM lane quarter this warp may access
+    const int r = quarter * 32 + lane;
+    const uint32_t t_lane = static_cast<uint32_t>(quarter * 32) << 16;
+    const int vpart = S::kSplit > 1 ? crank : 0;
+    while (ok && walk.next(g)) {
+      const int rows = g.st.n * p.heads;
+      const int tile0 = g.tile * TR + (S::kSplit == 1 ? crank * kBM : 0);
+      const int lrow = tile0 + r;
+      const bool row_ok = lrow < rows;
+      const bool warp_ok = __any_sync(0xffffffffu, row_ok);
+      const size_t grow = static_cast<size_t>(g.st.q0) * p.heads + (row_ok ? lrow : 0);
+      const int keys =
+          row_ok ? visible_keys(g.st.len - g.st.n + lrow / p.heads, g.st.len, p.block) : 0;
+
+      // Q. The previous segment's score MMAs are done: their last S was read.
+      if (warp_ok) {
+        const uint4* qc = reinterpret_cast<const uint4*>(p.q_c + grow * DC);
+        const uint4* qr = reinterpret_cast<const uint4*>(p.q_r + grow * DR);
+        if constexpr (S::kQcTmem > 0) {
+#pragma unroll
+          for (int c = 0; c < S::kQcTmem / 64; ++c) {
+            uint32_t w[32];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint4 v = row_ok ? __ldg(qc + c * 8 + i) : make_uint4(0u, 0u, 0u, 0u);
+              w[4 * i] = v.x;
+              w[4 * i + 1] = v.y;
+              w[4 * i + 2] = v.z;
+              w[4 * i + 3] = v.w;
+            }
+            tmem_st32(tmem + t_lane + S::kTmemQ + c * 32, w);
+          }
+        }
+        if constexpr (S::kQinTmem) {
+          uint32_t w[DR / 2];
+#pragma unroll
+          for (int i = 0; i < DR / 8; ++i) {
+            const uint4 v = row_ok ? __ldg(qr + i) : make_uint4(0u, 0u, 0u, 0u);
+            w[4 * i] = v.x;
+            w[4 * i + 1] = v.y;
+            w[4 * i + 2] = v.z;
+            w[4 * i + 3] = v.w;
+          }
+#pragma unroll
+          for (int c = 0; c < DR / 32; ++c)
+            tmem_st16(tmem + t_lane + S::kTmemQ + DC / 2 + c * 16, w + c * 16);
+        } else {
+          // the swizzle the MMA descriptors name: 16-byte pieces within a row
+#pragma unroll
+          for (int c = 0; c < S::kQcSmem / 64; ++c) {
+            uint8_t* dst = sQ + c * 16384 + r * 128;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              *reinterpret_cast<uint4*>(dst + ((i ^ (r & 7)) * 16)) =
+                  row_ok ? __ldg(qc + S::kQcTmem / 8 + c * 8 + i) : make_uint4(0u, 0u, 0u, 0u);
+          }
+          uint8_t* dst = sQ + S::kQKrOff + r * S::kKrRow;
+#pragma unroll
+          for (int i = 0; i < DR / 8; ++i) {
+            const int at = DR == 32 ? (i ^ ((r >> 1) & 3)) : (i ^ (r & 7));
+            *reinterpret_cast<uint4*>(dst + at * 16) =
+                row_ok ? __ldg(qr + i) : make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_smem();
+        }
+        if constexpr (S::kQcTmem > 0) tmem_wait_st();
+      }
+      tc_fence_before();
+      mbar_arrive(q_ready);
+
+      float m_run = -INFINITY, l_run = 0.f;
+      BlockPos<BN> pos(p, g.kb0);
+      for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, pos.step(p)) {
+        if (!mbar_wait(s_full, it & 1, wc)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        if (!warp_ok) {  // none of the warp's rows exists: keep the barriers going
+          mbar_arrive(s_free);
+          if (kb > g.kb0 && !mbar_wait(pv_done, (it - 1) & 1, wc)) {
+            ok = false;
+            break;
+          }
+          mbar_arrive(p_full);
+          continue;
+        }
+        uint32_t sr[BN];
+#pragma unroll
+        for (int c = 0; c < BN / 32; ++c)
+          tmem_ld32(tmem + t_lane + S::kTmemS + c * 32,
+                    *reinterpret_cast<uint32_t(*)[32]>(&sr[c * 32]));
+        tmem_wait_ld();
+        tc_fence_before();
+        mbar_arrive(s_free);  // the next block's scores may land
+        float sv[BN];
+#pragma unroll
+        for (int c = 0; c < BN; ++c) sv[c] = __uint_as_float(sr[c]);
+        const int valid = min(pos.rows(p), keys - pos.token(p));
+        if (valid < BN) {
+#pragma unroll
+          for (int c = 0; c < BN; ++c)
+            if (c >= valid) sv[c] = -INFINITY;
+        }
+        float m8[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m8[i] = sv[i];
+#pragma unroll
+        for (int c = 8; c + 16 <= BN; c += 16)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) m8[i] = fmax3(m8[i], sv[c + i], sv[c + 8 + i]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m8[i] = fmaxf(m8[i], sv[BN - 8 + i]);
+        const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
+                               fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7])));
+        const float m_blk = mx * p.scale_log2;
+        // The running maximum moves only when a block exceeds it by more than
+        // 2^8 (weights up to 256 are harmless in bf16 and fp32). A row that has
+        // seen no key yet has none; its weights are exp2(-inf) = 0.
+        float alpha = 1.f;
+        bool need = false;
+        if (kb == g.kb0) {
+          m_run = m_blk;
+        } else if (m_blk > m_run + kRescaleLog2) {
+          need = true;
+          alpha = ex2_approx(m_run - m_blk);
+          m_run = m_blk;
+        }
+        debug_count_rescale(need && row_ok, p.status);
+        l_run *= alpha;
+        const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
+        const uint64_t scale2 = f32x2_pack(p.scale_log2, p.scale_log2);
+        const uint64_t negm2 = f32x2_pack(neg_m, neg_m);
+        uint64_t l4[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l4[i] = 0ull;
+        uint32_t pk[BN / 2];
+#pragma unroll
+        for (int i = 0; i < BN / 2; ++i) {
+          float t0, t1;
+          f32x2_unpack(f32x2_fma(f32x2_pack(sv[2 * i], sv[2 * i + 1]), scale2, negm2), t0, t1);
+          const float p0 = ex2_approx(t0);
+          const float p1 = ex2_approx(t1);
+          l4[i & 3] = f32x2_add(l4[i & 3], f32x2_pack(p0, p1));
+          pk[i] = pack_bf16x2(p0, p1);
+        }
+        float l8[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f32x2_unpack(l4[i], l8[2 * i], l8[2 * i + 1]);
+        l_run += ((l8[0] + l8[1]) + (l8[2] + l8[3])) + ((l8[4] + l8[5]) + (l8[6] + l8[7]));
+        if (kb > g.kb0) {
+          // the previous PV has read P and finished with O
+          if (!mbar_wait(pv_done, (it - 1) & 1, wc)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          if (__any_sync(0xffffffffu, need)) {
+#pragma unroll 1
+            for (int c = 0; c < DV / 32; ++c) {
+              uint32_t ov[32];
+              tmem_ld32(tmem + t_lane + S::kTmemO + c * 32, ov);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                ov[i] = __float_as_uint(__uint_as_float(ov[i]) * alpha);
+              tmem_st32(tmem + t_lane + S::kTmemO + c * 32, ov);
+            }
+            tmem_wait_st();
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < BN / 64; ++c)
+          tmem_st32(tmem + t_lane + S::kTmemP + c * 32,
+                    *reinterpret_cast<uint32_t(*)[32]>(&pk[c * 32]));
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(p_full);
+      }
+
+      // O: finished rows as bf16, a cut tile's as fp32 partial rows
+      ok = ok && mbar_wait(pv_done, (it - 1) & 1, wc);
+      if (!ok) break;
+      tc_fence_after();
+      const bool whole = g.starts && g.ends;
+      const int slot = 2 * blockIdx.x + (g.starts ? 1 : 0);
+      if (warp_ok) {
+        // a row that saw no key is 0; a NaN sum stays one
+        const float inv_l = l_run == 0.f ? 0.f : 1.f / l_run;
+        const float f = whole ? inv_l : 1.f;
+#pragma unroll 1
+        for (int c = 0; c < DV / 32; ++c) {
+          uint32_t ov[32];
+          tmem_ld32(tmem + t_lane + S::kTmemO + c * 32, ov);
+          tmem_wait_ld();
+          if (row_ok && whole) {
+            uint4* dst = reinterpret_cast<uint4*>(p.o + grow * DC + vpart * DV + c * 32);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t w[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                w[k] = pack_bf16x2(__uint_as_float(ov[8 * i + 2 * k]) * f,
+                                   __uint_as_float(ov[8 * i + 2 * k + 1]) * f);
+              dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          } else if (row_ok) {
+            uint4* dst = reinterpret_cast<uint4*>(
+                p.part_o + (static_cast<size_t>(slot) * kBM + r) * DV + c * 32);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              dst[i] = make_uint4(ov[4 * i], ov[4 * i + 1], ov[4 * i + 2], ov[4 * i + 3]);
+          }
+          __syncwarp();  // the next TMEM load is the whole warp's
+        }
+        if (!whole && row_ok) p.part_ml[slot * kBM + r] = make_float2(m_run, l_run);
+        tc_fence_before();  // O was read before the next segment's first PV
+      }
+      if (!whole && r == 0) {
+        const int n_rows = max(0, min(kBM, rows - tile0));
+        p.part_desc[slot] = make_int4(g.st.q0 * p.heads + tile0, n_rows, g.ends ? 3 : 1, 0);
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, S::kTmemCols);
+  }
+  // neither CTA leaves while the other may still write into its shared memory
+  if constexpr (CL > 1) cluster_sync();
+}
+
+// Joins the partial rows of tiles that several shares cut: block (i, y) takes the
+// tile that CTA i begins and does not end. o = sum_k 2^(m_k - M) O_k over the
+// same of l_k, in the shares' order. Short chains: a warp per row; long ones (few
+// rows, long streams): all warps of the block on one row.
+template <int DC, int DV, int CL>
+__global__ void __launch_bounds__(kJoinThreads)
+    paged_join_kernel(const float* part_o, const float2* part_ml, const int4* part_desc,
+                      __nv_bfloat16* o, int ctas, long long out_rows) {
+  constexpr int kSplit = DC / DV, kWarps = kJoinThreads / 32, kV = DV / 32;
+  grid_dep_sync();
+  const int i = blockIdx.x;
+  const int4 d = part_desc[2 * i + 1];
+  if (!(d.z & 1)) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int vpart = kSplit > 1 ? i % CL : 0;
+  if (d.x < 0 || d.y > kBM || d.x + static_cast<long long>(d.y) > out_rows) return;
+  // the chain: this CTA's slot 1, then slot 0 of the CTAs after it in its place
+  // of their pairs, up to the one that ends the tile
+  int n = 1;
+  for (int k0 = 1; i + k0 * CL < ctas; k0 += 32) {
+    const int j = i + (k0 + lane) * CL;
+    const int f = j < ctas ? part_desc[2 * j].z : 0;
+    const unsigned stop = __ballot_sync(0xffffffffu, !(f & 1) || (f & 2));
+    if (stop) {
+      const int l = __ffs(stop) - 1;
+      n = k0 + l + (__shfl_sync(0xffffffffu, f, l) & 1);
+      break;
+    }
+    n = k0 + 32;
+  }
+  auto slot = [&](int k) { return k == 0 ? 2 * i + 1 : 2 * (i + k * CL); };
+  __shared__ float acc_s[kWarps][DV], l_s[kWarps];
+  const bool wide = n > 2 * kWarps;
+  const int step = wide ? kWarps : 1, k_first = wide ? warp : 0;
+  const int row_step = wide ? kJoinRows : kJoinRows * kWarps;
+  for (int row = wide ? blockIdx.y : blockIdx.y * kWarps + warp; row < d.y; row += row_step) {
+    float m = -INFINITY;
+    for (int k = lane; k < n; k += 32) m = fmaxf(m, part_ml[slot(k) * kBM + row].x);
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+    const float base = m == -INFINITY ? 0.f : m;
+    float acc[kV] = {}, l = 0.f;
+#pragma unroll 4
+    for (int k = k_first; k < n; k += step) {
+      const size_t at = static_cast<size_t>(slot(k)) * kBM + row;
+      const float2 ml = part_ml[at];
+      const float w = ex2_approx(ml.x - base);
+      l += w * ml.y;
+#pragma unroll
+      for (int c = 0; c < kV; ++c) acc[c] += w * part_o[at * DV + c * 32 + lane];
+    }
+    if (wide) {
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < kV; ++c) acc_s[warp][c * 32 + lane] = acc[c];
+      if (lane == 0) l_s[warp] = l;
+      __syncthreads();
+      for (int c = threadIdx.x; c < DV; c += kJoinThreads) {
+        float a = 0.f, t = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          a += acc_s[w][c];
+          t += l_s[w];
+        }
+        o[(static_cast<size_t>(d.x) + row) * DC + vpart * DV + c] =
+            __float2bfloat16_rn(t == 0.f ? 0.f : a / t);
+      }
+    } else {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int c = 0; c < kV; ++c)
+        o[(static_cast<size_t>(d.x) + row) * DC + vpart * DV + c * 32 + lane] =
+            __float2bfloat16_rn(acc[c] * inv);
+    }
+  }
+}
+
+template <int DC, int DR, int CL>
+int launch_paged(const PagedAttnArgs& a) {
+  using S = PagedShape<DC, DR>;
+  const bool divides = S::BN % a.page_tokens == 0;
+  PagedK k;
+  k.group = divides ? S::BN : a.page_tokens;
+  k.blocks = (k.group + S::BN - 1) / S::BN;
+  k.per_group = divides ? S::BN / a.page_tokens : 1;
+  k.box_rows = divides ? a.page_tokens : S::BN;
+  CUtensorMap tm_c, tm_kr;
+  const unsigned long long rows = static_cast<unsigned long long>(a.pages) * a.page_tokens;
+  if (!encode_map_2d_bf16(&tm_c, a.c, DC, rows, DC * 2ull, 64, k.box_rows,
+                          CU_TENSOR_MAP_SWIZZLE_128B) ||
+      !encode_map_2d_bf16(&tm_kr, a.kr, DR, rows, DR * 2ull, DR, k.box_rows,
+                          DR == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
+    return MLA_ERR_CUDA;
+  auto kern = paged_attn_kernel<DC, DR, CL>;
+  // resident CTAs of this instance (one per SM, whole clusters), asked once
+  static int resident = 0;
+  if (resident == 0) {
+    cudaError_t e =
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmemBytes);
+    int n = 0;
+    if (e == cudaSuccess) {
+      cudaLaunchConfig_t oc = {};
+      oc.gridDim = dim3(kMaxCtas / CL * CL);
+      oc.blockDim = dim3(kThreads);
+      oc.dynamicSmemBytes = S::kSmemBytes;
+      cudaLaunchAttribute at[1];
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = CL;
+      at[0].val.clusterDim.y = 1;
+      at[0].val.clusterDim.z = 1;
+      oc.attrs = at;
+      oc.numAttrs = 1;
+      e = cudaOccupancyMaxActiveClusters(&n, kern, &oc);
+    }
+    if (e != cudaSuccess || n < 1) {
+      (void)cudaGetLastError();
+      set_last_cuda_error(e);
+      return MLA_ERR_CUDA;
+    }
+    resident = n * CL < kMaxCtas ? n * CL : kMaxCtas / CL * CL;
+  }
+  k.q_c = static_cast<const __nv_bfloat16*>(a.q_c);
+  k.q_r = static_cast<const __nv_bfloat16*>(a.q_r);
+  k.q_start = a.q_start;
+  k.table = a.table;
+  k.lens = a.lens;
+  k.o = static_cast<__nv_bfloat16*>(a.o);
+  char* ws = static_cast<char*>(a.workspace);
+  k.part_o = reinterpret_cast<float*>(ws);
+  k.part_ml = reinterpret_cast<float2*>(ws + S::kPartBytes);
+  k.part_desc = reinterpret_cast<int4*>(ws + S::kPartBytes + S::kMlBytes);
+  k.total = a.total;
+  k.heads = a.heads;
+  k.seqs = a.seqs;
+  k.pages = a.pages;
+  k.page_tokens = a.page_tokens;
+  k.max_pages = a.max_pages;
+  k.block = a.causal_block;
+  k.scale_log2 = a.scale_log2;
+  k.status = a.status;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(resident);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = S::kSmemBytes;
+  cfg.stream = a.stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = CL;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see grid_dep_sync
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, tm_c, tm_kr, k);
+  if (e != cudaSuccess) {
+    (void)cudaGetLastError();
+    set_last_cuda_error(e);
+    return MLA_ERR_CUDA;
+  }
+  return launch_pdl(paged_join_kernel<DC, S::DV, CL>, dim3(resident, kJoinRows), kJoinThreads, 0,
+                    a.stream, k.part_o, k.part_ml, k.part_desc, k.o, resident,
+                    static_cast<long long>(a.total) * a.heads);
+}
+
+// Streams of two row tiles and more on average: CTA pairs, which read each key
+// tile from L2 once for 256 rows. Shorter ones would leave half a pair idle.
+template <int DC, int DR>
+int pick(const PagedAttnArgs& a) {
+  if constexpr (PagedShape<DC, DR>::kSplit == 2) {
+    return launch_paged<DC, DR, 2>(a);
+  } else {
+    return static_cast<long long>(a.total) * a.heads >= 2ll * kBM * a.seqs
+               ? launch_paged<DC, DR, 2>(a)
+               : launch_paged<DC, DR, 1>(a);
+  }
+}
+
+template <int DR>
+int pick_dc(const PagedAttnArgs& a) {
+  switch (a.d_c) {
+    case 64: return pick<64, DR>(a);
+    case 128: return pick<128, DR>(a);
+    case 192: return pick<192, DR>(a);
+    case 256: return pick<256, DR>(a);
+    case 512: return pick<512, DR>(a);
+    default: return MLA_ERR_UNSUPPORTED;
+  }
+}
+
+template <int DR>
+unsigned long long workspace_dc(int d_c) {
+  switch (d_c) {
+    case 64: return PagedShape<64, DR>::kWorkspace;
+    case 128: return PagedShape<128, DR>::kWorkspace;
+    case 192: return PagedShape<192, DR>::kWorkspace;
+    case 256: return PagedShape<256, DR>::kWorkspace;
+    case 512: return PagedShape<512, DR>::kWorkspace;
+    default: return 0;
   }
 }
 
 }  // namespace
 
 unsigned long long paged_attention_workspace(int d_c, int d_r) {
-  const bool ok = (d_c == 64 || d_c == 128 || d_c == 192 || d_c == 256 || d_c == 512) &&
-                  (d_r == 32 || d_r == 64);
-  return ok ? 16 : 0;
+  return d_r == 32 ? workspace_dc<32>(d_c) : (d_r == 64 ? workspace_dc<64>(d_c) : 0);
 }
 
 int launch_paged_attention(const PagedAttnArgs& a) {
-  return launch_pdl(paged_attn_simple_kernel, dim3(a.total * a.heads), kThreads, 0, a.stream, a);
+  return a.d_r == 32 ? pick_dc<32>(a) : pick_dc<64>(a);
 }
 
 }  // namespace vmla

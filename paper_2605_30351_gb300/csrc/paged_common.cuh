@@ -38,7 +38,7 @@ __device__ __forceinline__ void check_q_start(const int* q_start, int seqs, int 
 __device__ __forceinline__ int visible_keys(int a, int held, int block) {
   if (a < 0) return 0;
   if (block == 0) return held;
-  const long long end = (static_cast<long long>(a) / block + 1) * block;
+  const long long end = static_cast<long long>(a / block + 1) * block;
   return end < held ? static_cast<int>(end) : held;
 }
 
