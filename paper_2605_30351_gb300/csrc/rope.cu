@@ -5,7 +5,11 @@
 // -sin.
 //
 // Bound by memory: each value is read once and written once, the table's 8
-// bytes a (token, pair) are shared by all heads of a token.
+// bytes a (token, pair) are shared by all heads of a token. A thread takes one
+// 16-byte piece (half layout: the two pieces that pair up) of kHeads heads of a
+// token: its cosines and sines are fetched once for all of them, and kHeads
+// loads are in flight at once. Tensors whose rows or rotated part do not lie on
+// 16-byte boundaries take the kernel that moves single values.
 #include <cmath>
 
 #include <cuda_fp16.h>
@@ -50,7 +54,7 @@ __device__ __forceinline__ float2 pair_cs(const RopeK& p, long long t, int i) {
   return cs;
 }
 
-// One thread per (token, head, pair or copied channel).
+// Any strides and alignment: one thread per (token, head, pair or copied channel).
 template <typename T, bool HALF>
 __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeK p) {
   grid_dep_sync();
@@ -79,13 +83,109 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeK p) {
   }
 }
 
+constexpr int kHeads = 4;  // heads per thread of the 16-byte kernel
+
+// Unit of a head: a 16-byte piece, or in the half layout the two pieces that
+// pair up. Blocks take `tpb` tokens; rcp_* = ceil(2^32 / d) divide the block's
+// unit index (below 2^16).
+struct RopeV {
+  int units, groups, tpb;
+  unsigned rcp_units, rcp_groups;
+};
+
+template <typename T>
+struct Piece {
+  static constexpr int N = 16 / sizeof(T);
+  union {
+    uint4 v;
+    T e[N];
+  };
+  __device__ Piece() {}
+};
+
+template <typename T, bool HALF>
+__global__ void __launch_bounds__(kThreads) rope_vec_kernel(const RopeK p, const RopeV v) {
+  constexpr int N = 16 / sizeof(T);
+  constexpr int NP = HALF ? N : N / 2;  // pairs of a unit
+  grid_dep_sync();
+  const int o16 = p.offset / N, span = p.pairs / NP;  // the rotated units
+  const long long t0 = blockIdx.x * static_cast<long long>(v.tpb);
+  const int work = v.units * v.groups *
+                   static_cast<int>(min(static_cast<long long>(v.tpb), p.tokens - t0));
+  for (int k = threadIdx.x; k < work; k += kThreads) {
+    const int tg = v.units == 1 ? k : static_cast<int>(__umulhi(k, v.rcp_units));
+    const int tl = v.groups == 1 ? tg : static_cast<int>(__umulhi(tg, v.rcp_groups));
+    const int u = k - tg * v.units;
+    const int h0 = (tg - tl * v.groups) * kHeads, nh = min(kHeads, p.heads - h0);
+    const long long t = t0 + tl;
+    int piece = p.in_place ? o16 + u : u;
+    const bool turn = piece >= o16 && piece < o16 + span;
+    if (HALF && piece >= o16 + span) piece += span;
+    const T* x = static_cast<const T*>(p.x) + t * p.x_tok + h0 * p.x_head + piece * N;
+    T* y = static_cast<T*>(p.y) + t * p.y_tok + h0 * p.y_head + piece * N;
+    Piece<T> a[kHeads], b[kHeads];
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h)
+      if (h < nh) {
+        a[h].v = *reinterpret_cast<const uint4*>(x + h * p.x_head);
+        if (HALF && turn) b[h].v = *reinterpret_cast<const uint4*>(x + h * p.x_head + p.pairs);
+      }
+    if (turn) {
+      float2 cs[NP];
+      const int i0 = (piece - o16) * NP;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) cs[i] = pair_cs(p, t, i0 + i);
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          T& ea = HALF ? a[h].e[i] : a[h].e[2 * i];
+          T& eb = HALF ? b[h].e[i] : a[h].e[2 * i + 1];
+          const float fa = to_f(ea), fb = to_f(eb);
+          from_f(fa * cs[i].x - fb * cs[i].y, ea);
+          from_f(fa * cs[i].y + fb * cs[i].x, eb);
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h)
+      if (h < nh) {
+        *reinterpret_cast<uint4*>(y + h * p.y_head) = a[h].v;
+        if (HALF && turn) *reinterpret_cast<uint4*>(y + h * p.y_head + p.pairs) = b[h].v;
+      }
+  }
+}
+
+bool on_16(const RopeArgs& a, const RopeK& k, int size) {
+  const auto ok = [&](long long elems) { return elems * size % 16 == 0; };
+  return aligned_to(a.x, 16) && aligned_to(a.y, 16) && ok(a.x_tok) && ok(a.x_head) &&
+         ok(a.y_tok) && ok(a.y_head) && ok(a.offset) && (k.in_place || ok(a.head_dim)) &&
+         ok(a.layout == MLA_ROPE_HALF ? a.pairs : 2 * a.pairs);
+}
+
 template <typename T>
 int launch_typed(const RopeArgs& a, const RopeK& k) {
+  constexpr int N = 16 / sizeof(T);
+  const bool half = a.layout == MLA_ROPE_HALF;
+  if (on_16(a, k, sizeof(T))) {
+    RopeV v;
+    v.units = (k.in_place ? 2 * a.pairs : a.head_dim) / N - (half ? a.pairs / N : 0);
+    v.groups = (a.heads + kHeads - 1) / kHeads;
+    const long long per_token = static_cast<long long>(v.units) * v.groups;
+    if (per_token < 65536) {
+      v.tpb = per_token >= kThreads ? 1 : static_cast<int>(kThreads / per_token);
+      v.rcp_units = static_cast<unsigned>(((1ull << 32) + v.units - 1) / v.units);
+      v.rcp_groups = static_cast<unsigned>(((1ull << 32) + v.groups - 1) / v.groups);
+      const long long blocks = (a.tokens + v.tpb - 1) / v.tpb;
+      if (blocks < (1ll << 31))
+        return launch_pdl(half ? rope_vec_kernel<T, true> : rope_vec_kernel<T, false>,
+                          dim3(static_cast<unsigned>(blocks)), kThreads, 0, a.stream, k, v);
+    }
+  }
   const int items = a.pairs + (k.in_place ? 0 : a.head_dim - 2 * a.pairs);
   const long long n = a.tokens * a.heads * items;
   const long long want = (n + kThreads - 1) / kThreads;
   const int blocks = static_cast<int>(want < 152 * 16 ? want : 152 * 16);
-  return launch_pdl(a.layout == MLA_ROPE_HALF ? rope_kernel<T, true> : rope_kernel<T, false>,
+  return launch_pdl(half ? rope_kernel<T, true> : rope_kernel<T, false>,
                     dim3(blocks), kThreads, 0, a.stream, k);
 }
 
