@@ -10,10 +10,10 @@
 //     O += P . c                       N = d_c, c read again from the same tile
 //
 // Work is split evenly whatever the streams look like: all (row tile, key block)
-// pairs of the call form one sequence, and each CTA (or pair of CTAs) takes an
-// equal share of consecutive pairs. A chunk of thousands of tokens, one token of
-// one long stream and hundreds of ragged streams run on the same grid of one CTA
-// per SM. A row tile that lies in one share is finished there; one that several
+// pairs of the call form one sequence, and each CTA (or pair of CTAs) takes a
+// share of consecutive pairs of equal cost. A chunk of thousands of tokens, one
+// token of one long stream and hundreds of ragged streams run on the same grid of
+// one CTA per SM. A row tile that lies in one share is finished there; one that several
 // shares cut writes unnormalised fp32 partial rows with their maximum and sum to
 // the workspace, and paged_join_kernel adds them up in order. The shares depend
 // on q_start and lens only, which every CTA reads for itself: no plan kernel, no
@@ -41,8 +41,10 @@ constexpr int kBM = 128;       // rows per tile = TMEM lanes
 constexpr int kThreads = 224;  // 7 warps
 constexpr float kRescaleLog2 = 8.0f;
 constexpr int kMaxCtas = 152;  // the workspace holds two partial tiles for each
-constexpr int kJoinThreads = 256;
-constexpr int kJoinRows = 16;  // row groups of a joined tile
+constexpr int kJoinThreads = 512;
+constexpr int kJoinGrid = 2 * kMaxCtas;
+constexpr int kJoinCols = 16;      // columns of a warp's join item (of 32 rows)
+constexpr int kJoinLongRows = 2;   // rows of a block's item where many shares cut the tile
 
 template <int DC, int DR>
 struct PagedShape {
@@ -96,7 +98,7 @@ struct PagedK {
   __nv_bfloat16* o;
   float* part_o;
   float2* part_ml;
-  int4* part_desc;  // first row in o, rows, 1 = ends its tile, -
+  int4* part_desc;  // first row in o, rows, kPart*, 1 = many shares cut the tile
   int total, heads, seqs, pages, page_tokens, max_pages, block;
   // Key blocks never straddle a group of `group` tokens: BN tokens (per_group
   // whole pages) where the pages divide a block, else one page.
@@ -105,6 +107,10 @@ struct PagedK {
   float scale_log2;
   int* status;
 };
+
+// part_desc.z: the slot holds a partial tile, that ends its tile; the CTA's share
+// is empty (a chain of partial tiles passes over it)
+constexpr int kPartHeld = 1, kPartEnds = 2, kPartEmpty = 4;
 
 struct Stream {
   int q0, n, len;
@@ -130,55 +136,60 @@ __device__ __forceinline__ int tile_blocks(const PagedK& p, int n, int len, int 
   return max(1, whole * p.blocks + (rest + BN - 1) / BN);
 }
 
-__device__ __forceinline__ long long warp_total(long long v) {
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-  return v;
-}
+// Cost of a stream's row tiles in keys, as a straight line from the first to the
+// last tile's keys (exact for a whole chunk and token by token, and within a
+// mask block for others) plus kTileCost for loading Q and writing O: prefix sums
+// in closed form, so a share's ends are found without walking the tiles.
+constexpr int kTileCost = 256;
 
-// All key blocks of a stream; the whole warp calls it with its lanes' streams.
-template <int BN, int TR>
-__device__ __forceinline__ long long stream_blocks(const PagedK& p, const Stream& st) {
-  const int lane = threadIdx.x & 31;
-  const int tiles = (st.n * p.heads + TR - 1) / TR;
-  long long u = 0;
-  if (tiles <= 2)
-    for (int t = 0; t < tiles; ++t) u += tile_blocks<BN, TR>(p, st.n, st.len, t);
-  unsigned many = __ballot_sync(0xffffffffu, tiles > 2);
-  while (many) {
-    const int l = __ffs(many) - 1;
-    many &= many - 1;
-    const int n = __shfl_sync(0xffffffffu, st.n, l), len = __shfl_sync(0xffffffffu, st.len, l);
-    const int ts = __shfl_sync(0xffffffffu, tiles, l);
-    long long a = 0;
-    for (int t = lane; t < ts; t += 32) a += tile_blocks<BN, TR>(p, n, len, t);
-    a = warp_total(a);
-    if (lane == l) u = a;
+struct Cost {
+  long long first, slope;  // slope in 1/256 keys per tile
+  int tiles;
+  __device__ long long before(int t) const {  // of tiles 0 .. t-1
+    return t * first + ((slope * (static_cast<long long>(t) * (t - 1) / 2)) >> 8);
   }
-  return u;
-}
-
-struct Share {
-  int s, tile, off;  // first stream, row tile and key block
-  int pad;
-  long long count;   // key blocks
 };
 
-// Share `id` of `groups`: every thread of the block calls it. scratch: 8 long
-// longs, out: in shared memory.
+template <int TR>
+__device__ __forceinline__ Cost cost_of(const PagedK& p, const Stream& st) {
+  Cost c{0, 0, 0};
+  if (st.n == 0) return c;
+  const int rows = st.n * p.heads;
+  c.tiles = (rows + TR - 1) / TR;
+  const int k1 = visible_keys(st.len - 1, st.len, p.block);
+  c.first = k1 + kTileCost;
+  if (c.tiles > 1) {
+    const int k0 = visible_keys(st.len - st.n + (TR - 1) / p.heads, st.len, p.block);
+    if (c.tiles <= 4096) {  // the products stay below 2^63
+      c.first = k0 + kTileCost;
+      c.slope = static_cast<long long>(__fdividef((k1 - k0) * 256.f, c.tiles - 1.f));
+    } else {
+      c.first = (static_cast<long long>(k0) + k1) / 2 + kTileCost;
+    }
+  }
+  return c;
+}
+
+struct Place {
+  int s, tile, off;  // stream, row tile, key block
+};
+
+// The shares' ends: place of share id's first block and of the one after its
+// last. Every thread of the block calls it; scratch: 8 long longs and out: two
+// Places in shared memory. Returns the cost of a share.
 template <int BN, int TR>
-__device__ __forceinline__ void find_share(const PagedK& p, int id, int groups,
-                                           long long* scratch, Share* out) {
+__device__ __forceinline__ long long find_share(const PagedK& p, int id, int groups,
+                                                long long* scratch, Place* out) {
   constexpr int kWarps = kThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per = (p.seqs + kThreads - 1) / kThreads;
+  const int s0 = threadIdx.x * per;
   long long mine = 0;
-  for (int k = 0; k < per; ++k) {
-    const int s = threadIdx.x * per + k;
-    Stream st{0, 0, 0};
-    if (s < p.seqs) st = stream_at(p, s);
-    mine += stream_blocks<BN, TR>(p, st);
-  }
+  for (int k = 0; k < per; ++k)
+    if (s0 + k < p.seqs) {
+      const Cost c = cost_of<TR>(p, stream_at(p, s0 + k));
+      mine += c.before(c.tiles);
+    }
   long long x = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -186,7 +197,7 @@ __device__ __forceinline__ void find_share(const PagedK& p, int id, int groups,
     if (lane >= d) x += y;
   }
   if (lane == 31) scratch[warp] = x;
-  if (threadIdx.x == 0) out->count = 0;
+  if (threadIdx.x < 2) out[threadIdx.x] = Place{p.seqs, 0, 0};  // the end of the work
   __syncthreads();
   long long total = 0, base = x - mine;
 #pragma unroll
@@ -194,47 +205,49 @@ __device__ __forceinline__ void find_share(const PagedK& p, int id, int groups,
     if (w < warp) base += scratch[w];
     total += scratch[w];
   }
-  const long long active = min(static_cast<long long>(groups), total);
+  const int active = static_cast<int>(min(static_cast<long long>(groups), (total + BN - 1) / BN));
   if (id < active) {
-    const long long u0 = total * id / active, u1 = total * (id + 1) / active;
-    const unsigned owner = __ballot_sync(0xffffffffu, base <= u0 && u0 < base + mine);
-    if (owner) {  // this warp walks the streams of that lane
-      const int l = __ffs(owner) - 1;
-      long long rem = u0 - __shfl_sync(0xffffffffu, base, l);
-      int s = (warp * 32 + l) * per;
-      Stream st{0, 0, 0};
-      for (; s < p.seqs; ++s) {
-        st = stream_at(p, s);
-        const Stream one = lane == 0 ? st : Stream{0, 0, 0};
-        const long long u =
-            __shfl_sync(0xffffffffu, stream_blocks<BN, TR>(p, one), 0);
-        if (rem < u) break;
-        rem -= u;
+#pragma unroll 1
+    for (int e = 0; e < 2; ++e) {
+      // total * (id + e) / active: in 32 bits where it fits (a 64-bit division
+      // costs a tenth of a short call), else without the product's overflow
+      long long u;
+      if (total < (1 << 24)) {
+        u = static_cast<unsigned>(total) * (id + e) / static_cast<unsigned>(active);
+      } else {
+        const long long q = total / active, r = total - q * active;
+        u = q * (id + e) + r * (id + e) / active;
       }
-      const int tiles = (st.n * p.heads + TR - 1) / TR;
-      for (int t0 = 0; t0 < tiles; t0 += 32) {
-        const int v = t0 + lane < tiles ? tile_blocks<BN, TR>(p, st.n, st.len, t0 + lane) : 0;
-        long long y = v;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const long long z = __shfl_up_sync(0xffffffffu, y, d);
-          if (lane >= d) y += z;
+      if (u < base || u >= base + mine) continue;
+      long long rem = u - base;
+      for (int s = s0; s < min(s0 + per, p.seqs); ++s) {
+        const Stream st = stream_at(p, s);
+        const Cost c = cost_of<TR>(p, st);
+        const long long all = c.before(c.tiles);
+        if (rem >= all) {
+          rem -= all;
+          continue;
         }
-        const long long sum = __shfl_sync(0xffffffffu, y, 31);
-        if (rem < sum) {
-          if (rem < y && rem >= y - v) {
-            out->s = s;
-            out->tile = t0 + lane;
-            out->off = static_cast<int>(rem - (y - v));
-            out->count = u1 - u0;
-          }
-          break;
+        int lo = 0, hi = c.tiles - 1;  // the last tile that begins at or before rem
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) / 2;
+          if (c.before(mid) <= rem)
+            lo = mid;
+          else
+            hi = mid - 1;
         }
-        rem -= sum;
+        const long long at = c.before(lo);
+        const int blocks = tile_blocks<BN, TR>(p, st.n, st.len, lo);
+        const int off = static_cast<int>(
+            static_cast<float>(rem - at) *
+            __fdividef(static_cast<float>(blocks), static_cast<float>(c.before(lo + 1) - at)));
+        out[e] = Place{s, lo, min(off, blocks - 1)};
+        break;
       }
     }
   }
   __syncthreads();
+  return active > 0 ? static_cast<long long>(__fdividef(static_cast<float>(total), active)) : 0;
 }
 
 // Walks a share segment by segment: a segment is a run of key blocks of one row
@@ -242,39 +255,34 @@ __device__ __forceinline__ void find_share(const PagedK& p, int id, int groups,
 struct Segment {
   Stream st;
   int s, tile;
-  int kb0, kb1;        // key blocks [kb0, kb1)
-  bool starts, ends;   // the tile's first, last block is in it
+  int kb0, kb1, all;   // key blocks [kb0, kb1) of the tile's `all`
 };
 
 template <int BN, int TR>
 struct Walk {
   const PagedK& p;
   Stream st;
-  int s, tile, off;
-  long long left;
-  __device__ Walk(const PagedK& k, const Share& sh)
-      : p(k), s(sh.s), tile(sh.tile), off(sh.off), left(sh.count) {
-    if (left > 0) st = stream_at(p, s);
+  Place at, end;
+  __device__ Walk(const PagedK& k, const Place* ends) : p(k), at(ends[0]), end(ends[1]) {
+    st = at.s < p.seqs ? stream_at(p, at.s) : Stream{0, 0, 0};
   }
   __device__ bool next(Segment& g) {
-    if (left <= 0) return false;
-    while (tile * TR >= st.n * p.heads) {  // the next stream with new tokens
-      if (++s >= p.seqs) return false;
-      st = stream_at(p, s);
-      tile = 0;
+    while (at.s < p.seqs && at.tile * TR >= st.n * p.heads) {  // a stream with new tokens
+      at = Place{at.s + 1, 0, 0};
+      if (at.s < p.seqs) st = stream_at(p, at.s);
     }
-    const int all = tile_blocks<BN, TR>(p, st.n, st.len, tile);
-    const int take = static_cast<int>(min(static_cast<long long>(all - off), left));
+    if (at.s >= p.seqs || at.s > end.s) return false;
+    const bool last = at.s == end.s && at.tile == end.tile;
+    if (at.s == end.s && (at.tile > end.tile || (last && at.off >= end.off))) return false;
+    const int all = tile_blocks<BN, TR>(p, st.n, st.len, at.tile);
     g.st = st;
-    g.s = s;
-    g.tile = tile;
-    g.kb0 = off;
-    g.kb1 = off + take;
-    g.starts = off == 0;
-    g.ends = g.kb1 == all;
-    left -= take;
-    off = 0;
-    ++tile;
+    g.s = at.s;
+    g.tile = at.tile;
+    g.kb0 = at.off;
+    g.kb1 = last ? end.off : all;
+    g.all = all;
+    at.off = 0;
+    ++at.tile;
     return true;
   }
 };
@@ -317,8 +325,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* pv_done = p_full + 1;
   uint64_t* mma_drain = pv_done + 1;  // [2]
   long long* scratch = reinterpret_cast<long long*>(mma_drain + 2);  // [8]
-  Share* share = reinterpret_cast<Share*>(scratch + 8);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(share + 1);
+  Place* ends = reinterpret_cast<Place*>(scratch + 8);               // [2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ends + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5;
@@ -363,8 +371,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   if (threadIdx.x < 2) p.part_desc[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
-  find_share<BN, TR>(p, blockIdx.x / CL, gridDim.x / CL, scratch, share);
-  Walk<BN, TR> walk(p, *share);
+  const long long share =
+      find_share<BN, TR>(p, blockIdx.x / CL, gridDim.x / CL, scratch, ends);
+  Walk<BN, TR> walk(p, ends);
   Segment g;
   bool ok = true;
   int it = 0;  // key blocks so far: the phase of every per-block barrier
@@ -515,64 +524,72 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int r = quarter * 32 + lane;
     const uint32_t t_lane = static_cast<uint32_t>(quarter * 32) << 16;
     const int vpart = S::kSplit > 1 ? crank : 0;
-    while (ok && walk.next(g)) {
-      const int rows = g.st.n * p.heads;
-      const int tile0 = g.tile * TR + (S::kSplit == 1 ? crank * kBM : 0);
-      const int lrow = tile0 + r;
-      const bool row_ok = lrow < rows;
-      const bool warp_ok = __any_sync(0xffffffffu, row_ok);
-      const size_t grow = static_cast<size_t>(g.st.q0) * p.heads + (row_ok ? lrow : 0);
-      const int keys =
-          row_ok ? visible_keys(g.st.len - g.st.n + lrow / p.heads, g.st.len, p.block) : 0;
-
-      // Q. The previous segment's score MMAs are done: their last S was read.
-      if (warp_ok) {
-        const uint4* qc = reinterpret_cast<const uint4*>(p.q_c + grow * DC);
-        const uint4* qr = reinterpret_cast<const uint4*>(p.q_r + grow * DR);
-        if constexpr (S::kQcTmem > 0) {
+    struct Row {
+      int tile0, lrow, keys;  // the CTA's first row, this thread's, the keys it sees
+      size_t grow;            // its place in q and o
+      bool ok, warp_ok;       // the row exists; one of the warp's does
+    };
+    // The thread's row of a segment, and its Q: into TMEM (row-major, two values
+    // a column) and shared memory (the swizzle the MMA descriptors name). The
+    // score MMAs that read the previous Q are done: their last S was read.
+    auto load_row = [&](const Segment& sg) {
+      Row w;
+      const int rows = sg.st.n * p.heads;
+      w.tile0 = sg.tile * TR + (S::kSplit == 1 ? crank * kBM : 0);
+      w.lrow = w.tile0 + r;
+      w.ok = w.lrow < rows;
+      w.warp_ok = __any_sync(0xffffffffu, w.ok);
+      w.grow = static_cast<size_t>(sg.st.q0) * p.heads + (w.ok ? w.lrow : 0);
+      w.keys = w.ok ? visible_keys(sg.st.len - sg.st.n + w.lrow / p.heads, sg.st.len, p.block)
+                    : 0;
+      if (w.warp_ok) {
+        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+        const uint4* qc = reinterpret_cast<const uint4*>(p.q_c + w.grow * DC);
+        const uint4* qr = reinterpret_cast<const uint4*>(p.q_r + w.grow * DR);
+        // all loads of the row before the first store, up to 32 in flight
+        constexpr int kTm = S::kQcTmem / 8, kRr = DR / 8;
+        uint4 v[kTm + kRr + 1];
 #pragma unroll
-          for (int c = 0; c < S::kQcTmem / 64; ++c) {
-            uint32_t w[32];
+        for (int i = 0; i < kTm; ++i) v[i] = w.ok ? __ldg(qc + i) : zero;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint4 v = row_ok ? __ldg(qc + c * 8 + i) : make_uint4(0u, 0u, 0u, 0u);
-              w[4 * i] = v.x;
-              w[4 * i + 1] = v.y;
-              w[4 * i + 2] = v.z;
-              w[4 * i + 3] = v.w;
-            }
-            tmem_st32(tmem + t_lane + S::kTmemQ + c * 32, w);
+        for (int i = 0; i < kRr; ++i) v[kTm + i] = w.ok ? __ldg(qr + i) : zero;
+        if constexpr (S::kQcSmem > 0) {
+#pragma unroll 1
+          for (int c = 0; c < S::kQcSmem / 128; ++c) {
+            uint4 u[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              u[i] = w.ok ? __ldg(qc + kTm + c * 16 + i) : zero;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              *reinterpret_cast<uint4*>(sQ + (2 * c + i / 8) * 16384 + r * 128 +
+                                        (((i % 8) ^ (r & 7)) * 16)) = u[i];
           }
-        }
-        if constexpr (S::kQinTmem) {
-          uint32_t w[DR / 2];
-#pragma unroll
-          for (int i = 0; i < DR / 8; ++i) {
-            const uint4 v = row_ok ? __ldg(qr + i) : make_uint4(0u, 0u, 0u, 0u);
-            w[4 * i] = v.x;
-            w[4 * i + 1] = v.y;
-            w[4 * i + 2] = v.z;
-            w[4 * i + 3] = v.w;
-          }
-#pragma unroll
-          for (int c = 0; c < DR / 32; ++c)
-            tmem_st16(tmem + t_lane + S::kTmemQ + DC / 2 + c * 16, w + c * 16);
-        } else {
-          // the swizzle the MMA descriptors name: 16-byte pieces within a row
-#pragma unroll
-          for (int c = 0; c < S::kQcSmem / 64; ++c) {
-            uint8_t* dst = sQ + c * 16384 + r * 128;
+          if constexpr (S::kQcSmem % 128 != 0) {
+            constexpr int c = S::kQcSmem / 64 - 1;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              *reinterpret_cast<uint4*>(dst + ((i ^ (r & 7)) * 16)) =
-                  row_ok ? __ldg(qc + S::kQcTmem / 8 + c * 8 + i) : make_uint4(0u, 0u, 0u, 0u);
+              *reinterpret_cast<uint4*>(sQ + c * 16384 + r * 128 + ((i ^ (r & 7)) * 16)) =
+                  w.ok ? __ldg(qc + kTm + c * 8 + i) : zero;
           }
+        }
+        if constexpr (S::kQcTmem > 0) {
+#pragma unroll
+          for (int c = 0; c < S::kQcTmem / 32; ++c)
+            tmem_st16(tmem + t_lane + S::kTmemQ + c * 16,
+                      reinterpret_cast<const uint32_t*>(&v[4 * c]));
+        }
+        if constexpr (S::kQinTmem) {
+#pragma unroll
+          for (int c = 0; c < DR / 32; ++c)
+            tmem_st16(tmem + t_lane + S::kTmemQ + DC / 2 + c * 16,
+                      reinterpret_cast<const uint32_t*>(&v[kTm + 4 * c]));
+        } else {
           uint8_t* dst = sQ + S::kQKrOff + r * S::kKrRow;
 #pragma unroll
-          for (int i = 0; i < DR / 8; ++i) {
+          for (int i = 0; i < kRr; ++i) {
             const int at = DR == 32 ? (i ^ ((r >> 1) & 3)) : (i ^ (r & 7));
-            *reinterpret_cast<uint4*>(dst + at * 16) =
-                row_ok ? __ldg(qr + i) : make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(dst + at * 16) = v[kTm + i];
           }
           fence_proxy_async_smem();
         }
@@ -580,7 +597,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       tc_fence_before();
       mbar_arrive(q_ready);
-
+      return w;
+    };
+    bool have = walk.next(g);
+    if (!have && r == 0) p.part_desc[2 * blockIdx.x] = make_int4(0, 0, kPartEmpty, 0);
+    Row w{};
+    if (have) w = load_row(g);
+    while (have) {
       float m_run = -INFINITY, l_run = 0.f;
       BlockPos<BN> pos(p, g.kb0);
       for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, pos.step(p)) {
@@ -589,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           break;
         }
         tc_fence_after();
-        if (!warp_ok) {  // none of the warp's rows exists: keep the barriers going
+        if (!w.warp_ok) {  // none of the warp's rows exists: keep the barriers going
           mbar_arrive(s_free);
           if (kb > g.kb0 && !mbar_wait(pv_done, (it - 1) & 1, wc)) {
             ok = false;
@@ -609,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float sv[BN];
 #pragma unroll
         for (int c = 0; c < BN; ++c) sv[c] = __uint_as_float(sr[c]);
-        const int valid = min(pos.rows(p), keys - pos.token(p));
+        const int valid = min(pos.rows(p), w.keys - pos.token(p));
         if (valid < BN) {
 #pragma unroll
           for (int c = 0; c < BN; ++c)
@@ -639,7 +662,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           alpha = ex2_approx(m_run - m_blk);
           m_run = m_blk;
         }
-        debug_count_rescale(need && row_ok, p.status);
+        debug_count_rescale(need && w.ok, p.status);
         l_run *= alpha;
         const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
         const uint64_t scale2 = f32x2_pack(p.scale_log2, p.scale_log2);
@@ -691,48 +714,62 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_arrive(p_full);
       }
 
-      // O: finished rows as bf16, a cut tile's as fp32 partial rows
-      ok = ok && mbar_wait(pv_done, (it - 1) & 1, wc);
       if (!ok) break;
+      // The next segment's Q first, so that its scores are computed while this
+      // one's O is written.
+      const Row d = w;
+      const bool starts = g.kb0 == 0, stops = g.kb1 == g.all, whole = starts && stops;
+      const int n_rows = max(0, min(kBM, g.st.n * p.heads - d.tile0));
+      const int row0 = g.st.q0 * p.heads + d.tile0;
+      const bool many = static_cast<long long>(g.all - g.kb1) * BN > 8 * share;
+      have = walk.next(g);
+      if (have) w = load_row(g);
+      // O: finished rows as bf16, a cut tile's as fp32 partial rows, stored as
+      // [4 columns][rows] so that a warp's stores are contiguous
+      if (!mbar_wait(pv_done, (it - 1) & 1, wc)) {
+        ok = false;
+        break;
+      }
       tc_fence_after();
-      const bool whole = g.starts && g.ends;
-      const int slot = 2 * blockIdx.x + (g.starts ? 1 : 0);
-      if (warp_ok) {
+      const int slot = 2 * blockIdx.x + (starts ? 1 : 0);
+      if (d.warp_ok) {
         // a row that saw no key is 0; a NaN sum stays one
-        const float inv_l = l_run == 0.f ? 0.f : 1.f / l_run;
-        const float f = whole ? inv_l : 1.f;
+        const float f = l_run == 0.f ? 0.f : 1.f / l_run;
+        float4* part = reinterpret_cast<float4*>(p.part_o) +
+                       (static_cast<size_t>(slot) * (DV / 4)) * kBM + r;
+        uint4* dst = reinterpret_cast<uint4*>(p.o + d.grow * DC + vpart * DV);
 #pragma unroll 1
-        for (int c = 0; c < DV / 32; ++c) {
-          uint32_t ov[32];
-          tmem_ld32(tmem + t_lane + S::kTmemO + c * 32, ov);
+        for (int c = 0; c < DV / 64; ++c) {
+          uint32_t ov[64];
+          tmem_ld32(tmem + t_lane + S::kTmemO + c * 64, *reinterpret_cast<uint32_t(*)[32]>(ov));
+          tmem_ld32(tmem + t_lane + S::kTmemO + c * 64 + 32,
+                    *reinterpret_cast<uint32_t(*)[32]>(ov + 32));
           tmem_wait_ld();
-          if (row_ok && whole) {
-            uint4* dst = reinterpret_cast<uint4*>(p.o + grow * DC + vpart * DV + c * 32);
+          if (d.ok && whole) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t w[4];
+            for (int i = 0; i < 8; ++i) {
+              uint32_t x[4];
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                w[k] = pack_bf16x2(__uint_as_float(ov[8 * i + 2 * k]) * f,
+                x[k] = pack_bf16x2(__uint_as_float(ov[8 * i + 2 * k]) * f,
                                    __uint_as_float(ov[8 * i + 2 * k + 1]) * f);
-              dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+              dst[c * 8 + i] = make_uint4(x[0], x[1], x[2], x[3]);
             }
-          } else if (row_ok) {
-            uint4* dst = reinterpret_cast<uint4*>(
-                p.part_o + (static_cast<size_t>(slot) * kBM + r) * DV + c * 32);
+          } else if (d.ok) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              dst[i] = make_uint4(ov[4 * i], ov[4 * i + 1], ov[4 * i + 2], ov[4 * i + 3]);
+            for (int i = 0; i < 16; ++i)
+              part[(c * 16 + i) * kBM] =
+                  make_float4(__uint_as_float(ov[4 * i]), __uint_as_float(ov[4 * i + 1]),
+                              __uint_as_float(ov[4 * i + 2]), __uint_as_float(ov[4 * i + 3]));
           }
           __syncwarp();  // the next TMEM load is the whole warp's
         }
-        if (!whole && row_ok) p.part_ml[slot * kBM + r] = make_float2(m_run, l_run);
+        if (!whole && d.ok) p.part_ml[slot * kBM + r] = make_float2(m_run, l_run);
         tc_fence_before();  // O was read before the next segment's first PV
       }
-      if (!whole && r == 0) {
-        const int n_rows = max(0, min(kBM, rows - tile0));
-        p.part_desc[slot] = make_int4(g.st.q0 * p.heads + tile0, n_rows, g.ends ? 3 : 1, 0);
-      }
+      if (!whole && r == 0)
+        p.part_desc[slot] =
+            make_int4(row0, n_rows, kPartHeld | (stops ? kPartEnds : 0), many ? 1 : 0);
     }
   }
 
@@ -746,80 +783,194 @@ __global__ void __launch_bounds__(kThreads, 1)
   if constexpr (CL > 1) cluster_sync();
 }
 
-// Joins the partial rows of tiles that several shares cut: block (i, y) takes the
-// tile that CTA i begins and does not end. o = sum_k 2^(m_k - M) O_k over the
-// same of l_k, in the shares' order. Short chains: a warp per row; long ones (few
-// rows, long streams): all warps of the block on one row.
+// Joins the partial rows of tiles that several shares cut: o = sum_k 2^(m_k - M)
+// O_k over the same of l_k, in the shares' order. Every block finds the list of
+// work for itself: tiles that some CTA begins and does not end. Usually few shares
+// cut a tile, and a warp takes 32 rows x 16 columns of it, a lane per row. Where
+// many do (few rows, long streams: flagged by the CTA that begins the tile) a block
+// takes two rows and its threads split the chain.
 template <int DC, int DV, int CL>
 __global__ void __launch_bounds__(kJoinThreads)
     paged_join_kernel(const float* part_o, const float2* part_ml, const int4* part_desc,
                       __nv_bfloat16* o, int ctas, long long out_rows) {
-  constexpr int kSplit = DC / DV, kWarps = kJoinThreads / 32, kV = DV / 32;
+  constexpr int kSplit = DC / DV, kWarps = kJoinThreads / 32, kCg = DV / 4;
+  constexpr int kGroups = DV / kJoinCols;
+  __shared__ int4 desc[kMaxCtas];  // slots 1: tiles that begin
+  __shared__ int flags[kMaxCtas];  // slots 0: what follows
+  // prefix sums of the work: warps' items in the low half, blocks' in the high one
+  __shared__ int items[kMaxCtas + 1];
+  __shared__ int sums[8];
+  __shared__ float weight[kMaxCtas * kJoinLongRows], norm[kJoinLongRows];
+  __shared__ float4 red[kJoinThreads];
   grid_dep_sync();
-  const int i = blockIdx.x;
-  const int4 d = part_desc[2 * i + 1];
-  if (!(d.z & 1)) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int vpart = kSplit > 1 ? i % CL : 0;
-  if (d.x < 0 || d.y > kBM || d.x + static_cast<long long>(d.y) > out_rows) return;
-  // the chain: this CTA's slot 1, then slot 0 of the CTAs after it in its place
-  // of their pairs, up to the one that ends the tile
-  int n = 1;
-  for (int k0 = 1; i + k0 * CL < ctas; k0 += 32) {
-    const int j = i + (k0 + lane) * CL;
-    const int f = j < ctas ? part_desc[2 * j].z : 0;
-    const unsigned stop = __ballot_sync(0xffffffffu, !(f & 1) || (f & 2));
-    if (stop) {
-      const int l = __ffs(stop) - 1;
-      n = k0 + l + (__shfl_sync(0xffffffffu, f, l) & 1);
-      break;
-    }
-    n = k0 + 32;
+  int cnt = 0;
+  if (threadIdx.x < ctas) {
+    const int4 d = part_desc[2 * threadIdx.x + 1];
+    flags[threadIdx.x] = part_desc[2 * threadIdx.x].z;
+    desc[threadIdx.x] = d;
+    if ((d.z & kPartHeld) && d.x >= 0 && d.y > 0 && d.y <= kBM &&
+        d.x + static_cast<long long>(d.y) <= out_rows)
+      cnt = d.w ? ((d.y + kJoinLongRows - 1) / kJoinLongRows) << 16
+                : (d.y + 31) / 32 * kGroups;
   }
-  auto slot = [&](int k) { return k == 0 ? 2 * i + 1 : 2 * (i + k * CL); };
-  __shared__ float acc_s[kWarps][DV], l_s[kWarps];
-  const bool wide = n > 2 * kWarps;
-  const int step = wide ? kWarps : 1, k_first = wide ? warp : 0;
-  const int row_step = wide ? kJoinRows : kJoinRows * kWarps;
-  for (int row = wide ? blockIdx.y : blockIdx.y * kWarps + warp; row < d.y; row += row_step) {
-    float m = -INFINITY;
-    for (int k = lane; k < n; k += 32) m = fmaxf(m, part_ml[slot(k) * kBM + row].x);
+  if (warp < 5) {
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
-    const float base = m == -INFINITY ? 0.f : m;
-    float acc[kV] = {}, l = 0.f;
-#pragma unroll 4
-    for (int k = k_first; k < n; k += step) {
-      const size_t at = static_cast<size_t>(slot(k)) * kBM + row;
-      const float2 ml = part_ml[at];
-      const float w = ex2_approx(ml.x - base);
-      l += w * ml.y;
-#pragma unroll
-      for (int c = 0; c < kV; ++c) acc[c] += w * part_o[at * DV + c * 32 + lane];
+    for (int s = 1; s < 32; s <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, cnt, s);
+      if (lane >= s) cnt += y;
     }
-    if (wide) {
-      __syncthreads();
-#pragma unroll
-      for (int c = 0; c < kV; ++c) acc_s[warp][c * 32 + lane] = acc[c];
-      if (lane == 0) l_s[warp] = l;
-      __syncthreads();
-      for (int c = threadIdx.x; c < DV; c += kJoinThreads) {
-        float a = 0.f, t = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          a += acc_s[w][c];
-          t += l_s[w];
-        }
-        o[(static_cast<size_t>(d.x) + row) * DC + vpart * DV + c] =
-            __float2bfloat16_rn(t == 0.f ? 0.f : a / t);
+    if (lane == 31) sums[warp] = cnt;
+  }
+  __syncthreads();
+  if (warp < 5) {
+    for (int w = 0; w < warp; ++w) cnt += sums[w];
+    if (threadIdx.x < kMaxCtas) items[threadIdx.x + 1] = cnt;
+    if (threadIdx.x == 0) items[0] = 0;
+  }
+  __syncthreads();
+  // the tile of item `it`; sh = 0 or 16 picks the half of the prefix sums
+  auto tile_of = [&](int it, int sh) {
+    int lo = 0, hi = ctas - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (((items[mid] >> sh) & 0xffff) <= it)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    return lo;
+  };
+  // the chain of tile i: slot 1 of CTA i, then slot 0 of the CTAs after it in its
+  // place of their pairs, up to the one that ends the tile
+  auto chain_of = [&](int i) {
+    for (int k0 = 1; i + k0 * CL < ctas; k0 += 32) {
+      const int j = i + (k0 + lane) * CL;
+      const int f = j < ctas ? flags[j] : 0;
+      const unsigned stop = __ballot_sync(
+          0xffffffffu, !(f & (kPartHeld | kPartEmpty)) || (f & kPartEnds));
+      if (stop) {
+        const int l = __ffs(stop) - 1;
+        return k0 + l + ((__shfl_sync(0xffffffffu, f, l) & kPartHeld) ? 1 : 0);
       }
-    } else {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-      for (int c = 0; c < kV; ++c)
-        o[(static_cast<size_t>(d.x) + row) * DC + vpart * DV + c * 32 + lane] =
-            __float2bfloat16_rn(acc[c] * inv);
     }
+    return (ctas - 1 - i) / CL + 1;
+  };
+
+  const int short_items = items[ctas] & 0xffff, long_items = items[ctas] >> 16;
+  for (int it = blockIdx.x + gridDim.x * warp; it < short_items; it += gridDim.x * kWarps) {
+    const int i = tile_of(it, 0), n = chain_of(i);
+    const int4 d = desc[i];
+    const int sub = it - (items[i] & 0xffff);
+    const int rb = sub / kGroups, cg0 = (sub - rb * kGroups) * (kJoinCols / 4);
+    const int row = rb * 32 + lane;
+    const bool ok = row < d.y;
+    float m = -INFINITY, l = 0.f;
+    float4 acc[4] = {};
+    // running maximum over the chain, two partial rows at a time in flight
+#pragma unroll 2
+    for (int k = 0; k < n; ++k) {
+      const int sl = k == 0 ? 2 * i + 1 : 2 * (i + k * CL);
+      const bool held = k == 0 || (flags[i + k * CL] & kPartHeld);
+      if (!ok || !held) continue;
+      const float2 ml = part_ml[sl * kBM + row];
+      float4 v[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        v[c] = reinterpret_cast<const float4*>(
+            part_o)[(static_cast<size_t>(sl) * kCg + cg0 + c) * kBM + row];
+      const float m_new = fmaxf(m, ml.x);
+      const float base = m_new == -INFINITY ? 0.f : m_new;
+      const float a = ex2_approx(m - base), b = ex2_approx(ml.x - base);
+      m = m_new;
+      l = l * a + ml.y * b;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        acc[c].x = acc[c].x * a + v[c].x * b;
+        acc[c].y = acc[c].y * a + v[c].y * b;
+        acc[c].z = acc[c].z * a + v[c].z * b;
+        acc[c].w = acc[c].w * a + v[c].w * b;
+      }
+    }
+    if (ok) {
+      const int vpart = kSplit > 1 ? i % CL : 0;
+      const float f = l == 0.f ? 0.f : 1.f / l;
+      uint4* dst = reinterpret_cast<uint4*>(o + (static_cast<size_t>(d.x) + row) * DC +
+                                            vpart * DV + cg0 * 4);
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        dst[c] = make_uint4(pack_bf16x2(acc[2 * c].x * f, acc[2 * c].y * f),
+                            pack_bf16x2(acc[2 * c].z * f, acc[2 * c].w * f),
+                            pack_bf16x2(acc[2 * c + 1].x * f, acc[2 * c + 1].y * f),
+                            pack_bf16x2(acc[2 * c + 1].z * f, acc[2 * c + 1].w * f));
+    }
+  }
+
+  for (int it = blockIdx.x; it < long_items; it += gridDim.x) {
+    const int i = tile_of(it, 16), n = chain_of(i);
+    const int4 d = desc[i];
+    const int row0 = (it - (items[i] >> 16)) * kJoinLongRows;
+    const int nr = min(kJoinLongRows, d.y - row0);
+    auto slot = [&](int k) { return k == 0 ? 2 * i + 1 : 2 * (i + k * CL); };
+    auto held = [&](int k) { return k == 0 || (flags[i + k * CL] & kPartHeld); };
+    if (warp < nr) {  // weights: a warp per row
+      float m = -INFINITY;
+#pragma unroll 5
+      for (int k = lane; k < n; k += 32) {
+        const float x = part_ml[slot(k) * kBM + row0 + warp].x;
+        m = fmaxf(m, held(k) ? x : -INFINITY);
+      }
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+      const float base = m == -INFINITY ? 0.f : m;
+      float l = 0.f;
+#pragma unroll 5
+      for (int k = lane; k < n; k += 32) {
+        const float2 ml = part_ml[slot(k) * kBM + row0 + warp];
+        const float wt = held(k) ? ex2_approx(ml.x - base) : 0.f;
+        if (wt != 0.f) l += wt * ml.y;  // an empty share's slot may hold anything
+        weight[k * kJoinLongRows + warp] = wt;
+      }
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+      if (lane == 0) norm[warp] = l == 0.f ? 0.f : 1.f / l;
+    }
+    __syncthreads();
+    const int pairs = nr * kCg;  // (4 columns, row), rows fastest
+    const int split = kJoinThreads / pairs;
+    const int ks = threadIdx.x / pairs, pr = threadIdx.x - ks * pairs;
+    const int cg = pr / nr, row = pr - cg * nr;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (ks < split) {
+#pragma unroll 8
+      for (int k = ks; k < n; k += split) {
+        const float wt = weight[k * kJoinLongRows + row];
+        const float4 v = reinterpret_cast<const float4*>(
+            part_o)[(static_cast<size_t>(slot(k)) * kCg + cg) * kBM + row0 + row];
+        const bool some = wt != 0.f;
+        acc.x += some ? wt * v.x : 0.f;
+        acc.y += some ? wt * v.y : 0.f;
+        acc.z += some ? wt * v.z : 0.f;
+        acc.w += some ? wt * v.w : 0.f;
+      }
+      red[threadIdx.x] = acc;
+    }
+    __syncthreads();
+    if (ks == 0) {
+      for (int k = 1; k < split; ++k) {
+        const float4 v = red[k * pairs + pr];
+        acc.x += v.x;
+        acc.y += v.y;
+        acc.z += v.z;
+        acc.w += v.w;
+      }
+      const int vpart = kSplit > 1 ? i % CL : 0;
+      const float f = norm[row];
+      *reinterpret_cast<uint2*>(o + (static_cast<size_t>(d.x) + row0 + row) * DC + vpart * DV +
+                                cg * 4) =
+          make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
+    }
+    __syncthreads();  // weight, norm and red are the next item's
   }
 }
 
@@ -906,8 +1057,8 @@ int launch_paged(const PagedAttnArgs& a) {
     set_last_cuda_error(e);
     return MLA_ERR_CUDA;
   }
-  return launch_pdl(paged_join_kernel<DC, S::DV, CL>, dim3(resident, kJoinRows), kJoinThreads, 0,
-                    a.stream, k.part_o, k.part_ml, k.part_desc, k.o, resident,
+  return launch_pdl(paged_join_kernel<DC, S::DV, CL>, dim3(kJoinGrid), kJoinThreads, 0, a.stream,
+                    k.part_o, k.part_ml, k.part_desc, k.o, resident,
                     static_cast<long long>(a.total) * a.heads);
 }
 

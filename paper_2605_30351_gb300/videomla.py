@@ -208,7 +208,9 @@ def mla_rope_table_fill(cfg):
 
 def _stream_ptr(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the handle of torch.cuda.current_stream() without the Stream object,
+        # which costs as much as a small call's launch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -222,6 +224,14 @@ def _dev(t, dtype, shape, name):
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _ptr(t, dtype, shape, name):
+    """_dev for calls that take microseconds: the address as an int."""
+    if type(t) is torch.Tensor and t.is_cuda and t.dtype is dtype and t.shape == shape \
+            and t.is_contiguous():
+        return t.data_ptr()
+    return _dev(t, dtype, shape, name)
 
 
 class LatentCache:
@@ -461,18 +471,23 @@ def mla_rope_apply(rope, x, pos, y, inverse=False, stream=None):
     for t, name in ((x, "x"), (y, "y")):
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise TypeError(f"{name} must be a CUDA tensor")
-        if t.dim() != 3 or t.shape[2] < 1 or (t.shape[2] > 1 and t.stride(2) != 1):
-            raise ValueError(f"{name} must be [tokens, heads, head_dim] with contiguous channels")
-    if x.dtype not in _DTYPES or y.dtype != x.dtype:
+    shape, dtype = x.shape, _DTYPES.get(x.dtype)
+    if dtype is None or y.dtype is not x.dtype:
         raise TypeError(f"x and y must both be bfloat16, float16 or float32, got {x.dtype}, {y.dtype}")
-    if x.shape != y.shape:
-        raise ValueError(f"y must have shape {tuple(x.shape)}, got {tuple(y.shape)}")
-    tokens, heads, dim = x.shape
+    if y.shape != shape:
+        raise ValueError(f"y must have shape {tuple(shape)}, got {tuple(y.shape)}")
+    if len(shape) != 3 or shape[2] < 1:
+        raise ValueError("x and y must be [tokens, heads, head_dim]")
+    tokens, heads, dim = shape
+    xt, xh, xc = x.stride()
+    yt, yh, yc = y.stride()
+    if dim > 1 and (xc != 1 or yc != 1):
+        raise ValueError("x and y must have contiguous channels")
     _check("mla_rope_apply",
            load().mla_rope_apply(
-               rope.ref, x.data_ptr(), _dev(pos, torch.int32, (tokens, rope.axes), "pos"),
-               y.data_ptr(), _DTYPES[x.dtype], tokens, heads, dim, x.stride(0), x.stride(1),
-               y.stride(0), y.stride(1), int(bool(inverse)), _stream_ptr(stream)))
+               rope.ref, x.data_ptr(), _ptr(pos, torch.int32, (tokens, rope.axes), "pos"),
+               y.data_ptr(), dtype, tokens, heads, dim, xt, xh, yt, yh, 1 if inverse else 0,
+               _stream_ptr(stream)))
 
 
 class PagedCache:
@@ -519,13 +534,13 @@ def mla_pages_resize(cache, new_lens, stream=None):
     back or added, a shared last page that grows is copied first."""
     _check("mla_pages_resize",
            load().mla_pages_resize(cache.ref,
-                                   _dev(new_lens, torch.int32, (cache.struct.seqs,), "new_lens"),
+                                   _ptr(new_lens, torch.int32, (cache.struct.seqs,), "new_lens"),
                                    _stream_ptr(stream)))
 
 
 def _pairs_of(src, dst):
     n = src.shape[0] if isinstance(src, torch.Tensor) and src.dim() == 1 else 0
-    return _dev(src, torch.int32, (n,), "src"), _dev(dst, torch.int32, (n,), "dst"), n
+    return _ptr(src, torch.int32, (n,), "src"), _ptr(dst, torch.int32, (n,), "dst"), n
 
 
 def mla_pages_fork(cache, src, dst, stream=None):
@@ -546,8 +561,8 @@ def mla_pages_compact(cache, new_table, new_refs, stream=None):
     i32 = torch.int32
     _check("mla_pages_compact",
            load().mla_pages_compact(cache.ref,
-                                    _dev(new_table, i32, cache.table.shape, "new_table"),
-                                    _dev(new_refs, i32, cache.refs.shape, "new_refs"),
+                                    _ptr(new_table, i32, cache.table.shape, "new_table"),
+                                    _ptr(new_refs, i32, cache.refs.shape, "new_refs"),
                                     _stream_ptr(stream)))
 
 
@@ -559,10 +574,10 @@ def mla_paged_append(cache, layer, c_new, kr_new, q_start, pos, rope, stream=Non
     total = c_new.shape[0] if isinstance(c_new, torch.Tensor) and c_new.dim() == 2 else 0
     _check("mla_paged_append",
            load().mla_paged_append(
-               cache.ref, int(layer), _dev(c_new, bf, (total, st.d_c), "c_new"),
-               _dev(kr_new, bf, (total, st.d_r), "kr_new"), total,
-               _dev(q_start, i32, (st.seqs + 1,), "q_start"),
-               _dev(pos, i32, (total, rope.axes), "pos"), rope.ref, _stream_ptr(stream)))
+               cache.ref, int(layer), _ptr(c_new, bf, (total, st.d_c), "c_new"),
+               _ptr(kr_new, bf, (total, st.d_r), "kr_new"), total,
+               _ptr(q_start, i32, (st.seqs + 1,), "q_start"),
+               _ptr(pos, i32, (total, rope.axes), "pos"), rope.ref, _stream_ptr(stream)))
 
 
 def mla_paged_workspace_bytes(cache):
@@ -582,12 +597,12 @@ def mla_paged_attention(cache, layer, q_c, q_r, q_start, head_dim, causal_block,
     total, heads = q_c.shape[:2]
     _check("mla_paged_attention",
            load().mla_paged_attention(
-               cache.ref, int(layer), _dev(q_c, bf, (total, heads, st.d_c), "q_c"),
-               _dev(q_r, bf, (total, heads, st.d_r), "q_r"), total, heads,
-               _dev(q_start, torch.int32, (st.seqs + 1,), "q_start"), int(head_dim),
+               cache.ref, int(layer), _ptr(q_c, bf, (total, heads, st.d_c), "q_c"),
+               _ptr(q_r, bf, (total, heads, st.d_r), "q_r"), total, heads,
+               _ptr(q_start, torch.int32, (st.seqs + 1,), "q_start"), int(head_dim),
                int(causal_block), workspace.data_ptr(),
                workspace.numel() * workspace.element_size(),
-               _dev(o, bf, (total, heads, st.d_c), "o"), _stream_ptr(stream)))
+               _ptr(o, bf, (total, heads, st.d_c), "o"), _stream_ptr(stream)))
 
 
 def mla_selftest_bounded_wait(limit_ns, stream=None):
