@@ -176,20 +176,26 @@ struct Place {
 
 // The shares' ends: place of share id's first block and of the one after its
 // last. Every thread of the block calls it; scratch: 8 long longs and out: two
-// Places in shared memory. Returns the cost of a share.
+// Places in shared memory. Three warps look for each end, all streams among their
+// 96 threads: one search's latency, not two, is part of every call. Returns the
+// cost of a share.
 template <int BN, int TR>
 __device__ __forceinline__ long long find_share(const PagedK& p, int id, int groups,
                                                 long long* scratch, Place* out) {
-  constexpr int kWarps = kThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int per = (p.seqs + kThreads - 1) / kThreads;
-  const int s0 = threadIdx.x * per;
+  const int e = warp / 3;  // which end; the seventh warp only waits
+  const int per = (p.seqs + 95) / 96;
+  const int s0 = (threadIdx.x - e * 96) * per;
   long long mine = 0;
-  for (int k = 0; k < per; ++k)
-    if (s0 + k < p.seqs) {
-      const Cost c = cost_of<TR>(p, stream_at(p, s0 + k));
-      mine += c.before(c.tiles);
-    }
+  Stream st{0, 0, 0};
+  Cost c{0, 0, 0};
+  if (e < 2)
+    for (int k = 0; k < per; ++k)
+      if (s0 + k < p.seqs) {
+        st = stream_at(p, s0 + k);
+        c = cost_of<TR>(p, st);
+        mine += c.before(c.tiles);
+      }
   long long x = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -199,35 +205,32 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
   if (lane == 31) scratch[warp] = x;
   if (threadIdx.x < 2) out[threadIdx.x] = Place{p.seqs, 0, 0};  // the end of the work
   __syncthreads();
-  long long total = 0, base = x - mine;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) base += scratch[w];
-    total += scratch[w];
-  }
+  const long long total = scratch[0] + scratch[1] + scratch[2];
   const int active = static_cast<int>(min(static_cast<long long>(groups), (total + BN - 1) / BN));
-  if (id < active) {
-#pragma unroll 1
-    for (int e = 0; e < 2; ++e) {
-      // total * (id + e) / active: in 32 bits where it fits (a 64-bit division
-      // costs a tenth of a short call), else without the product's overflow
-      long long u;
-      if (total < (1 << 24)) {
-        u = static_cast<unsigned>(total) * (id + e) / static_cast<unsigned>(active);
-      } else {
-        const long long q = total / active, r = total - q * active;
-        u = q * (id + e) + r * (id + e) / active;
-      }
-      if (u < base || u >= base + mine) continue;
+  if (id < active && e < 2) {
+    long long base = x - mine;
+    for (int w = 3 * e; w < warp; ++w) base += scratch[w];
+    // total * (id + e) / active: in 32 bits where it fits (a 64-bit division is a
+    // noticeable part of a short call), else without the product's overflow
+    long long u;
+    if (total < (1 << 24)) {
+      u = static_cast<unsigned>(total) * (id + e) / static_cast<unsigned>(active);
+    } else {
+      const long long q = total / active, r = total - q * active;
+      u = q * (id + e) + r * (id + e) / active;
+    }
+    if (u >= base && u < base + mine) {
       long long rem = u - base;
-      for (int s = s0; s < min(s0 + per, p.seqs); ++s) {
-        const Stream st = stream_at(p, s);
-        const Cost c = cost_of<TR>(p, st);
-        const long long all = c.before(c.tiles);
-        if (rem >= all) {
+      int s = s0;
+      if (per > 1)
+        for (; s < p.seqs; ++s) {
+          st = stream_at(p, s);
+          c = cost_of<TR>(p, st);
+          const long long all = c.before(c.tiles);
+          if (rem < all) break;
           rem -= all;
-          continue;
         }
+      if (s < p.seqs) {
         int lo = 0, hi = c.tiles - 1;  // the last tile that begins at or before rem
         while (lo < hi) {
           const int mid = (lo + hi + 1) / 2;
@@ -242,7 +245,6 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
             static_cast<float>(rem - at) *
             __fdividef(static_cast<float>(blocks), static_cast<float>(c.before(lo + 1) - at)));
         out[e] = Place{s, lo, min(off, blocks - 1)};
-        break;
       }
     }
   }
@@ -867,29 +869,50 @@ __global__ void __launch_bounds__(kJoinThreads)
     const bool ok = row < d.y;
     float m = -INFINITY, l = 0.f;
     float4 acc[4] = {};
-    // running maximum over the chain, two partial rows at a time in flight
-#pragma unroll 2
-    for (int k = 0; k < n; ++k) {
-      const int sl = k == 0 ? 2 * i + 1 : 2 * (i + k * CL);
-      const bool held = k == 0 || (flags[i + k * CL] & kPartHeld);
-      if (!ok || !held) continue;
-      const float2 ml = part_ml[sl * kBM + row];
-      float4 v[4];
+    // the chain in groups of four, all loads of a group in flight together; rows
+    // and slots that hold nothing are loaded and not used
+#pragma unroll 1
+    for (int k0 = 0; k0 < n; k0 += 4) {
+      float2 ml[4];
+      float4 v[4][4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        v[c] = reinterpret_cast<const float4*>(
-            part_o)[(static_cast<size_t>(sl) * kCg + cg0 + c) * kBM + row];
-      const float m_new = fmaxf(m, ml.x);
+      for (int k = 0; k < 4; ++k) {
+        const int kk = min(k0 + k, n - 1);
+        const int sl = kk == 0 ? 2 * i + 1 : 2 * (i + kk * CL);
+        ml[k] = part_ml[sl * kBM + row];
+        if (!ok || k0 + k >= n || (kk > 0 && !(flags[i + kk * CL] & kPartHeld)))
+          ml[k] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          v[k][c] = reinterpret_cast<const float4*>(
+              part_o)[(static_cast<size_t>(sl) * kCg + cg0 + c) * kBM + row];
+      }
+      const float m_new =
+          fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
       const float base = m_new == -INFINITY ? 0.f : m_new;
-      const float a = ex2_approx(m - base), b = ex2_approx(ml.x - base);
+      const float a = ex2_approx(m - base);
       m = m_new;
-      l = l * a + ml.y * b;
+      l *= a;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        acc[c].x = acc[c].x * a + v[c].x * b;
-        acc[c].y = acc[c].y * a + v[c].y * b;
-        acc[c].z = acc[c].z * a + v[c].z * b;
-        acc[c].w = acc[c].w * a + v[c].w * b;
+        acc[c].x *= a;
+        acc[c].y *= a;
+        acc[c].z *= a;
+        acc[c].w *= a;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float b = ex2_approx(ml[k].x - base);
+        if (b != 0.f) {
+          l += ml[k].y * b;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            acc[c].x += v[k][c].x * b;
+            acc[c].y += v[k][c].y * b;
+            acc[c].z += v[k][c].z * b;
+            acc[c].w += v[k][c].w * b;
+          }
+        }
       }
     }
     if (ok) {
