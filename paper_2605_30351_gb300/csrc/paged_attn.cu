@@ -20,11 +20,19 @@
 // host round trip, and the same result from call to call.
 //
 //   warp 0     finds the pages of a key block and copies them by TMA into a ring
-//              of stages (one box per page and 64 columns)
+//              of stages (one box per page and 64 columns). A row tile's Q takes
+//              its turn in the same ring, so it is on its way while the previous
+//              tile's last blocks are computed
 //   warp 1     clears rows of a stage that hold no token of the stream (they may
 //              hold NaN, and 0 * NaN would reach O), issues the score MMAs
-//   warp 6     issues O += P V
-//   warps 2-5  load Q, then the softmax: thread i owns row i
+//   warp 2     issues O += P V
+//   warps 4-7  move Q from the ring to its place, then the softmax: thread i owns
+//              row i. It copies a block's scores to registers at once, so the next
+//              block's are computed while it works on the exponentials. Two threads
+//              per row, and two groups of warps that take blocks in turns, were
+//              both slower (a 4,680-token chunk on 32,760 keys at d_c = 192: 936
+//              and 840 us against 809): what they save in a block's latency they
+//              lose to exchanging maxima, registers and power.
 // Pairs (CL = 2): two consecutive row tiles walk the same key blocks; each CTA
 // fetches half of the boxes and multicasts them to both. At d_c = 512 the two
 // CTAs of a pair share one row tile instead and hold 256 columns of O each.
@@ -38,38 +46,39 @@ namespace vmla {
 namespace {
 
 constexpr int kBM = 128;       // rows per tile = TMEM lanes
-constexpr int kThreads = 224;  // 7 warps
+constexpr int kThreads = 256;  // 8 warps (the fourth has no role)
 constexpr float kRescaleLog2 = 8.0f;
 constexpr int kMaxCtas = 152;  // the workspace holds two partial tiles for each
 constexpr int kJoinThreads = 512;
-constexpr int kJoinGrid = 2 * kMaxCtas;
+constexpr int kJoinGrid = kMaxCtas;
 constexpr int kJoinCols = 16;      // columns of a warp's join item (of 32 rows)
 constexpr int kJoinLongRows = 2;   // rows of a block's item where many shares cut the tile
 
 template <int DC, int DR>
 struct PagedShape {
-  static constexpr int BN = DC > 256 ? 64 : 128;   // keys per block
+  static constexpr int BN = DC >= 256 ? 64 : 128;  // keys per block
   static constexpr int DV = DC > 256 ? 256 : DC;   // output columns per CTA
   static constexpr int DK = DC + DR;
   static constexpr int kSplit = DC / DV;           // CTAs that share a row tile
   static constexpr int kTileBytes = BN * DK * 2;   // one stage
-  static constexpr int kCBox = BN * 128;           // [BN keys x 64 columns] of c
+  static constexpr int kCBox = BN * 128;           // [BN rows x 64 columns] of c
   static constexpr int kKrOff = DC * BN * 2;       // the d_r columns of a stage
   static constexpr int kBoxes = DC / 64 + 1;       // boxes per page
-  // TMEM columns: S, P (bf16, two a column), O, and Q as far as it fits
+  static constexpr int kQStages = kBM / BN;        // stages that Q takes
+  // TMEM columns: S, P (bf16, two a column), O, and Q as far as it fits; the rest
+  // of Q stays in shared memory
   static constexpr int kTmemS = 0;
   static constexpr int kTmemP = BN;
   static constexpr int kTmemO = BN + BN / 2;
   static constexpr int kTmemQ = kTmemO + DV;
-  static constexpr int kBarBytes = 512;
-  static constexpr int kSmemCap = 232448;
-  static constexpr bool kQinTmem = kTmemQ + DK / 2 <= 512;
-  static constexpr bool kQSmemFits = 1024 + kBarBytes + kBM * DK * 2 + 2 * kTileBytes <= kSmemCap;
-  static constexpr int kQcTmem =
-      kQinTmem ? DC : (kQSmemFits ? 0 : ((512 - kTmemQ) * 2 / 64) * 64);
+  static constexpr bool kQrTmem = kTmemQ + DK / 2 <= 512;
+  static constexpr int kQcFit = (512 - kTmemQ) * 2 / 64 * 64;
+  static constexpr int kQcTmem = kQcFit < DC ? kQcFit : DC;
   static constexpr int kQcSmem = DC - kQcTmem;
   static constexpr int kQKrOff = kQcSmem * kBM * 2;
-  static constexpr int kQBytes = kQinTmem ? 0 : kQKrOff + kBM * DR * 2;
+  static constexpr int kQBytes = kQrTmem ? 0 : kQKrOff + kBM * DR * 2;
+  static constexpr int kBarBytes = 512;  // barriers and small words
+  static constexpr int kSmemCap = 232448;
   static constexpr int kFit = (kSmemCap - 1024 - kBarBytes - kQBytes) / kTileBytes;
   static constexpr int kMaxStages = BN == 128 ? 4 : 6;
   static constexpr int kStages = kFit > kMaxStages ? kMaxStages : kFit;
@@ -84,14 +93,13 @@ struct PagedShape {
   static constexpr unsigned long long kPartBytes = 2ull * kMaxCtas * kBM * DV * 4;
   static constexpr unsigned long long kMlBytes = 2ull * kMaxCtas * kBM * 8;
   static constexpr unsigned long long kWorkspace = kPartBytes + kMlBytes + 2ull * kMaxCtas * 16;
-  static_assert(kTmemQ + kQcTmem / 2 <= 512 && kStages >= 2, "TMEM and stages must fit");
+  static_assert(kTmemQ + kQcTmem / 2 <= 512 && kStages >= 2 && kStages >= kQStages,
+                "TMEM and stages must fit");
   static_assert(kTileBytes % 1024 == 0 && kKrOff % 1024 == 0 && kQKrOff % 1024 == 0,
                 "swizzle-atom alignment");
 };
 
 struct PagedK {
-  const __nv_bfloat16* q_c;
-  const __nv_bfloat16* q_r;
   const int* q_start;
   const int* table;
   const int* lens;
@@ -183,7 +191,7 @@ template <int BN, int TR>
 __device__ __forceinline__ long long find_share(const PagedK& p, int id, int groups,
                                                 long long* scratch, Place* out) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int e = warp / 3;  // which end; the seventh warp only waits
+  const int e = warp / 3;  // which end; the other warps only wait
   const int per = (p.seqs + 95) / 96;
   const int s0 = (threadIdx.x - e * 96) * per;
   long long mine = 0;
@@ -202,7 +210,7 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
     const long long y = __shfl_up_sync(0xffffffffu, x, d);
     if (lane >= d) x += y;
   }
-  if (lane == 31) scratch[warp] = x;
+  if (lane == 31 && e < 2) scratch[warp] = x;
   if (threadIdx.x < 2) out[threadIdx.x] = Place{p.seqs, 0, 0};  // the end of the work
   __syncthreads();
   const long long total = scratch[0] + scratch[1] + scratch[2];
@@ -307,9 +315,11 @@ struct BlockPos {
 template <int DC, int DR, int CL>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_attn_kernel(const __grid_constant__ CUtensorMap tm_c,
-                      const __grid_constant__ CUtensorMap tm_kr, const PagedK p) {
+                      const __grid_constant__ CUtensorMap tm_kr,
+                      const __grid_constant__ CUtensorMap tm_qc,
+                      const __grid_constant__ CUtensorMap tm_qr, const PagedK p) {
   using S = PagedShape<DC, DR>;
-  constexpr int BN = S::BN, DV = S::DV, NST = S::kStages;
+  constexpr int BN = S::BN, DV = S::DV, NST = S::kStages, QST = S::kQStages;
   constexpr int TR = kBM * CL / S::kSplit;  // rows of a CTA's, or a pair's, tile
   constexpr uint16_t kPair = static_cast<uint16_t>((1u << CL) - 1u);
   static_assert(S::kSplit == 1 || CL == S::kSplit, "split tiles take a pair");
@@ -321,11 +331,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* q_ready = bars;
   uint64_t* kv_full = bars + 1;
   uint64_t* kv_empty = kv_full + NST;
-  uint64_t* s_full = kv_empty + NST;
-  uint64_t* s_free = s_full + 1;
-  uint64_t* p_full = s_free + 1;
+  uint64_t* s_free = kv_empty + NST;
+  uint64_t* s_full = s_free + 1;
+  uint64_t* p_full = s_full + 1;
   uint64_t* pv_done = p_full + 1;
-  uint64_t* mma_drain = pv_done + 1;  // [2]
+  uint64_t* mma_drain = pv_done + 1;  // [2]: one per issuing thread
   long long* scratch = reinterpret_cast<long long*>(mma_drain + 2);  // [8]
   Place* ends = reinterpret_cast<Place*>(scratch + 8);               // [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ends + 2);
@@ -341,8 +351,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&kv_full[s], 1);
       mbar_init(&kv_empty[s], CL);
     }
-    mbar_init(s_full, 1);
     mbar_init(s_free, kBM);
+    mbar_init(s_full, 1);
     mbar_init(p_full, kBM);
     mbar_init(pv_done, 1);
     mbar_init(&mma_drain[0], 1);
@@ -351,6 +361,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_mbar_init();
     tma_prefetch_desc(&tm_c);
     tma_prefetch_desc(&tm_kr);
+    tma_prefetch_desc(&tm_qc);
+    tma_prefetch_desc(&tm_qr);
   }
   if (warp == 1) {
     tmem_alloc(tmem_slot, S::kTmemCols);
@@ -364,6 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if constexpr (CL > 1) cluster_sync();
   grid_dep_sync();
   const int crank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int first_row = S::kSplit == 1 ? crank * kBM : 0;  // of the pair's tile
   if (blockIdx.x == 0) {
     check_q_start(p.q_start, p.seqs, p.total, p.status);
     for (int s = threadIdx.x; s < p.seqs; s += kThreads) {
@@ -378,150 +391,195 @@ __global__ void __launch_bounds__(kThreads, 1)
   Walk<BN, TR> walk(p, ends);
   Segment g;
   bool ok = true;
-  int it = 0;  // key blocks so far: the phase of every per-block barrier
+  int it = 0;  // key blocks so far: the phases of the per-block barriers
+  int sc = 0;  // ring stages so far, Q's included: the phases of kv_full, kv_empty
 
-  if (warp == 0) {
-    // ------------------------------------------------------------ producer
-    while (ok && walk.next(g)) {
-      const int* row = p.table + static_cast<size_t>(g.s) * p.max_pages;
-      BlockPos<BN> pos(p, g.kb0);
-      for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, pos.step(p)) {
-        const int st = it % NST;
-        const int valid = min(pos.rows(p), g.st.len - pos.token(p));
-        const int boxes =
-            p.per_group == 1 ? (valid > 0) : (max(valid, 0) + p.page_tokens - 1) / p.page_tokens;
-        if (it >= NST) ok = mbar_wait(&kv_empty[st], ((it / NST) - 1) & 1, wc);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        uint8_t* kv = sKV + st * S::kTileBytes;
-        if (lane == 0) {
-          if (boxes)
-            mbar_arrive_expect_tx(&kv_full[st], boxes * p.box_rows * S::DK * 2);
-          else
-            mbar_arrive(&kv_full[st]);
-        }
-        __syncwarp();
-        for (int bx = lane; bx < boxes * S::kBoxes; bx += 32) {
-          if (CL > 1 && (bx & 1) != crank) continue;
-          const int i = bx / S::kBoxes, cb = bx - i * S::kBoxes;
-          const int page = __ldg(row + pos.grp * p.per_group + i);
-          int r = p.pages * p.page_tokens;  // past the pool: zeros
-          if (page >= 0 && page < p.pages)
-            r = page * p.page_tokens + pos.sub * BN;
-          else
-            record_status(p.status, MLA_ERR_RANGE);
-          const bool is_c = cb < DC / 64;
-          uint8_t* dst = is_c ? kv + cb * S::kCBox + i * p.box_rows * 128
-                              : kv + S::kKrOff + i * p.box_rows * static_cast<int>(S::kKrRow);
-          const CUtensorMap* map = is_c ? &tm_c : &tm_kr;
-          const int x = is_c ? cb * 64 : 0;
+  if (warp < 4) {
+    if (warp == 0) {
+      // ------------------------------------------------------------ producer
+      auto acquire = [&]() {  // stage sc is free
+        bool free = true;
+        if (sc >= NST) {
           if constexpr (CL == 1)
-            tma_load_2d(dst, map, &kv_full[st], x, r);
-          else
-            tma_load_2d_mc(dst, map, &kv_full[st], x, r, kPair);
+            free = mbar_wait(&kv_empty[sc % NST], ((sc / NST) - 1) & 1, wc);
+          else  // the peer's threads arrive on it too
+            free = mbar_wait_cluster(&kv_empty[sc % NST], ((sc / NST) - 1) & 1, wc);
+        }
+        return __all_sync(0xffffffffu, free);
+      };
+      while (ok && walk.next(g)) {
+        const int rows = g.st.n * p.heads;
+        for (int q = 0; q < QST; ++q, ++sc) {
+          ok = acquire();
+          if (!ok) break;
+          const int r0 = g.tile * TR + first_row + q * BN;
+          const int boxes = max(0, min(BN / 32, (rows - r0 + 31) / 32));
+          uint8_t* st = sKV + (sc % NST) * S::kTileBytes;
+          uint64_t* full = &kv_full[sc % NST];
+          if (lane == 0) {
+            if (boxes)
+              mbar_arrive_expect_tx(full, boxes * 32 * S::DK * 2);
+            else
+              mbar_arrive(full);
+          }
+          __syncwarp();
+          for (int bx = lane; bx < boxes * S::kBoxes; bx += 32) {
+            const int i = bx / S::kBoxes, cb = bx - i * S::kBoxes;
+            const int r = g.st.q0 * p.heads + r0 + 32 * i;
+            if (cb < DC / 64)
+              tma_load_2d(st + cb * S::kCBox + i * 32 * 128, &tm_qc, full, cb * 64, r);
+            else
+              tma_load_2d(st + S::kKrOff + i * 32 * S::kKrRow, &tm_qr, full, 0, r);
+          }
+        }
+        if (!ok) break;
+        const int* row = p.table + static_cast<size_t>(g.s) * p.max_pages;
+        BlockPos<BN> pos(p, g.kb0);
+        for (int kb = g.kb0; kb < g.kb1; ++kb, ++sc, pos.step(p)) {
+          const int valid = min(pos.rows(p), g.st.len - pos.token(p));
+          const int boxes =
+              p.per_group == 1 ? (valid > 0) : (max(valid, 0) + p.page_tokens - 1) / p.page_tokens;
+          ok = acquire();
+          if (!ok) break;
+          uint8_t* kv = sKV + (sc % NST) * S::kTileBytes;
+          uint64_t* full = &kv_full[sc % NST];
+          if (lane == 0) {
+            if (boxes)
+              mbar_arrive_expect_tx(full, boxes * p.box_rows * S::DK * 2);
+            else
+              mbar_arrive(full);
+          }
+          __syncwarp();
+          for (int bx = lane; bx < boxes * S::kBoxes; bx += 32) {
+            if (CL > 1 && (bx & 1) != crank) continue;
+            const int i = bx / S::kBoxes, cb = bx - i * S::kBoxes;
+            const int page = __ldg(row + pos.grp * p.per_group + i);
+            int r = p.pages * p.page_tokens;  // past the pool: zeros
+            if (page >= 0 && page < p.pages)
+              r = page * p.page_tokens + pos.sub * BN;
+            else
+              record_status(p.status, MLA_ERR_RANGE);
+            const bool is_c = cb < DC / 64;
+            uint8_t* dst = is_c ? kv + cb * S::kCBox + i * p.box_rows * 128
+                                : kv + S::kKrOff + i * p.box_rows * static_cast<int>(S::kKrRow);
+            const CUtensorMap* map = is_c ? &tm_c : &tm_kr;
+            const int x = is_c ? cb * 64 : 0;
+            if constexpr (CL == 1)
+              tma_load_2d(dst, map, full, x, r);
+            else
+              tma_load_2d_mc(dst, map, full, x, r, kPair);
+          }
         }
       }
-    }
-    // every stage's last use must be released before the CTA may exit
-    for (int st = 0; st < NST && st < it && !*abort_flag; ++st)
-      mbar_wait(&kv_empty[st], (((it - st + NST - 1) / NST) - 1) & 1, wc);
-    if (*abort_flag)  // let every copy this CTA started land before exit
-      for (int u = it > NST ? it - NST : 0; u < it; ++u)
-        mbar_wait_drain(&kv_full[u % NST], (u / NST) & 1, p.status);
-    __syncwarp();
-  } else if (warp == 1) {
-    // ---------------------------------------------------------- QK issuer
-    const uint32_t qa = smem_u32(sQ);
-    int seg = 0;
-    while (ok && walk.next(g)) {
-      ok = __all_sync(0xffffffffu, mbar_wait(q_ready, seg & 1, wc));
-      ++seg;
-      if (!ok) break;
-      BlockPos<BN> pos(p, g.kb0);
-      for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, pos.step(p)) {
-        const int st = it % NST;
-        // S's previous contents must have been read, and the keys have landed
-        if (it >= 1) ok = mbar_wait(s_free, (it - 1) & 1, wc);
-        ok = ok && mbar_wait(&kv_full[st], (it / NST) & 1, wc);
-        ok = __all_sync(0xffffffffu, ok);
+      // every stage's last use must be released before the CTA may exit
+      for (int st = 0; st < NST && st < sc && !*abort_flag; ++st)
+        mbar_wait(&kv_empty[st], (((sc - st + NST - 1) / NST) - 1) & 1, wc);
+      if (*abort_flag)  // let every copy this CTA started land before exit
+        for (int u = sc > NST ? sc - NST : 0; u < sc; ++u)
+          mbar_wait_drain(&kv_full[u % NST], (u / NST) & 1, p.status);
+      __syncwarp();
+    } else if (warp == 1) {
+      // ---------------------------------------------------------- QK issuer
+      const uint32_t qa = smem_u32(sQ);
+      int seg = 0;
+      while (ok && walk.next(g)) {
+        ok = __all_sync(0xffffffffu, mbar_wait(q_ready, seg & 1, wc));
+        ++seg;
         if (!ok) break;
-        uint8_t* kv = sKV + st * S::kTileBytes;
-        const int valid = max(0, min(pos.rows(p), g.st.len - pos.token(p)));
-        if (valid < BN) {
-          const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-          for (int cb = 0; cb < DC / 64; ++cb)
-            for (int i = valid * 8 + lane; i < BN * 8; i += 32)
-              *reinterpret_cast<uint4*>(kv + cb * S::kCBox + i * 16) = zero;
-          fence_proxy_async_smem();
+        // Q has left its stages: give them back, to both CTAs of a pair
+        for (int q = 0; q < QST; ++q, ++sc)
+          if (lane < CL) {
+            if constexpr (CL == 1)
+              mbar_arrive(&kv_empty[sc % NST]);
+            else
+              mbar_arrive_cluster(dsmem_addr(smem_u32(&kv_empty[sc % NST]), lane));
+          }
+        BlockPos<BN> pos(p, g.kb0);
+        for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, ++sc, pos.step(p)) {
+          const int st = sc % NST;
+          // S's previous contents have been read, and the keys have landed
+          if (it >= 1) ok = mbar_wait(s_free, (it - 1) & 1, wc);
+          ok = ok && mbar_wait(&kv_full[st], (sc / NST) & 1, wc);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          uint8_t* kv = sKV + st * S::kTileBytes;
+          const int valid = max(0, min(pos.rows(p), g.st.len - pos.token(p)));
+          if (valid < BN) {
+            const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+            for (int cb = 0; cb < DC / 64; ++cb)
+              for (int i = valid * 8 + lane; i < BN * 8; i += 32)
+                *reinterpret_cast<uint4*>(kv + cb * S::kCBox + i * 16) = zero;
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          if (lane == 0) {
+            tc_fence_after();
+            const uint32_t ka = smem_u32(kv);
+            const uint32_t d = tmem + S::kTmemS;
+#pragma unroll
+            for (int cb = 0; cb < DC / 64; ++cb)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint64_t bd = sdesc(ka + cb * S::kCBox + k * 32, 16, 1024, kSw128);
+                const uint32_t acc = (cb | k) != 0 ? 1u : 0u;
+                if (cb < S::kQcTmem / 64)
+                  umma_ts(d, tmem + S::kTmemQ + (cb * 4 + k) * 8, bd, S::kIdescQK, acc);
+                else
+                  umma_ss(d, sdesc(qa + (cb - S::kQcTmem / 64) * 16384 + k * 32, 16, 1024, kSw128),
+                          bd, S::kIdescQK, acc);
+              }
+#pragma unroll
+            for (int k = 0; k < DR / 16; ++k) {
+              const uint64_t bd = sdesc(ka + S::kKrOff + k * 32, 16, S::kKrSbo, S::kKrSw);
+              if constexpr (S::kQrTmem)
+                umma_ts(d, tmem + S::kTmemQ + DC / 2 + k * 8, bd, S::kIdescQK, 1u);
+              else
+                umma_ss(d, sdesc(qa + S::kQKrOff + k * 32, 16, S::kKrSbo, S::kKrSw), bd,
+                        S::kIdescQK, 1u);
+            }
+            umma_commit(s_full);
+          }
           __syncwarp();
         }
-        if (lane == 0) {
-          tc_fence_after();
-          const uint32_t ka = smem_u32(kv);
+      }
+      if (!ok && lane == 0) {  // wait for every MMA issued before TMEM is freed
+        umma_commit(&mma_drain[0]);
+        mbar_wait_drain(&mma_drain[0], 0, p.status);
+      }
+      __syncwarp();
+    } else if (warp == 2) {
+      // ---------------------------------------------------------- PV issuer
+      if (lane == 0) {
+        const int vpart = S::kSplit > 1 ? crank : 0;
+        while (ok && walk.next(g)) {
+          sc += QST;
+          for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, ++sc) {
+            ok = mbar_wait(p_full, it & 1, wc);
+            if (!ok) break;
+            tc_fence_after();
+            const int st = sc % NST;
+            const uint32_t va = smem_u32(sKV) + st * S::kTileBytes + vpart * (DV / 64) * S::kCBox;
 #pragma unroll
-          for (int cb = 0; cb < DC / 64; ++cb)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint64_t bd = sdesc(ka + cb * S::kCBox + k * 32, 16, 1024, kSw128);
-              const uint32_t acc = (cb | k) != 0 ? 1u : 0u;
-              if (cb < S::kQcTmem / 64)
-                umma_ts(tmem + S::kTmemS, tmem + S::kTmemQ + (cb * 4 + k) * 8, bd, S::kIdescQK,
-                        acc);
-              else
-                umma_ss(tmem + S::kTmemS,
-                        sdesc(qa + (cb - S::kQcTmem / 64) * 16384 + k * 32, 16, 1024, kSw128), bd,
-                        S::kIdescQK, acc);
-            }
-#pragma unroll
-          for (int k = 0; k < DR / 16; ++k) {
-            const uint64_t bd = sdesc(ka + S::kKrOff + k * 32, 16, S::kKrSbo, S::kKrSw);
-            if constexpr (S::kQinTmem)
-              umma_ts(tmem + S::kTmemS, tmem + S::kTmemQ + DC / 2 + k * 8, bd, S::kIdescQK, 1u);
+            for (int s = 0; s < BN / 16; ++s)
+              umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + s * 8,
+                      sdesc(va + s * 2048, S::kCBox, 1024, kSw128), S::kIdescPV,
+                      (kb > g.kb0 || s > 0) ? 1u : 0u);
+            if constexpr (CL == 1)
+              umma_commit(&kv_empty[st]);
             else
-              umma_ss(tmem + S::kTmemS, sdesc(qa + S::kQKrOff + k * 32, 16, S::kKrSbo, S::kKrSw),
-                      bd, S::kIdescQK, 1u);
+              umma_commit_mc(&kv_empty[st], kPair);
+            umma_commit(pv_done);
           }
-          umma_commit(s_full);
         }
-        __syncwarp();
-      }
-    }
-    if (!ok && lane == 0) {  // wait for every MMA issued before TMEM is freed
-      umma_commit(&mma_drain[0]);
-      mbar_wait_drain(&mma_drain[0], 0, p.status);
-    }
-    __syncwarp();
-  } else if (warp == 6) {
-    // ---------------------------------------------------------- PV issuer
-    if (lane == 0) {
-      const int vpart = S::kSplit > 1 ? crank : 0;
-      while (ok && walk.next(g)) {
-        for (int kb = g.kb0; kb < g.kb1; ++kb, ++it) {
-          ok = mbar_wait(p_full, it & 1, wc);
-          if (!ok) break;
-          tc_fence_after();
-          const int st = it % NST;
-          const uint32_t va = smem_u32(sKV) + st * S::kTileBytes + vpart * (DV / 64) * S::kCBox;
-#pragma unroll
-          for (int s = 0; s < BN / 16; ++s)
-            umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + s * 8,
-                    sdesc(va + s * 2048, S::kCBox, 1024, kSw128), S::kIdescPV,
-                    (kb > g.kb0 || s > 0) ? 1u : 0u);
-          if constexpr (CL == 1)
-            umma_commit(&kv_empty[st]);
-          else
-            umma_commit_mc(&kv_empty[st], kPair);
-          umma_commit(pv_done);
+        if (!ok) {
+          umma_commit(&mma_drain[1]);
+          mbar_wait_drain(&mma_drain[1], 0, p.status);
         }
       }
-      if (!ok) {
-        umma_commit(&mma_drain[1]);
-        mbar_wait_drain(&mma_drain[1], 0, p.status);
-      }
+      __syncwarp();
     }
-    __syncwarp();
   } else {
-    // ------------------------------------------------ softmax (warps 2..5)
+    // --------------------------------------------------- softmax (warps 4..7)
     const int quarter = warp & 3;  // TMEM lane quarter this warp may access
     const int r = quarter * 32 + lane;
     const uint32_t t_lane = static_cast<uint32_t>(quarter * 32) << 16;
@@ -531,67 +589,53 @@ __global__ void __launch_bounds__(kThreads, 1)
       size_t grow;            // its place in q and o
       bool ok, warp_ok;       // the row exists; one of the warp's does
     };
-    // The thread's row of a segment, and its Q: into TMEM (row-major, two values
-    // a column) and shared memory (the swizzle the MMA descriptors name). The
-    // score MMAs that read the previous Q are done: their last S was read.
-    auto load_row = [&](const Segment& sg) {
-      Row w;
+    // The thread's row of a segment, and its Q, from the ring stage into TMEM
+    // (row-major, two values a column) and shared memory (the swizzle the MMA
+    // descriptors name). The score MMAs that read the previous Q are done: their
+    // scores were awaited.
+    auto load_row = [&](const Segment& sg, Row& w) {
       const int rows = sg.st.n * p.heads;
-      w.tile0 = sg.tile * TR + (S::kSplit == 1 ? crank * kBM : 0);
+      w.tile0 = sg.tile * TR + first_row;
       w.lrow = w.tile0 + r;
       w.ok = w.lrow < rows;
       w.warp_ok = __any_sync(0xffffffffu, w.ok);
       w.grow = static_cast<size_t>(sg.st.q0) * p.heads + (w.ok ? w.lrow : 0);
       w.keys = w.ok ? visible_keys(sg.st.len - sg.st.n + w.lrow / p.heads, sg.st.len, p.block)
                     : 0;
+      const int slot = sc + (QST > 1 ? r / BN : 0), rr = QST > 1 ? r % BN : r;
+      if (!mbar_wait(&kv_full[slot % NST], (slot / NST) & 1, wc)) return false;
       if (w.warp_ok) {
-        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-        const uint4* qc = reinterpret_cast<const uint4*>(p.q_c + w.grow * DC);
-        const uint4* qr = reinterpret_cast<const uint4*>(p.q_r + w.grow * DR);
-        // all loads of the row before the first store, up to 32 in flight
+        const uint8_t* st = sKV + (slot % NST) * S::kTileBytes;
+        auto c_piece = [&](int i) {  // 16-byte piece i of the row's q_c
+          return *reinterpret_cast<const uint4*>(st + (i / 8) * S::kCBox + rr * 128 +
+                                                 (((i % 8) ^ (rr & 7)) * 16));
+        };
+        auto r_piece = [&](int i) {
+          const int at = DR == 32 ? (i ^ ((rr >> 1) & 3)) : (i ^ (rr & 7));
+          return *reinterpret_cast<const uint4*>(st + S::kKrOff + rr * S::kKrRow + at * 16);
+        };
         constexpr int kTm = S::kQcTmem / 8, kRr = DR / 8;
-        uint4 v[kTm + kRr + 1];
+        constexpr int kGrp = S::kQcTmem / 32 + (S::kQrTmem ? DR / 32 : 0);
 #pragma unroll
-        for (int i = 0; i < kTm; ++i) v[i] = w.ok ? __ldg(qc + i) : zero;
+        for (int gi = 0; gi < kGrp; ++gi) {
+          uint4 v[4];
 #pragma unroll
-        for (int i = 0; i < kRr; ++i) v[kTm + i] = w.ok ? __ldg(qr + i) : zero;
-        if constexpr (S::kQcSmem > 0) {
-#pragma unroll 1
-          for (int c = 0; c < S::kQcSmem / 128; ++c) {
-            uint4 u[16];
+          for (int i = 0; i < 4; ++i)
+            v[i] = gi < S::kQcTmem / 32 ? c_piece(4 * gi + i) : r_piece(4 * gi - kTm + i);
+          tmem_st16(tmem + t_lane + S::kTmemQ + gi * 16, reinterpret_cast<const uint32_t*>(v));
+        }
+        if constexpr (!S::kQrTmem) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              u[i] = w.ok ? __ldg(qc + kTm + c * 16 + i) : zero;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              *reinterpret_cast<uint4*>(sQ + (2 * c + i / 8) * 16384 + r * 128 +
-                                        (((i % 8) ^ (r & 7)) * 16)) = u[i];
-          }
-          if constexpr (S::kQcSmem % 128 != 0) {
-            constexpr int c = S::kQcSmem / 64 - 1;
+          for (int c = 0; c < S::kQcSmem / 64; ++c)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
               *reinterpret_cast<uint4*>(sQ + c * 16384 + r * 128 + ((i ^ (r & 7)) * 16)) =
-                  w.ok ? __ldg(qc + kTm + c * 8 + i) : zero;
-          }
-        }
-        if constexpr (S::kQcTmem > 0) {
-#pragma unroll
-          for (int c = 0; c < S::kQcTmem / 32; ++c)
-            tmem_st16(tmem + t_lane + S::kTmemQ + c * 16,
-                      reinterpret_cast<const uint32_t*>(&v[4 * c]));
-        }
-        if constexpr (S::kQinTmem) {
-#pragma unroll
-          for (int c = 0; c < DR / 32; ++c)
-            tmem_st16(tmem + t_lane + S::kTmemQ + DC / 2 + c * 16,
-                      reinterpret_cast<const uint32_t*>(&v[kTm + 4 * c]));
-        } else {
+                  c_piece(kTm + c * 8 + i);
           uint8_t* dst = sQ + S::kQKrOff + r * S::kKrRow;
 #pragma unroll
           for (int i = 0; i < kRr; ++i) {
             const int at = DR == 32 ? (i ^ ((r >> 1) & 3)) : (i ^ (r & 7));
-            *reinterpret_cast<uint4*>(dst + at * 16) = v[kTm + i];
+            *reinterpret_cast<uint4*>(dst + at * 16) = r_piece(i);
           }
           fence_proxy_async_smem();
         }
@@ -599,13 +643,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       tc_fence_before();
       mbar_arrive(q_ready);
-      return w;
+      sc += QST;
+      return true;
     };
     bool have = walk.next(g);
     if (!have && r == 0) p.part_desc[2 * blockIdx.x] = make_int4(0, 0, kPartEmpty, 0);
     Row w{};
-    if (have) w = load_row(g);
-    while (have) {
+    if (have) ok = load_row(g, w);
+    while (ok && have) {
       float m_run = -INFINITY, l_run = 0.f;
       BlockPos<BN> pos(p, g.kb0);
       for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, pos.step(p)) {
@@ -704,7 +749,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ov[i] = __float_as_uint(__uint_as_float(ov[i]) * alpha);
               tmem_st32(tmem + t_lane + S::kTmemO + c * 32, ov);
             }
-            tmem_wait_st();
           }
         }
 #pragma unroll
@@ -717,6 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
 
       if (!ok) break;
+      sc += g.kb1 - g.kb0;
       // The next segment's Q first, so that its scores are computed while this
       // one's O is written.
       const Row d = w;
@@ -725,13 +770,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int row0 = g.st.q0 * p.heads + d.tile0;
       const bool many = static_cast<long long>(g.all - g.kb1) * BN > 8 * share;
       have = walk.next(g);
-      if (have) w = load_row(g);
+      if (have) ok = load_row(g, w);
       // O: finished rows as bf16, a cut tile's as fp32 partial rows, stored as
       // [4 columns][rows] so that a warp's stores are contiguous
-      if (!mbar_wait(pv_done, (it - 1) & 1, wc)) {
-        ok = false;
-        break;
-      }
+      ok = ok && mbar_wait(pv_done, (it - 1) & 1, wc);
+      if (!ok) break;
       tc_fence_after();
       const int slot = 2 * blockIdx.x + (starts ? 1 : 0);
       if (d.warp_ok) {
@@ -741,26 +784,24 @@ __global__ void __launch_bounds__(kThreads, 1)
                        (static_cast<size_t>(slot) * (DV / 4)) * kBM + r;
         uint4* dst = reinterpret_cast<uint4*>(p.o + d.grow * DC + vpart * DV);
 #pragma unroll 1
-        for (int c = 0; c < DV / 64; ++c) {
-          uint32_t ov[64];
-          tmem_ld32(tmem + t_lane + S::kTmemO + c * 64, *reinterpret_cast<uint32_t(*)[32]>(ov));
-          tmem_ld32(tmem + t_lane + S::kTmemO + c * 64 + 32,
-                    *reinterpret_cast<uint32_t(*)[32]>(ov + 32));
+        for (int c = 0; c < DV / 32; ++c) {
+          uint32_t ov[32];
+          tmem_ld32(tmem + t_lane + S::kTmemO + c * 32, ov);
           tmem_wait_ld();
           if (d.ok && whole) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4; ++i) {
               uint32_t x[4];
 #pragma unroll
               for (int k = 0; k < 4; ++k)
                 x[k] = pack_bf16x2(__uint_as_float(ov[8 * i + 2 * k]) * f,
                                    __uint_as_float(ov[8 * i + 2 * k + 1]) * f);
-              dst[c * 8 + i] = make_uint4(x[0], x[1], x[2], x[3]);
+              dst[c * 4 + i] = make_uint4(x[0], x[1], x[2], x[3]);
             }
           } else if (d.ok) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              part[(c * 16 + i) * kBM] =
+            for (int i = 0; i < 8; ++i)
+              part[(c * 8 + i) * kBM] =
                   make_float4(__uint_as_float(ov[4 * i]), __uint_as_float(ov[4 * i + 1]),
                               __uint_as_float(ov[4 * i + 2]), __uint_as_float(ov[4 * i + 3]));
           }
@@ -1013,6 +1054,13 @@ int launch_paged(const PagedAttnArgs& a) {
       !encode_map_2d_bf16(&tm_kr, a.kr, DR, rows, DR * 2ull, DR, k.box_rows,
                           DR == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
     return MLA_ERR_CUDA;
+  CUtensorMap tm_qc, tm_qr;  // boxes of 32 rows: short tiles fetch what they have
+  const unsigned long long q_rows = static_cast<unsigned long long>(a.total) * a.heads;
+  if (!encode_map_2d_bf16(&tm_qc, a.q_c, DC, q_rows, DC * 2ull, 64, 32,
+                          CU_TENSOR_MAP_SWIZZLE_128B) ||
+      !encode_map_2d_bf16(&tm_qr, a.q_r, DR, q_rows, DR * 2ull, DR, 32,
+                          DR == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
+    return MLA_ERR_CUDA;
   auto kern = paged_attn_kernel<DC, DR, CL>;
   // resident CTAs of this instance (one per SM, whole clusters), asked once
   static int resident = 0;
@@ -1041,8 +1089,6 @@ int launch_paged(const PagedAttnArgs& a) {
     }
     resident = n * CL < kMaxCtas ? n * CL : kMaxCtas / CL * CL;
   }
-  k.q_c = static_cast<const __nv_bfloat16*>(a.q_c);
-  k.q_r = static_cast<const __nv_bfloat16*>(a.q_r);
   k.q_start = a.q_start;
   k.table = a.table;
   k.lens = a.lens;
@@ -1074,7 +1120,7 @@ int launch_paged(const PagedAttnArgs& a) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, tm_c, tm_kr, k);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, tm_c, tm_kr, tm_qc, tm_qr, k);
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     set_last_cuda_error(e);
