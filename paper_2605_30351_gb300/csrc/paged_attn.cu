@@ -51,12 +51,13 @@ constexpr float kRescaleLog2 = 8.0f;
 constexpr int kMaxCtas = 152;  // the workspace holds two partial tiles for each
 constexpr int kJoinThreads = 512;
 constexpr int kJoinGrid = kMaxCtas;
-constexpr int kJoinCols = 16;      // columns of a warp's join item (of 32 rows)
-constexpr int kJoinLongRows = 2;   // rows of a block's item where many shares cut the tile
+constexpr int kJoinCols = 16;  // columns of a warp's join item of 32 rows
 
 template <int DC, int DR>
 struct PagedShape {
-  static constexpr int BN = DC >= 256 ? 64 : 128;  // keys per block
+  // Keys per block: a score MMA of 64 keys takes the time of one of 128 (about 70
+  // clocks a step of 16 values: reading A bounds it), so 64 only where 128 do not fit
+  static constexpr int BN = DC > 256 ? 64 : 128;
   static constexpr int DV = DC > 256 ? 256 : DC;   // output columns per CTA
   static constexpr int DK = DC + DR;
   static constexpr int kSplit = DC / DV;           // CTAs that share a row tile
@@ -106,7 +107,7 @@ struct PagedK {
   __nv_bfloat16* o;
   float* part_o;
   float2* part_ml;
-  int4* part_desc;  // first row in o, rows, kPart*, 1 = many shares cut the tile
+  int4* part_desc;  // first row in o, rows, kPart*, 1 = row after row, 2 = and many shares
   int total, heads, seqs, pages, page_tokens, max_pages, block;
   // Key blocks never straddle a group of `group` tokens: BN tokens (per_group
   // whole pages) where the pages divide a block, else one page.
@@ -115,6 +116,12 @@ struct PagedK {
   float scale_log2;
   int* status;
 };
+
+// Partial rows lie as [4 columns][128 rows], which a warp (a lane per row) writes in
+// full lines, except those of short tiles (up to 32 rows) and of tiles that many
+// shares cut: they lie row after row, as the join reads them.
+constexpr int kFewRows = 32;
+constexpr int kManyShares = 8;
 
 // part_desc.z: the slot holds a partial tile, that ends its tile; the CTA's share
 // is empty (a chain of partial tiles passes over it)
@@ -497,13 +504,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         BlockPos<BN> pos(p, g.kb0);
         for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, ++sc, pos.step(p)) {
           const int st = sc % NST;
-          // S's previous contents have been read, and the keys have landed
-          if (it >= 1) ok = mbar_wait(s_free, (it - 1) & 1, wc);
-          ok = ok && mbar_wait(&kv_full[st], (sc / NST) & 1, wc);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
           uint8_t* kv = sKV + st * S::kTileBytes;
           const int valid = max(0, min(pos.rows(p), g.st.len - pos.token(p)));
+          ok = __all_sync(0xffffffffu, mbar_wait(&kv_full[st], (sc / NST) & 1, wc));
+          if (!ok) break;
           if (valid < BN) {
             const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
             for (int cb = 0; cb < DC / 64; ++cb)
@@ -512,6 +516,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             fence_proxy_async_smem();
             __syncwarp();
           }
+          // S's previous contents have been read
+          if (it >= 1) ok = __all_sync(0xffffffffu, mbar_wait(s_free, (it - 1) & 1, wc));
+          if (!ok) break;
           if (lane == 0) {
             tc_fence_after();
             const uint32_t ka = smem_u32(kv);
@@ -768,7 +775,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool starts = g.kb0 == 0, stops = g.kb1 == g.all, whole = starts && stops;
       const int n_rows = max(0, min(kBM, g.st.n * p.heads - d.tile0));
       const int row0 = g.st.q0 * p.heads + d.tile0;
-      const bool many = static_cast<long long>(g.all - g.kb1) * BN > 8 * share;
+      const bool many = static_cast<long long>(g.all) * BN > kManyShares * share;
+      const bool by_row = many || n_rows <= kFewRows;
       have = walk.next(g);
       if (have) ok = load_row(g, w);
       // O: finished rows as bf16, a cut tile's as fp32 partial rows, stored as
@@ -780,9 +788,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (d.warp_ok) {
         // a row that saw no key is 0; a NaN sum stays one
         const float f = l_run == 0.f ? 0.f : 1.f / l_run;
-        float4* part = reinterpret_cast<float4*>(p.part_o) +
-                       (static_cast<size_t>(slot) * (DV / 4)) * kBM + r;
-        uint4* dst = reinterpret_cast<uint4*>(p.o + d.grow * DC + vpart * DV);
+        float* part = p.part_o + static_cast<size_t>(slot) * DV * kBM;
+        __nv_bfloat16* dst = p.o + d.grow * DC + vpart * DV;
 #pragma unroll 1
         for (int c = 0; c < DV / 32; ++c) {
           uint32_t ov[32];
@@ -790,18 +797,23 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_wait_ld();
           if (d.ok && whole) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t x[4];
+            for (int i = 0; i < 2; ++i) {
+              uint32_t x[8];
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                x[k] = pack_bf16x2(__uint_as_float(ov[8 * i + 2 * k]) * f,
-                                   __uint_as_float(ov[8 * i + 2 * k + 1]) * f);
-              dst[c * 4 + i] = make_uint4(x[0], x[1], x[2], x[3]);
+              for (int k = 0; k < 8; ++k)
+                x[k] = pack_bf16x2(__uint_as_float(ov[16 * i + 2 * k]) * f,
+                                   __uint_as_float(ov[16 * i + 2 * k + 1]) * f);
+              *reinterpret_cast<uint4*>(dst + c * 32 + i * 16) = make_uint4(x[0], x[1], x[2], x[3]);
+              *reinterpret_cast<uint4*>(dst + c * 32 + i * 16 + 8) =
+                  make_uint4(x[4], x[5], x[6], x[7]);
             }
+          } else if (d.ok && by_row) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st_global_32(part + r * DV + c * 32 + i * 8, ov + 8 * i);
           } else if (d.ok) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              part[(c * 8 + i) * kBM] =
+              reinterpret_cast<float4*>(part)[(c * 8 + i) * kBM + r] =
                   make_float4(__uint_as_float(ov[4 * i]), __uint_as_float(ov[4 * i + 1]),
                               __uint_as_float(ov[4 * i + 2]), __uint_as_float(ov[4 * i + 3]));
           }
@@ -812,7 +824,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!whole && r == 0)
         p.part_desc[slot] =
-            make_int4(row0, n_rows, kPartHeld | (stops ? kPartEnds : 0), many ? 1 : 0);
+            make_int4(row0, n_rows, kPartHeld | (stops ? kPartEnds : 0), many ? 2 : by_row);
     }
   }
 
@@ -828,23 +840,24 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Joins the partial rows of tiles that several shares cut: o = sum_k 2^(m_k - M)
 // O_k over the same of l_k, in the shares' order. Every block finds the list of
-// work for itself: tiles that some CTA begins and does not end. Usually few shares
-// cut a tile, and a warp takes 32 rows x 16 columns of it, a lane per row. Where
-// many do (few rows, long streams: flagged by the CTA that begins the tile) a block
-// takes two rows and its threads split the chain.
+// work for itself: tiles that some CTA begins and does not end. A warp takes 32 rows
+// x 16 columns, a lane per row; one row of a tile that lies row after row; and
+// where many shares cut the tile (long streams) a block takes one row, each of its
+// warps every 16th partial row.
 template <int DC, int DV, int CL>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(kJoinThreads, 1)
     paged_join_kernel(const float* part_o, const float2* part_ml, const int4* part_desc,
                       __nv_bfloat16* o, int ctas, long long out_rows) {
   constexpr int kSplit = DC / DV, kWarps = kJoinThreads / 32, kCg = DV / 4;
   constexpr int kGroups = DV / kJoinCols;
-  __shared__ int4 desc[kMaxCtas];  // slots 1: tiles that begin
-  __shared__ int flags[kMaxCtas];  // slots 0: what follows
+  constexpr int kV = (DV + 127) / 128;  // 4-column pieces of a row per lane
+  __shared__ int4 desc[kMaxCtas];       // slots 1: tiles that begin
+  __shared__ int flags[kMaxCtas];       // slots 0: what follows
   // prefix sums of the work: warps' items in the low half, blocks' in the high one
   __shared__ int items[kMaxCtas + 1];
   __shared__ int sums[8];
-  __shared__ float weight[kMaxCtas * kJoinLongRows], norm[kJoinLongRows];
-  __shared__ float4 red[kJoinThreads];
+  __shared__ float row_m[kWarps], row_l[kWarps];
+  __shared__ __align__(16) float row_o[kWarps][DV];
   grid_dep_sync();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int cnt = 0;
@@ -854,8 +867,7 @@ __global__ void __launch_bounds__(kJoinThreads)
     desc[threadIdx.x] = d;
     if ((d.z & kPartHeld) && d.x >= 0 && d.y > 0 && d.y <= kBM &&
         d.x + static_cast<long long>(d.y) <= out_rows)
-      cnt = d.w ? ((d.y + kJoinLongRows - 1) / kJoinLongRows) << 16
-                : (d.y + 31) / 32 * kGroups;
+      cnt = d.w == 2 ? d.y << 16 : (d.w == 1 ? d.y : (d.y + 31) / 32 * kGroups);
   }
   if (warp < 5) {
 #pragma unroll
@@ -899,12 +911,79 @@ __global__ void __launch_bounds__(kJoinThreads)
     }
     return (ctas - 1 - i) / CL + 1;
   };
+  auto slot_of = [&](int i, int k) { return k == 0 ? 2 * i + 1 : 2 * (i + k * CL); };
+  auto holds = [&](int i, int k) { return k == 0 || (flags[i + k * CL] & kPartHeld); };
 
-  const int short_items = items[ctas] & 0xffff, long_items = items[ctas] >> 16;
-  for (int it = blockIdx.x + gridDim.x * warp; it < short_items; it += gridDim.x * kWarps) {
+  // One row of tile i, partial rows first, first + step, ... of its chain: maximum,
+  // sum and the lane's columns 4 (lane + 32 c).
+  auto row_part = [&](int i, int row, int n, int first, int step, float& m, float& l,
+                      float4 (&acc)[kV]) {
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int c = 0; c < kV; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int base = first; base < n; base += 32 * step) {
+      const int k = base + lane * step;
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (k < n && holds(i, k)) ml = part_ml[slot_of(i, k) * kBM + row];
+      float mx = ml.x;
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+      const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
+      const float a = ex2_approx(m - ref), w = ex2_approx(ml.x - ref);
+      float wl = w * ml.y;
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1) wl += __shfl_xor_sync(0xffffffffu, wl, s);
+      m = m_new;
+      l = l * a + wl;
+#pragma unroll
+      for (int c = 0; c < kV; ++c) {
+        acc[c].x *= a;
+        acc[c].y *= a;
+        acc[c].z *= a;
+        acc[c].w *= a;
+      }
+      const int cnt = min(32, (n - base + step - 1) / step);
+#pragma unroll 8
+      for (int t = 0; t < cnt; ++t) {
+        const float wt = __shfl_sync(0xffffffffu, w, t);
+        const float4* src = reinterpret_cast<const float4*>(
+            part_o + (static_cast<size_t>(slot_of(i, base + t * step)) * kBM + row) * DV);
+#pragma unroll
+        for (int c = 0; c < kV; ++c)
+          if (lane + 32 * c < kCg) {
+            const float4 v = src[lane + 32 * c];
+            const bool some = wt != 0.f;  // an empty share's slot may hold anything
+            acc[c].x += some ? wt * v.x : 0.f;
+            acc[c].y += some ? wt * v.y : 0.f;
+            acc[c].z += some ? wt * v.z : 0.f;
+            acc[c].w += some ? wt * v.w : 0.f;
+          }
+      }
+    }
+  };
+  auto out_row = [&](int i, int row) {
+    return o + (static_cast<size_t>(desc[i].x) + row) * DC + (kSplit > 1 ? i % CL : 0) * DV;
+  };
+
+  const int warp_items = items[ctas] & 0xffff, block_items = items[ctas] >> 16;
+  for (int it = blockIdx.x + gridDim.x * warp; it < warp_items; it += gridDim.x * kWarps) {
     const int i = tile_of(it, 0), n = chain_of(i);
     const int4 d = desc[i];
     const int sub = it - (items[i] & 0xffff);
+    if (d.w == 1) {
+      float m, l;
+      float4 acc[kV];
+      row_part(i, sub, n, 0, 1, m, l, acc);
+      const float f = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int c = 0; c < kV; ++c)
+        if (lane + 32 * c < kCg)
+          reinterpret_cast<uint2*>(out_row(i, sub))[lane + 32 * c] =
+              make_uint2(pack_bf16x2(acc[c].x * f, acc[c].y * f),
+                         pack_bf16x2(acc[c].z * f, acc[c].w * f));
+      continue;
+    }
     const int rb = sub / kGroups, cg0 = (sub - rb * kGroups) * (kJoinCols / 4);
     const int row = rb * 32 + lane;
     const bool ok = row < d.y;
@@ -918,11 +997,9 @@ __global__ void __launch_bounds__(kJoinThreads)
       float4 v[4][4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int kk = min(k0 + k, n - 1);
-        const int sl = kk == 0 ? 2 * i + 1 : 2 * (i + kk * CL);
+        const int kk = min(k0 + k, n - 1), sl = slot_of(i, kk);
         ml[k] = part_ml[sl * kBM + row];
-        if (!ok || k0 + k >= n || (kk > 0 && !(flags[i + kk * CL] & kPartHeld)))
-          ml[k] = make_float2(-INFINITY, 0.f);
+        if (!ok || k0 + k >= n || !holds(i, kk)) ml[k] = make_float2(-INFINITY, 0.f);
 #pragma unroll
         for (int c = 0; c < 4; ++c)
           v[k][c] = reinterpret_cast<const float4*>(
@@ -930,8 +1007,8 @@ __global__ void __launch_bounds__(kJoinThreads)
       }
       const float m_new =
           fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
-      const float base = m_new == -INFINITY ? 0.f : m_new;
-      const float a = ex2_approx(m - base);
+      const float ref = m_new == -INFINITY ? 0.f : m_new;
+      const float a = ex2_approx(m - ref);
       m = m_new;
       l *= a;
 #pragma unroll
@@ -943,7 +1020,7 @@ __global__ void __launch_bounds__(kJoinThreads)
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float b = ex2_approx(ml[k].x - base);
+        const float b = ex2_approx(ml[k].x - ref);
         if (b != 0.f) {
           l += ml[k].y * b;
 #pragma unroll
@@ -957,10 +1034,8 @@ __global__ void __launch_bounds__(kJoinThreads)
       }
     }
     if (ok) {
-      const int vpart = kSplit > 1 ? i % CL : 0;
       const float f = l == 0.f ? 0.f : 1.f / l;
-      uint4* dst = reinterpret_cast<uint4*>(o + (static_cast<size_t>(d.x) + row) * DC +
-                                            vpart * DV + cg0 * 4);
+      uint4* dst = reinterpret_cast<uint4*>(out_row(i, row) + cg0 * 4);
 #pragma unroll
       for (int c = 0; c < 2; ++c)
         dst[c] = make_uint4(pack_bf16x2(acc[2 * c].x * f, acc[2 * c].y * f),
@@ -970,71 +1045,33 @@ __global__ void __launch_bounds__(kJoinThreads)
     }
   }
 
-  for (int it = blockIdx.x; it < long_items; it += gridDim.x) {
-    const int i = tile_of(it, 16), n = chain_of(i);
-    const int4 d = desc[i];
-    const int row0 = (it - (items[i] >> 16)) * kJoinLongRows;
-    const int nr = min(kJoinLongRows, d.y - row0);
-    auto slot = [&](int k) { return k == 0 ? 2 * i + 1 : 2 * (i + k * CL); };
-    auto held = [&](int k) { return k == 0 || (flags[i + k * CL] & kPartHeld); };
-    if (warp < nr) {  // weights: a warp per row
-      float m = -INFINITY;
-#pragma unroll 5
-      for (int k = lane; k < n; k += 32) {
-        const float x = part_ml[slot(k) * kBM + row0 + warp].x;
-        m = fmaxf(m, held(k) ? x : -INFINITY);
-      }
+  for (int it = blockIdx.x; it < block_items; it += gridDim.x) {
+    const int i = tile_of(it, 16), n = chain_of(i), row = it - (items[i] >> 16);
+    float m, l;
+    float4 acc[kV];
+    row_part(i, row, n, warp, kWarps, m, l, acc);
 #pragma unroll
-      for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
-      const float base = m == -INFINITY ? 0.f : m;
-      float l = 0.f;
-#pragma unroll 5
-      for (int k = lane; k < n; k += 32) {
-        const float2 ml = part_ml[slot(k) * kBM + row0 + warp];
-        const float wt = held(k) ? ex2_approx(ml.x - base) : 0.f;
-        if (wt != 0.f) l += wt * ml.y;  // an empty share's slot may hold anything
-        weight[k * kJoinLongRows + warp] = wt;
-      }
-#pragma unroll
-      for (int s = 16; s > 0; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
-      if (lane == 0) norm[warp] = l == 0.f ? 0.f : 1.f / l;
+    for (int c = 0; c < kV; ++c)
+      if (lane + 32 * c < kCg) reinterpret_cast<float4*>(row_o[warp])[lane + 32 * c] = acc[c];
+    if (lane == 0) {
+      row_m[warp] = m;
+      row_l[warp] = l;
     }
     __syncthreads();
-    const int pairs = nr * kCg;  // (4 columns, row), rows fastest
-    const int split = kJoinThreads / pairs;
-    const int ks = threadIdx.x / pairs, pr = threadIdx.x - ks * pairs;
-    const int cg = pr / nr, row = pr - cg * nr;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (ks < split) {
-#pragma unroll 8
-      for (int k = ks; k < n; k += split) {
-        const float wt = weight[k * kJoinLongRows + row];
-        const float4 v = reinterpret_cast<const float4*>(
-            part_o)[(static_cast<size_t>(slot(k)) * kCg + cg) * kBM + row0 + row];
-        const bool some = wt != 0.f;
-        acc.x += some ? wt * v.x : 0.f;
-        acc.y += some ? wt * v.y : 0.f;
-        acc.z += some ? wt * v.z : 0.f;
-        acc.w += some ? wt * v.w : 0.f;
+    if (threadIdx.x < DV) {
+      float top = row_m[0], sum = 0.f, v = 0.f;
+#pragma unroll
+      for (int w = 1; w < kWarps; ++w) top = fmaxf(top, row_m[w]);
+      const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float wt = ex2_approx(row_m[w] - ref);
+        sum += wt * row_l[w];
+        v += wt * row_o[w][threadIdx.x];
       }
-      red[threadIdx.x] = acc;
+      out_row(i, row)[threadIdx.x] = __float2bfloat16_rn(sum == 0.f ? 0.f : v / sum);
     }
-    __syncthreads();
-    if (ks == 0) {
-      for (int k = 1; k < split; ++k) {
-        const float4 v = red[k * pairs + pr];
-        acc.x += v.x;
-        acc.y += v.y;
-        acc.z += v.z;
-        acc.w += v.w;
-      }
-      const int vpart = kSplit > 1 ? i % CL : 0;
-      const float f = norm[row];
-      *reinterpret_cast<uint2*>(o + (static_cast<size_t>(d.x) + row0 + row) * DC + vpart * DV +
-                                cg * 4) =
-          make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
-    }
-    __syncthreads();  // weight, norm and red are the next item's
+    __syncthreads();  // the rows in shared memory are the next item's
   }
 }
 

@@ -264,6 +264,13 @@ __device__ __forceinline__ void bulk_wait_read_all() {
   asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 
+// One 32-byte store (a whole sector); the address 32-byte aligned.
+__device__ __forceinline__ void st_global_32(void* dst, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]),
+               "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
 // Writes one staged row of NCH 16-byte chunks (d holds them in order) so that
 // the eight threads of a quarter warp, which hold eight consecutive rows,
 // reach eight different bank groups: step j writes chunk j ^ m, m taken from
