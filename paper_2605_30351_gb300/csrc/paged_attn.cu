@@ -944,7 +944,7 @@ __global__ void __launch_bounds__(kJoinThreads, 1)
         acc[c].w *= a;
       }
       const int cnt = min(32, (n - base + step - 1) / step);
-#pragma unroll 8
+#pragma unroll 3
       for (int t = 0; t < cnt; ++t) {
         const float wt = __shfl_sync(0xffffffffu, w, t);
         const float4* src = reinterpret_cast<const float4*>(
