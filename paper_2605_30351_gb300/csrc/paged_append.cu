@@ -34,38 +34,68 @@ __global__ void __launch_bounds__(kThreads) paged_append_kernel(const AppendK p)
   if (blockIdx.x == 0) check_q_start(p.q_start, p.seqs, p.total, p.status);
   const int lane = threadIdx.x & 31;
   const int warps = gridDim.x * (kThreads / 32);
+  const int c16 = p.d_c / 8, m = p.d_r / 2;
   for (int t = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < p.total; t += warps) {
-    const int s = stream_of(p.q_start, p.seqs, t, lane);
-    const int q0 = __ldg(p.q_start + s), q1 = __ldg(p.q_start + s + 1);
-    const int len = __ldg(p.lens + s);
-    const long long a = static_cast<long long>(len) - (q1 - q0) + (t - q0);
-    const long long j = a / p.page_tokens;
-    int page = -1;
-    if (t >= q0 && t < q1 && q1 <= p.total && a >= 0 && j < p.max_pages)
-      page = __ldg(p.table + static_cast<size_t>(s) * p.max_pages + j);
-    if (page < 0 || page >= p.pages) {
-      if (lane == 0) record_status(p.status, MLA_ERR_RANGE);
-      continue;
-    }
-    const size_t row = static_cast<size_t>(page) * p.page_tokens + (a - j * p.page_tokens);
-    const int c16 = p.d_c / 8;
-    for (int i = lane; i < c16; i += 32)
-      p.c[row * c16 + i] = __ldg(p.c_new + static_cast<size_t>(t) * c16 + i);
-    const int m = p.d_r / 2;
+    // the row's first pieces and the first pair's angle are on their way while
+    // the token's place is found
+    const uint4* src = p.c_new + static_cast<size_t>(t) * c16;
     const __nv_bfloat16* x = p.kr_new + static_cast<size_t>(t) * p.d_r;
-    __nv_bfloat16* y = p.kr + row * p.d_r;
-    for (int i = lane; i < m; i += 32) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (lane < c16) v = __ldg(src + lane);
+    auto angle = [&](int i) {
       const int axis = p.axes == 1 || i < p.pairs_t ? 0 : (i < p.pairs_t + p.pairs_h ? 1 : 2);
       int co = __ldg(p.pos + static_cast<size_t>(t) * p.axes + axis);
       if (co < 0 || co >= p.rope_len) {
         record_status(p.status, MLA_ERR_RANGE);
         co = 0;
       }
-      const float2 cs = __ldg(p.rope + static_cast<size_t>(co) * m + i);
+      return __ldg(p.rope + static_cast<size_t>(co) * m + i);
+    };
+    float2 cs = make_float2(0.f, 0.f);
+    float a = 0.f, b = 0.f;
+    if (lane < m) {
+      cs = angle(lane);
+      a = __bfloat162float(x[HALF ? lane : 2 * lane]);
+      b = __bfloat162float(x[HALF ? lane + m : 2 * lane + 1]);
+    }
+    int s, q0, q1, len;
+    if (p.seqs <= 32) {  // every stream's numbers in one load, a lane per stream
+      const int q = lane <= p.seqs ? __ldg(p.q_start + min(lane, p.seqs)) : 0;
+      const int n = lane < p.seqs ? __ldg(p.lens + lane) : 0;
+      const unsigned le = __ballot_sync(0xffffffffu, lane < p.seqs && q <= t);
+      s = le ? 31 - __clz(le) : 0;
+      q0 = __shfl_sync(0xffffffffu, q, s);
+      q1 = s == 31 ? __ldg(p.q_start + 32) : __shfl_sync(0xffffffffu, q, (s + 1) & 31);
+      len = __shfl_sync(0xffffffffu, n, s);
+    } else {
+      s = stream_of(p.q_start, p.seqs, t, lane);
+      q0 = __ldg(p.q_start + s);
+      q1 = __ldg(p.q_start + s + 1);
+      len = __ldg(p.lens + s);
+    }
+    const long long place = static_cast<long long>(len) - (q1 - q0) + (t - q0);
+    const long long j = place / p.page_tokens;
+    int page = -1;
+    if (t >= q0 && t < q1 && q1 <= p.total && place >= 0 && j < p.max_pages)
+      page = __ldg(p.table + static_cast<size_t>(s) * p.max_pages + j);
+    if (page < 0 || page >= p.pages) {
+      if (lane == 0) record_status(p.status, MLA_ERR_RANGE);
+      continue;
+    }
+    const size_t row = static_cast<size_t>(page) * p.page_tokens + (place - j * p.page_tokens);
+    uint4* dst = p.c + row * c16;
+    if (lane < c16) dst[lane] = v;
+    for (int i = lane + 32; i < c16; i += 32) dst[i] = __ldg(src + i);
+    __nv_bfloat16* y = p.kr + row * p.d_r;
+    for (int i = lane; i < m; i += 32) {
       const int ia = HALF ? i : 2 * i, ib = HALF ? i + m : 2 * i + 1;
-      const float u = __bfloat162float(x[ia]), v = __bfloat162float(x[ib]);
-      y[ia] = __float2bfloat16_rn(u * cs.x - v * cs.y);
-      y[ib] = __float2bfloat16_rn(u * cs.y + v * cs.x);
+      if (i != lane) {
+        cs = angle(i);
+        a = __bfloat162float(x[ia]);
+        b = __bfloat162float(x[ib]);
+      }
+      y[ia] = __float2bfloat16_rn(a * cs.x - b * cs.y);
+      y[ib] = __float2bfloat16_rn(a * cs.y + b * cs.x);
     }
   }
 }

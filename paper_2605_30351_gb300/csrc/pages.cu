@@ -193,17 +193,29 @@ __global__ void __launch_bounds__(kMeta) resize_kernel(const Pool p, const int* 
   if (threadIdx.x == 0) plan[0] = n_copies;
 }
 
-// Copies pieces of pages in every layer: item i of *count, or of n where count
-// is null. A block per (item, layer) at a time.
+// n 16-byte pieces by the block: kFlight loads of a thread before its first store,
+// so that a unit of a page and layer (28 KB at 64 tokens of 224 values) is mostly in
+// flight at once.
+constexpr int kFlight = 4;
+
+__device__ __forceinline__ void copy_pieces(const uint4* src, uint4* dst, int n) {
+  for (int i0 = threadIdx.x; i0 < n; i0 += kCopy * kFlight) {
+    uint4 v[kFlight];
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k)
+      if (i0 + k * kCopy < n) v[k] = src[i0 + k * kCopy];
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k)
+      if (i0 + k * kCopy < n) dst[i0 + k * kCopy] = v[k];
+  }
+}
+
+// The first `rows` rows of page `from` to page `to`, one layer.
 __device__ __forceinline__ void copy_rows(const Pool& p, int from, int to, int rows, int layer) {
   const size_t base = static_cast<size_t>(layer) * p.pages;
-  const int nc = rows * p.c16, nk = rows * p.k16;
-  const uint4* cs = p.c + (base + from) * p.page_tokens * p.c16;
-  uint4* cd = p.c + (base + to) * p.page_tokens * p.c16;
-  for (int i = threadIdx.x; i < nc; i += kCopy) cd[i] = cs[i];
-  const uint4* ks = p.kr + (base + from) * p.page_tokens * p.k16;
-  uint4* kd = p.kr + (base + to) * p.page_tokens * p.k16;
-  for (int i = threadIdx.x; i < nk; i += kCopy) kd[i] = ks[i];
+  const size_t a = (base + from) * p.page_tokens, b = (base + to) * p.page_tokens;
+  copy_pieces(p.c + a * p.c16, p.c + b * p.c16, rows * p.c16);
+  copy_pieces(p.kr + a * p.k16, p.kr + b * p.k16, rows * p.k16);
 }
 
 __global__ void __launch_bounds__(kCopy) copy_plan_kernel(const Pool p, const int* plan) {
