@@ -155,7 +155,7 @@ __device__ __forceinline__ int tile_blocks(const PagedK& p, int n, int len, int 
 // last tile's keys (exact for a whole chunk and token by token, and within a
 // mask block for others) plus kTileCost for loading Q and writing O: prefix sums
 // in closed form, so a share's ends are found without walking the tiles.
-constexpr int kTileCost = 256;
+constexpr int kTileCost = 512;
 
 struct Cost {
   long long first, slope;  // slope in 1/256 keys per tile
