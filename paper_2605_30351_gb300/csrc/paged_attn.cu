@@ -39,16 +39,14 @@
 #include <cmath>
 
 #include "internal.h"
-#include "paged_common.cuh"
+#include "paged_attn.cuh"
 #include "ptx_sm103.cuh"
 
 namespace vmla {
 namespace {
 
-constexpr int kBM = 128;       // rows per tile = TMEM lanes
 constexpr int kThreads = 256;  // 8 warps (the fourth has no role)
 constexpr float kRescaleLog2 = 8.0f;
-constexpr int kMaxCtas = 152;  // the workspace holds two partial tiles for each
 constexpr int kJoinThreads = 512;
 constexpr int kJoinGrid = kMaxCtas;
 constexpr int kJoinCols = 16;  // columns of a warp's join item of 32 rows
@@ -90,233 +88,10 @@ struct PagedShape {
   static constexpr uint32_t kKrSbo = 8 * kKrRow;
   static constexpr uint32_t kIdescQK = idesc_bf16_f32(kBM, BN, false, false);
   static constexpr uint32_t kIdescPV = idesc_bf16_f32(kBM, DV, false, true);
-  // workspace of one launch: partial rows, their (maximum, sum), descriptors
-  static constexpr unsigned long long kPartBytes = 2ull * kMaxCtas * kBM * DV * 4;
-  static constexpr unsigned long long kMlBytes = 2ull * kMaxCtas * kBM * 8;
-  static constexpr unsigned long long kWorkspace = kPartBytes + kMlBytes + 2ull * kMaxCtas * 16;
   static_assert(kTmemQ + kQcTmem / 2 <= 512 && kStages >= 2 && kStages >= kQStages,
                 "TMEM and stages must fit");
   static_assert(kTileBytes % 1024 == 0 && kKrOff % 1024 == 0 && kQKrOff % 1024 == 0,
                 "swizzle-atom alignment");
-};
-
-struct PagedK {
-  const int* q_start;
-  const int* table;
-  const int* lens;
-  __nv_bfloat16* o;
-  float* part_o;
-  float2* part_ml;
-  int4* part_desc;  // first row in o, rows, kPart*, 1 = row after row, 2 = and many shares
-  int total, heads, seqs, pages, page_tokens, max_pages, block;
-  // Key blocks never straddle a group of `group` tokens: BN tokens (per_group
-  // whole pages) where the pages divide a block, else one page.
-  int group, blocks, per_group;
-  int box_rows;
-  float scale_log2;
-  int* status;
-};
-
-// Partial rows lie as [4 columns][128 rows], which a warp (a lane per row) writes in
-// full lines, except those of short tiles (up to 32 rows) and of tiles that many
-// shares cut: they lie row after row, as the join reads them.
-constexpr int kFewRows = 32;
-constexpr int kManyShares = 8;
-
-// part_desc.z: the slot holds a partial tile, that ends its tile; the CTA's share
-// is empty (a chain of partial tiles passes over it)
-constexpr int kPartHeld = 1, kPartEnds = 2, kPartEmpty = 4;
-
-struct Stream {
-  int q0, n, len;
-};
-
-__device__ __forceinline__ Stream stream_at(const PagedK& p, int s) {
-  Stream t{__ldg(p.q_start + s), __ldg(p.q_start + s + 1), __ldg(p.lens + s)};
-  const int q1 = t.n;
-  t.n = q1 - t.q0;
-  if (t.q0 < 0 || q1 < t.q0 || q1 > p.total || t.len < 0 ||
-      t.len > static_cast<long long>(p.max_pages) * p.page_tokens)
-    t.n = 0;
-  return t;
-}
-
-// Key blocks of row tile `tile` (TR rows) of a stream: what its last row, which
-// sees most, needs; at least one, so that rows that see nothing are written.
-template <int BN, int TR>
-__device__ __forceinline__ int tile_blocks(const PagedK& p, int n, int len, int tile) {
-  const int last = min(n * p.heads, (tile + 1) * TR) - 1;
-  const int keys = visible_keys(len - n + last / p.heads, len, p.block);
-  const int whole = keys / p.group, rest = keys - whole * p.group;
-  return max(1, whole * p.blocks + (rest + BN - 1) / BN);
-}
-
-// Cost of a stream's row tiles in keys, as a straight line from the first to the
-// last tile's keys (exact for a whole chunk and token by token, and within a
-// mask block for others) plus kTileCost for loading Q and writing O: prefix sums
-// in closed form, so a share's ends are found without walking the tiles.
-constexpr int kTileCost = 512;
-
-struct Cost {
-  long long first, slope;  // slope in 1/256 keys per tile
-  int tiles;
-  __device__ long long before(int t) const {  // of tiles 0 .. t-1
-    return t * first + ((slope * (static_cast<long long>(t) * (t - 1) / 2)) >> 8);
-  }
-};
-
-template <int TR>
-__device__ __forceinline__ Cost cost_of(const PagedK& p, const Stream& st) {
-  Cost c{0, 0, 0};
-  if (st.n == 0) return c;
-  const int rows = st.n * p.heads;
-  c.tiles = (rows + TR - 1) / TR;
-  const int k1 = visible_keys(st.len - 1, st.len, p.block);
-  c.first = k1 + kTileCost;
-  if (c.tiles > 1) {
-    const int k0 = visible_keys(st.len - st.n + (TR - 1) / p.heads, st.len, p.block);
-    if (c.tiles <= 4096) {  // the products stay below 2^63
-      c.first = k0 + kTileCost;
-      c.slope = static_cast<long long>(__fdividef((k1 - k0) * 256.f, c.tiles - 1.f));
-    } else {
-      c.first = (static_cast<long long>(k0) + k1) / 2 + kTileCost;
-    }
-  }
-  return c;
-}
-
-struct Place {
-  int s, tile, off;  // stream, row tile, key block
-};
-
-// The shares' ends: place of share id's first block and of the one after its
-// last. Every thread of the block calls it; scratch: 8 long longs and out: two
-// Places in shared memory. Three warps look for each end, all streams among their
-// 96 threads: one search's latency, not two, is part of every call. Returns the
-// cost of a share.
-template <int BN, int TR>
-__device__ __forceinline__ long long find_share(const PagedK& p, int id, int groups,
-                                                long long* scratch, Place* out) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int e = warp / 3;  // which end; the other warps only wait
-  const int per = (p.seqs + 95) / 96;
-  const int s0 = (threadIdx.x - e * 96) * per;
-  long long mine = 0;
-  Stream st{0, 0, 0};
-  Cost c{0, 0, 0};
-  if (e < 2)
-    for (int k = 0; k < per; ++k)
-      if (s0 + k < p.seqs) {
-        st = stream_at(p, s0 + k);
-        c = cost_of<TR>(p, st);
-        mine += c.before(c.tiles);
-      }
-  long long x = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, d);
-    if (lane >= d) x += y;
-  }
-  if (lane == 31 && e < 2) scratch[warp] = x;
-  if (threadIdx.x < 2) out[threadIdx.x] = Place{p.seqs, 0, 0};  // the end of the work
-  __syncthreads();
-  const long long total = scratch[0] + scratch[1] + scratch[2];
-  const int active = static_cast<int>(min(static_cast<long long>(groups), (total + BN - 1) / BN));
-  if (id < active && e < 2) {
-    long long base = x - mine;
-    for (int w = 3 * e; w < warp; ++w) base += scratch[w];
-    // total * (id + e) / active: in 32 bits where it fits (a 64-bit division is a
-    // noticeable part of a short call), else without the product's overflow
-    long long u;
-    if (total < (1 << 24)) {
-      u = static_cast<unsigned>(total) * (id + e) / static_cast<unsigned>(active);
-    } else {
-      const long long q = total / active, r = total - q * active;
-      u = q * (id + e) + r * (id + e) / active;
-    }
-    if (u >= base && u < base + mine) {
-      long long rem = u - base;
-      int s = s0;
-      if (per > 1)
-        for (; s < p.seqs; ++s) {
-          st = stream_at(p, s);
-          c = cost_of<TR>(p, st);
-          const long long all = c.before(c.tiles);
-          if (rem < all) break;
-          rem -= all;
-        }
-      if (s < p.seqs) {
-        int lo = 0, hi = c.tiles - 1;  // the last tile that begins at or before rem
-        while (lo < hi) {
-          const int mid = (lo + hi + 1) / 2;
-          if (c.before(mid) <= rem)
-            lo = mid;
-          else
-            hi = mid - 1;
-        }
-        const long long at = c.before(lo);
-        const int blocks = tile_blocks<BN, TR>(p, st.n, st.len, lo);
-        const int off = static_cast<int>(
-            static_cast<float>(rem - at) *
-            __fdividef(static_cast<float>(blocks), static_cast<float>(c.before(lo + 1) - at)));
-        out[e] = Place{s, lo, min(off, blocks - 1)};
-      }
-    }
-  }
-  __syncthreads();
-  return active > 0 ? static_cast<long long>(__fdividef(static_cast<float>(total), active)) : 0;
-}
-
-// Walks a share segment by segment: a segment is a run of key blocks of one row
-// tile. Every role of the CTA walks it for itself.
-struct Segment {
-  Stream st;
-  int s, tile;
-  int kb0, kb1, all;   // key blocks [kb0, kb1) of the tile's `all`
-};
-
-template <int BN, int TR>
-struct Walk {
-  const PagedK& p;
-  Stream st;
-  Place at, end;
-  __device__ Walk(const PagedK& k, const Place* ends) : p(k), at(ends[0]), end(ends[1]) {
-    st = at.s < p.seqs ? stream_at(p, at.s) : Stream{0, 0, 0};
-  }
-  __device__ bool next(Segment& g) {
-    while (at.s < p.seqs && at.tile * TR >= st.n * p.heads) {  // a stream with new tokens
-      at = Place{at.s + 1, 0, 0};
-      if (at.s < p.seqs) st = stream_at(p, at.s);
-    }
-    if (at.s >= p.seqs || at.s > end.s) return false;
-    const bool last = at.s == end.s && at.tile == end.tile;
-    if (at.s == end.s && (at.tile > end.tile || (last && at.off >= end.off))) return false;
-    const int all = tile_blocks<BN, TR>(p, st.n, st.len, at.tile);
-    g.st = st;
-    g.s = at.s;
-    g.tile = at.tile;
-    g.kb0 = at.off;
-    g.kb1 = last ? end.off : all;
-    g.all = all;
-    at.off = 0;
-    ++at.tile;
-    return true;
-  }
-};
-
-// Place of key block kb: its first token, and the rows of its group from there.
-template <int BN>
-struct BlockPos {
-  int grp, sub;
-  __device__ BlockPos(const PagedK& p, int kb) : grp(kb / p.blocks), sub(kb % p.blocks) {}
-  __device__ int token(const PagedK& p) const { return grp * p.group + sub * BN; }
-  __device__ int rows(const PagedK& p) const { return min(BN, p.group - sub * BN); }
-  __device__ void step(const PagedK& p) {
-    if (++sub == p.blocks) {
-      sub = 0;
-      ++grp;
-    }
-  }
 };
 
 template <int DC, int DR, int CL>
@@ -1075,15 +850,17 @@ __global__ void __launch_bounds__(kJoinThreads, 1)
   }
 }
 
+template <int DC, int DV, int CL>
+int launch_join(const PagedK& k, int ctas, const PagedAttnArgs& a) {
+  return launch_pdl(paged_join_kernel<DC, DV, CL>, dim3(kJoinGrid), kJoinThreads, 0, a.stream,
+                    k.part_o, k.part_ml, k.part_desc, k.o, ctas,
+                    static_cast<long long>(a.total) * a.heads);
+}
+
 template <int DC, int DR, int CL>
 int launch_paged(const PagedAttnArgs& a) {
   using S = PagedShape<DC, DR>;
-  const bool divides = S::BN % a.page_tokens == 0;
-  PagedK k;
-  k.group = divides ? S::BN : a.page_tokens;
-  k.blocks = (k.group + S::BN - 1) / S::BN;
-  k.per_group = divides ? S::BN / a.page_tokens : 1;
-  k.box_rows = divides ? a.page_tokens : S::BN;
+  const PagedK k = paged_params(a, S::BN, S::DV);
   CUtensorMap tm_c, tm_kr;
   const unsigned long long rows = static_cast<unsigned long long>(a.pages) * a.page_tokens;
   if (!encode_map_2d_bf16(&tm_c, a.c, DC, rows, DC * 2ull, 64, k.box_rows,
@@ -1126,23 +903,6 @@ int launch_paged(const PagedAttnArgs& a) {
     }
     resident = n * CL < kMaxCtas ? n * CL : kMaxCtas / CL * CL;
   }
-  k.q_start = a.q_start;
-  k.table = a.table;
-  k.lens = a.lens;
-  k.o = static_cast<__nv_bfloat16*>(a.o);
-  char* ws = static_cast<char*>(a.workspace);
-  k.part_o = reinterpret_cast<float*>(ws);
-  k.part_ml = reinterpret_cast<float2*>(ws + S::kPartBytes);
-  k.part_desc = reinterpret_cast<int4*>(ws + S::kPartBytes + S::kMlBytes);
-  k.total = a.total;
-  k.heads = a.heads;
-  k.seqs = a.seqs;
-  k.pages = a.pages;
-  k.page_tokens = a.page_tokens;
-  k.max_pages = a.max_pages;
-  k.block = a.causal_block;
-  k.scale_log2 = a.scale_log2;
-  k.status = a.status;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(resident);
   cfg.blockDim = dim3(kThreads);
@@ -1163,9 +923,7 @@ int launch_paged(const PagedAttnArgs& a) {
     set_last_cuda_error(e);
     return MLA_ERR_CUDA;
   }
-  return launch_pdl(paged_join_kernel<DC, S::DV, CL>, dim3(kJoinGrid), kJoinThreads, 0, a.stream,
-                    k.part_o, k.part_ml, k.part_desc, k.o, resident,
-                    static_cast<long long>(a.total) * a.heads);
+  return launch_join<DC, S::DV, CL>(k, resident, a);
 }
 
 // Streams of two row tiles and more on average: CTA pairs, which read each key
@@ -1193,25 +951,35 @@ int pick_dc(const PagedAttnArgs& a) {
   }
 }
 
-template <int DR>
-unsigned long long workspace_dc(int d_c) {
+}  // namespace
+
+unsigned long long paged_attention_workspace(int d_c, int d_r) {
+  if (d_r != 32 && d_r != 64) return 0;
   switch (d_c) {
-    case 64: return PagedShape<64, DR>::kWorkspace;
-    case 128: return PagedShape<128, DR>::kWorkspace;
-    case 192: return PagedShape<192, DR>::kWorkspace;
-    case 256: return PagedShape<256, DR>::kWorkspace;
-    case 512: return PagedShape<512, DR>::kWorkspace;
+    case 64:
+    case 128:
+    case 192:
+    case 256: return PartLayout(d_c).total;
+    case 512: return PartLayout(256).total;
     default: return 0;
   }
 }
 
-}  // namespace
-
-unsigned long long paged_attention_workspace(int d_c, int d_r) {
-  return d_r == 32 ? workspace_dc<32>(d_c) : (d_r == 64 ? workspace_dc<64>(d_c) : 0);
+int launch_paged_join(const PagedK& k, int ctas, const PagedAttnArgs& a) {
+  switch (a.d_c) {
+    case 64: return launch_join<64, 64, 1>(k, ctas, a);
+    case 128: return launch_join<128, 128, 1>(k, ctas, a);
+    case 192: return launch_join<192, 192, 1>(k, ctas, a);
+    case 256: return launch_join<256, 256, 1>(k, ctas, a);
+    default: return MLA_ERR_UNSUPPORTED;
+  }
 }
 
 int launch_paged_attention(const PagedAttnArgs& a) {
+  // Up to 16 rows a stream on average, as one token of 8 to 16 heads: the kernel of
+  // 16-row tiles
+  if (a.d_c <= 256 && static_cast<long long>(a.total) * a.heads <= 16ll * a.seqs)
+    return launch_paged_decode(a);
   return a.d_r == 32 ? pick_dc<32>(a) : pick_dc<64>(a);
 }
 
