@@ -719,21 +719,33 @@ __global__ void __launch_bounds__(kJoinThreads, 1)
         acc[c].w *= a;
       }
       const int cnt = min(32, (n - base + step - 1) / step);
-#pragma unroll 3
-      for (int t = 0; t < cnt; ++t) {
-        const float wt = __shfl_sync(0xffffffffu, w, t);
-        const float4* src = reinterpret_cast<const float4*>(
-            part_o + (static_cast<size_t>(slot_of(i, base + t * step)) * kBM + row) * DV);
+      // four rows at a time, all loads of a group in flight together (past the
+      // chain's end the last row again, at weight 0)
+#pragma unroll 1
+      for (int t0 = 0; t0 < cnt; t0 += 4) {
+        float4 v[4][kV];
 #pragma unroll
-        for (int c = 0; c < kV; ++c)
-          if (lane + 32 * c < kCg) {
-            const float4 v = src[lane + 32 * c];
-            const bool some = wt != 0.f;  // an empty share's slot may hold anything
-            acc[c].x += some ? wt * v.x : 0.f;
-            acc[c].y += some ? wt * v.y : 0.f;
-            acc[c].z += some ? wt * v.z : 0.f;
-            acc[c].w += some ? wt * v.w : 0.f;
+        for (int t = 0; t < 4; ++t) {
+          const float4* src = reinterpret_cast<const float4*>(
+              part_o +
+              (static_cast<size_t>(slot_of(i, base + min(t0 + t, cnt - 1) * step)) * kBM + row) *
+                  DV);
+#pragma unroll
+          for (int c = 0; c < kV; ++c)
+            if (lane + 32 * c < kCg) v[t][c] = src[lane + 32 * c];
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const float wt = __shfl_sync(0xffffffffu, w, t0 + t);
+          if (wt == 0.f) continue;  // an empty share's slot may hold anything
+#pragma unroll
+          for (int c = 0; c < kV; ++c) {
+            acc[c].x += wt * v[t][c].x;
+            acc[c].y += wt * v[t][c].y;
+            acc[c].z += wt * v[t][c].z;
+            acc[c].w += wt * v[t][c].w;
           }
+        }
       }
     }
   };

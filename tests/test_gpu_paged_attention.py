@@ -337,3 +337,51 @@ def test_refusals():
              q_start=torch.tensor([0, 1], dtype=torch.int32, device="cuda"))
     assert e.value.code == V.MLA_ERR_UNSUPPORTED
     call(q_c=p.q_c[:0], q_r=p.q_r[:0], o=o[:0])
+
+
+# ---------------------------------------------- streams of up to 16 rows on average
+@pytest.mark.parametrize("page", [8, 9, 15, 16, 24, 32, 48, 64, 96, 100, 128, 200, 1560])
+@pytest.mark.parametrize("d_c,d_r", [(192, 32), (64, 64)])
+def test_one_token_page_sizes(page, d_c, d_r):
+    run_check(Problem([1, 15, 16, 17, 129, 700, 3000], [1] * 7, page=page, d_c=d_c, d_r=d_r,
+                      heads=8, seed=page), 1)
+
+
+@pytest.mark.parametrize("d_c", [64, 128, 192, 256, 512])
+@pytest.mark.parametrize("d_r", [32, 64])
+@pytest.mark.parametrize("heads", [1, 5, 16])
+def test_one_token_widths(d_c, d_r, heads):
+    run_check(Problem([1000, 128, 0, 333], [1, 1, 0, 1], page=32, d_c=d_c, d_r=d_r, heads=heads),
+              0)
+
+
+@pytest.mark.parametrize("block", [0, 1, 3])
+def test_mostly_idle_streams(block):
+    """Few rows on average, and one stream with several tiles of 16 of them, more
+    new tokens than another one holds."""
+    new = [0] * 30
+    new[3], new[17], new[29] = 21, 5, 1
+    lens = [40] * 30
+    lens[3], lens[17], lens[29] = 800, 3, 260
+    run_check(Problem(lens, new, heads=12, page=16), block)
+
+
+def test_one_token_sharp_and_long():
+    p = Problem([20000, 64, 4097], [1, 1, 1], heads=16, gain=8.0, page=16, seed=11)
+    o = run_check(p, 1)
+    assert torch.equal(o, p.run(1))
+    p.workspace.fill_(255)
+    assert torch.equal(o, p.run(1))
+
+
+def test_one_token_bad_pages_count_as_zeros():
+    p = Problem([300, 200], [1, 1])
+    ref = p.run(1)
+    for bad in (-1, 10 ** 6, -2 ** 31):
+        keep = p.cache.table[0, 1].item()
+        p.cache.table[0, 1] = bad
+        o = p.run(1)
+        assert V.mla_device_status(clear=True) == V.MLA_ERR_RANGE
+        assert torch.isfinite(o).all() and torch.equal(o[1], ref[1])
+        p.cache.table[0, 1] = keep
+    assert torch.equal(p.run(1), ref)
