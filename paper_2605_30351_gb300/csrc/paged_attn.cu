@@ -65,10 +65,14 @@ struct PagedShape {
   static constexpr int kBoxes = DC / 64 + 1;       // boxes per page
   static constexpr int kQStages = kBM / BN;        // stages that Q takes
   // TMEM columns: S, P (bf16, two a column), O, and Q as far as it fits; the rest
-  // of Q stays in shared memory
+  // of Q stays in shared memory. Where everything fits (d_c up to 128) S has two
+  // buffers and P takes the place of the scores it came from, so that the next
+  // block's scores are there before this one's weights are: with little MMA work a
+  // block the softmax sets the pace.
+  static constexpr int kBufs = 2 * BN + DV + DK / 2 <= 512 ? 2 : 1;
   static constexpr int kTmemS = 0;
-  static constexpr int kTmemP = BN;
-  static constexpr int kTmemO = BN + BN / 2;
+  static constexpr int kTmemP = kBufs == 2 ? 0 : BN;
+  static constexpr int kTmemO = kBufs == 2 ? 2 * BN : BN + BN / 2;
   static constexpr int kTmemQ = kTmemO + DV;
   static constexpr bool kQrTmem = kTmemQ + DK / 2 <= 512;
   static constexpr int kQcFit = (512 - kTmemQ) * 2 / 64 * 64;
@@ -101,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                       const __grid_constant__ CUtensorMap tm_qc,
                       const __grid_constant__ CUtensorMap tm_qr, const PagedK p) {
   using S = PagedShape<DC, DR>;
-  constexpr int BN = S::BN, DV = S::DV, NST = S::kStages, QST = S::kQStages;
+  constexpr int BN = S::BN, DV = S::DV, NST = S::kStages, QST = S::kQStages, NB = S::kBufs;
   constexpr int TR = kBM * CL / S::kSplit;  // rows of a CTA's, or a pair's, tile
   constexpr uint16_t kPair = static_cast<uint16_t>((1u << CL) - 1u);
   static_assert(S::kSplit == 1 || CL == S::kSplit, "split tiles take a pair");
@@ -114,10 +118,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* kv_full = bars + 1;
   uint64_t* kv_empty = kv_full + NST;
   uint64_t* s_free = kv_empty + NST;
-  uint64_t* s_full = s_free + 1;
-  uint64_t* p_full = s_full + 1;
-  uint64_t* pv_done = p_full + 1;
-  uint64_t* mma_drain = pv_done + 1;  // [2]: one per issuing thread
+  uint64_t* s_full = s_free + 1;           // [NB] each: by the buffer of the block,
+  uint64_t* p_full = s_full + NB;          // so that a waiter one block behind still
+  uint64_t* pv_done = p_full + NB;         // finds the phase it waits for
+  uint64_t* mma_drain = pv_done + NB;      // [2]: one per issuing thread
   long long* scratch = reinterpret_cast<long long*>(mma_drain + 2);  // [8]
   Place* ends = reinterpret_cast<Place*>(scratch + 8);               // [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ends + 2);
@@ -134,9 +138,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&kv_empty[s], CL);
     }
     mbar_init(s_free, kBM);
-    mbar_init(s_full, 1);
-    mbar_init(p_full, kBM);
-    mbar_init(pv_done, 1);
+    for (int i = 0; i < NB; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_full[i], kBM);
+      mbar_init(&pv_done[i], 1);
+    }
     mbar_init(&mma_drain[0], 1);
     mbar_init(&mma_drain[1], 1);
     *abort_flag = 0;
@@ -174,6 +180,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   Segment g;
   bool ok = true;
   int it = 0;  // key blocks so far: the phases of the per-block barriers
+  auto phase = [](int block) { return static_cast<uint32_t>(block / NB) & 1u; };
   int sc = 0;  // ring stages so far, Q's included: the phases of kv_full, kv_empty
 
   if (warp < 4) {
@@ -291,13 +298,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             fence_proxy_async_smem();
             __syncwarp();
           }
-          // S's previous contents have been read
-          if (it >= 1) ok = __all_sync(0xffffffffu, mbar_wait(s_free, (it - 1) & 1, wc));
+          // S's previous contents have been read: the scores by the softmax, or with
+          // two buffers the weights that took their place by their PV
+          if (it >= NB)
+            ok = __all_sync(0xffffffffu,
+                            NB == 1 ? mbar_wait(s_free, (it - 1) & 1, wc)
+                                    : mbar_wait(&pv_done[it % NB], phase(it - NB), wc));
           if (!ok) break;
           if (lane == 0) {
             tc_fence_after();
             const uint32_t ka = smem_u32(kv);
-            const uint32_t d = tmem + S::kTmemS;
+            const uint32_t d = tmem + S::kTmemS + (it % NB) * BN;
 #pragma unroll
             for (int cb = 0; cb < DC / 64; ++cb)
 #pragma unroll
@@ -319,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 umma_ss(d, sdesc(qa + S::kQKrOff + k * 32, 16, S::kKrSbo, S::kKrSw), bd,
                         S::kIdescQK, 1u);
             }
-            umma_commit(s_full);
+            umma_commit(&s_full[it % NB]);
           }
           __syncwarp();
         }
@@ -336,21 +347,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         while (ok && walk.next(g)) {
           sc += QST;
           for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, ++sc) {
-            ok = mbar_wait(p_full, it & 1, wc);
+            ok = mbar_wait(&p_full[it % NB], phase(it), wc);
             if (!ok) break;
             tc_fence_after();
             const int st = sc % NST;
             const uint32_t va = smem_u32(sKV) + st * S::kTileBytes + vpart * (DV / 64) * S::kCBox;
 #pragma unroll
             for (int s = 0; s < BN / 16; ++s)
-              umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + s * 8,
+              umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + (it % NB) * BN + s * 8,
                       sdesc(va + s * 2048, S::kCBox, 1024, kSw128), S::kIdescPV,
                       (kb > g.kb0 || s > 0) ? 1u : 0u);
             if constexpr (CL == 1)
               umma_commit(&kv_empty[st]);
             else
               umma_commit_mc(&kv_empty[st], kPair);
-            umma_commit(pv_done);
+            umma_commit(&pv_done[it % NB]);
           }
         }
         if (!ok) {
@@ -436,28 +447,32 @@ __global__ void __launch_bounds__(kThreads, 1)
       float m_run = -INFINITY, l_run = 0.f;
       BlockPos<BN> pos(p, g.kb0);
       for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, pos.step(p)) {
-        if (!mbar_wait(s_full, it & 1, wc)) {
+        if (!mbar_wait(&s_full[it % NB], phase(it), wc)) {
           ok = false;
           break;
         }
         tc_fence_after();
         if (!w.warp_ok) {  // none of the warp's rows exists: keep the barriers going
-          mbar_arrive(s_free);
-          if (kb > g.kb0 && !mbar_wait(pv_done, (it - 1) & 1, wc)) {
-            ok = false;
-            break;
+          if constexpr (NB == 1) {
+            mbar_arrive(s_free);
+            if (kb > g.kb0 && !mbar_wait(pv_done, (it - 1) & 1, wc)) {
+              ok = false;
+              break;
+            }
           }
-          mbar_arrive(p_full);
+          mbar_arrive(&p_full[it % NB]);
           continue;
         }
         uint32_t sr[BN];
 #pragma unroll
         for (int c = 0; c < BN / 32; ++c)
-          tmem_ld32(tmem + t_lane + S::kTmemS + c * 32,
+          tmem_ld32(tmem + t_lane + S::kTmemS + (it % NB) * BN + c * 32,
                     *reinterpret_cast<uint32_t(*)[32]>(&sr[c * 32]));
         tmem_wait_ld();
-        tc_fence_before();
-        mbar_arrive(s_free);  // the next block's scores may land
+        if constexpr (NB == 1) {
+          tc_fence_before();
+          mbar_arrive(s_free);  // the next block's scores may land
+        }
         float sv[BN];
 #pragma unroll
         for (int c = 0; c < BN; ++c) sv[c] = __uint_as_float(sr[c]);
@@ -513,14 +528,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) f32x2_unpack(l4[i], l8[2 * i], l8[2 * i + 1]);
         l_run += ((l8[0] + l8[1]) + (l8[2] + l8[3])) + ((l8[4] + l8[5]) + (l8[6] + l8[7]));
-        if (kb > g.kb0) {
-          // the previous PV has read P and finished with O
-          if (!mbar_wait(pv_done, (it - 1) & 1, wc)) {
+        // the previous PV has read P (one buffer) and finished with O
+        const bool rescale = __any_sync(0xffffffffu, need);
+        if (kb > g.kb0 && (NB == 1 || rescale)) {
+          if (!mbar_wait(&pv_done[(it - 1) % NB], phase(it - 1), wc)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          if (__any_sync(0xffffffffu, need)) {
+          if (rescale) {
 #pragma unroll 1
             for (int c = 0; c < DV / 32; ++c) {
               uint32_t ov[32];
@@ -535,11 +551,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
 #pragma unroll
         for (int c = 0; c < BN / 64; ++c)
-          tmem_st32(tmem + t_lane + S::kTmemP + c * 32,
+          tmem_st32(tmem + t_lane + S::kTmemP + (it % NB) * BN + c * 32,
                     *reinterpret_cast<uint32_t(*)[32]>(&pk[c * 32]));
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(p_full);
+        mbar_arrive(&p_full[it % NB]);
       }
 
       if (!ok) break;
@@ -556,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (have) ok = load_row(g, w);
       // O: finished rows as bf16, a cut tile's as fp32 partial rows, stored as
       // [4 columns][rows] so that a warp's stores are contiguous
-      ok = ok && mbar_wait(pv_done, (it - 1) & 1, wc);
+      ok = ok && mbar_wait(&pv_done[(it - 1) % NB], phase(it - 1), wc);
       if (!ok) break;
       tc_fence_after();
       const int slot = 2 * blockIdx.x + (starts ? 1 : 0);
