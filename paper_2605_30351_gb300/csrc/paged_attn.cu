@@ -186,6 +186,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp < 4) {
     if (warp == 0) {
       // ------------------------------------------------------------ producer
+      const int page_shift = 31 - __clz(p.page_tokens);  // pages that divide a block
       auto acquire = [&]() {  // stage sc is free
         bool free = true;
         if (sc >= NST) {
@@ -198,6 +199,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       while (ok && walk.next(g)) {
         const int rows = g.st.n * p.heads;
+        // a lane per page of a block, looked up one block ahead of its copies
+        const int* table = p.table + static_cast<size_t>(g.s) * p.max_pages;
+        BlockPos<BN> pos(p, g.kb0);
+        auto boxes_at = [&](const BlockPos<BN>& at) {  // pages of a block that hold tokens
+          const int valid = min(at.rows(p), g.st.len - at.token(p));
+          return p.per_group == 1 ? (valid > 0 ? 1 : 0)
+                                  : (max(valid, 0) + p.page_tokens - 1) >> page_shift;
+        };
+        auto look_up = [&](const BlockPos<BN>& at) {
+          return lane < boxes_at(at) ? __ldg(table + at.grp * p.per_group + lane) : -1;
+        };
+        int page_ahead = look_up(pos);
         for (int q = 0; q < QST; ++q, ++sc) {
           ok = acquire();
           if (!ok) break;
@@ -222,12 +235,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         if (!ok) break;
-        const int* row = p.table + static_cast<size_t>(g.s) * p.max_pages;
-        BlockPos<BN> pos(p, g.kb0);
-        for (int kb = g.kb0; kb < g.kb1; ++kb, ++sc, pos.step(p)) {
-          const int valid = min(pos.rows(p), g.st.len - pos.token(p));
-          const int boxes =
-              p.per_group == 1 ? (valid > 0) : (max(valid, 0) + p.page_tokens - 1) / p.page_tokens;
+        for (int kb = g.kb0; kb < g.kb1; ++kb, ++sc) {
+          const int boxes = boxes_at(pos), sub = pos.sub, page_now = page_ahead;
+          pos.step(p);
+          if (kb + 1 < g.kb1) page_ahead = look_up(pos);
           ok = acquire();
           if (!ok) break;
           uint8_t* kv = sKV + (sc % NST) * S::kTileBytes;
@@ -239,13 +250,13 @@ __global__ void __launch_bounds__(kThreads, 1)
               mbar_arrive(full);
           }
           __syncwarp();
-          for (int bx = lane; bx < boxes * S::kBoxes; bx += 32) {
-            if (CL > 1 && (bx & 1) != crank) continue;
-            const int i = bx / S::kBoxes, cb = bx - i * S::kBoxes;
-            const int page = __ldg(row + pos.grp * p.per_group + i);
+          for (int b0 = 0; b0 < boxes * S::kBoxes; b0 += 32) {
+            const int bx = b0 + lane, i = bx / S::kBoxes, cb = bx - i * S::kBoxes;
+            const int page = __shfl_sync(0xffffffffu, page_now, i & 31);
+            if (i >= boxes || (CL > 1 && (bx & 1) != crank)) continue;
             int r = p.pages * p.page_tokens;  // past the pool: zeros
             if (page >= 0 && page < p.pages)
-              r = page * p.page_tokens + pos.sub * BN;
+              r = page * p.page_tokens + sub * BN;
             else
               record_status(p.status, MLA_ERR_RANGE);
             const bool is_c = cb < DC / 64;
@@ -393,8 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       w.ok = w.lrow < rows;
       w.warp_ok = __any_sync(0xffffffffu, w.ok);
       w.grow = static_cast<size_t>(sg.st.q0) * p.heads + (w.ok ? w.lrow : 0);
-      w.keys = w.ok ? visible_keys(sg.st.len - sg.st.n + w.lrow / p.heads, sg.st.len, p.block)
-                    : 0;
+      w.keys = w.ok ? keys_seen(p, sg.st.len - sg.st.n + p.by_heads(w.lrow), sg.st.len) : 0;
       const int slot = sc + (QST > 1 ? r / BN : 0), rr = QST > 1 ? r % BN : r;
       if (!mbar_wait(&kv_full[slot % NST], (slot / NST) & 1, wc)) return false;
       if (w.warp_ok) {

@@ -20,6 +20,24 @@ struct PartLayout {
         total(desc + 2ull * kMaxCtas * 16) {}
 };
 
+// What a short call pays for is the code that it runs for the first time, about 15
+// ns an instruction: divisions by the call's own numbers are prepared on the host.
+// n / d for 0 <= n < 2^31 and d >= 1: mul = floor(2^shift / d) + 1 with shift = 31 +
+// ceil(log2 d), so the error of n * mul / 2^shift, at most n / 2^shift, stays below
+// the next multiple of 1 / d.
+struct Div {
+  unsigned mul;
+  int shift;
+  __device__ __forceinline__ int operator()(int n) const {
+    return static_cast<int>((static_cast<unsigned long long>(n) * mul) >> shift);
+  }
+};
+inline Div div_by(int d) {
+  int s = 0;
+  while ((1ll << s) < d) ++s;
+  return Div{static_cast<unsigned>((1ull << (31 + s)) / static_cast<unsigned>(d) + 1), 31 + s};
+}
+
 struct PagedK {
   const int* q_start;
   const int* table;
@@ -33,6 +51,7 @@ struct PagedK {
   // whole pages) where the pages divide a block, else one page.
   int group, blocks, per_group;
   int box_rows;
+  Div by_heads, by_group, by_blocks, by_mask;  // by_mask: by `block`
   float scale_log2;
   int* status;
 };
@@ -61,13 +80,22 @@ __device__ __forceinline__ Stream stream_at(const PagedK& p, int s) {
   return t;
 }
 
+// Keys that the token at place a (it may be negative) of a stream of `held` tokens
+// sees.
+__device__ __forceinline__ int keys_seen(const PagedK& p, int a, int held) {
+  if (a < 0) return 0;
+  if (p.block == 0) return held;
+  const long long end = static_cast<long long>(p.by_mask(a) + 1) * p.block;
+  return end < held ? static_cast<int>(end) : held;
+}
+
 // Key blocks of row tile `tile` (TR rows) of a stream: what its last row, which
 // sees most, needs; at least one, so that rows that see nothing are written.
 template <int BN, int TR>
 __device__ __forceinline__ int tile_blocks(const PagedK& p, int n, int len, int tile) {
   const int last = min(n * p.heads, (tile + 1) * TR) - 1;
-  const int keys = visible_keys(len - n + last / p.heads, len, p.block);
-  const int whole = keys / p.group, rest = keys - whole * p.group;
+  const int keys = keys_seen(p, len - n + p.by_heads(last), len);
+  const int whole = p.by_group(keys), rest = keys - whole * p.group;
   return max(1, whole * p.blocks + (rest + BN - 1) / BN);
 }
 
@@ -91,10 +119,10 @@ __device__ __forceinline__ Cost cost_of(const PagedK& p, const Stream& st) {
   if (st.n == 0) return c;
   const int rows = st.n * p.heads;
   c.tiles = (rows + TR - 1) / TR;
-  const int k1 = visible_keys(st.len - 1, st.len, p.block);
+  const int k1 = keys_seen(p, st.len - 1, st.len);
   c.first = k1 + kTileCost;
   if (c.tiles > 1) {
-    const int k0 = visible_keys(st.len - st.n + (TR - 1) / p.heads, st.len, p.block);
+    const int k0 = keys_seen(p, st.len - st.n + p.by_heads(TR - 1), st.len);
     if (c.tiles <= 4096) {  // the products stay below 2^63
       c.first = k0 + kTileCost;
       c.slope = static_cast<long long>(__fdividef((k1 - k0) * 256.f, c.tiles - 1.f));
@@ -107,6 +135,8 @@ __device__ __forceinline__ Cost cost_of(const PagedK& p, const Stream& st) {
 
 struct Place {
   int s, tile, off;  // stream, row tile, key block
+  int all;           // the tile's key blocks
+  Stream st;
 };
 
 // The shares' ends: place of share id's first block and of the one after its
@@ -138,7 +168,7 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
     if (lane >= d) x += y;
   }
   if (lane == 31 && e < 2) scratch[warp] = x;
-  if (threadIdx.x < 2) out[threadIdx.x] = Place{p.seqs, 0, 0};  // the end of the work
+  if (threadIdx.x < 2) out[threadIdx.x].s = p.seqs;  // the end of the work
   __syncthreads();
   const long long total = scratch[0] + scratch[1] + scratch[2];
   const int active = static_cast<int>(min(static_cast<long long>(groups), (total + BN - 1) / BN));
@@ -179,7 +209,7 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
         const int off = static_cast<int>(
             static_cast<float>(rem - at) *
             __fdividef(static_cast<float>(blocks), static_cast<float>(c.before(lo + 1) - at)));
-        out[e] = Place{s, lo, min(off, blocks - 1)};
+        out[e] = Place{s, lo, min(off, blocks - 1), blocks, st};
       }
     }
   }
@@ -199,27 +229,39 @@ template <int BN, int TR>
 struct Walk {
   const PagedK& p;
   Stream st;
-  Place at, end;
-  __device__ Walk(const PagedK& k, const Place* ends) : p(k), at(ends[0]), end(ends[1]) {
-    st = at.s < p.seqs ? stream_at(p, at.s) : Stream{0, 0, 0};
+  int s, tile, off, all;  // all < 0: not known yet
+  int end_s, end_tile, end_off;
+  __device__ Walk(const PagedK& k, const Place* ends) : p(k) {
+    st = ends[0].st;  // the first segment needs no arithmetic: the search had it all
+    s = ends[0].s;
+    tile = ends[0].tile;
+    off = ends[0].off;
+    all = ends[0].all;
+    end_s = ends[1].s;
+    end_tile = ends[1].tile;
+    end_off = ends[1].off;
   }
   __device__ bool next(Segment& g) {
-    while (at.s < p.seqs && at.tile * TR >= st.n * p.heads) {  // a stream with new tokens
-      at = Place{at.s + 1, 0, 0};
-      if (at.s < p.seqs) st = stream_at(p, at.s);
+    if (s >= p.seqs) return false;
+    if (all < 0) {
+      while (tile * TR >= st.n * p.heads) {  // a stream with new tokens
+        if (++s >= p.seqs) return false;
+        st = stream_at(p, s);
+        tile = 0;
+      }
+      all = tile_blocks<BN, TR>(p, st.n, st.len, tile);
     }
-    if (at.s >= p.seqs || at.s > end.s) return false;
-    const bool last = at.s == end.s && at.tile == end.tile;
-    if (at.s == end.s && (at.tile > end.tile || (last && at.off >= end.off))) return false;
-    const int all = tile_blocks<BN, TR>(p, st.n, st.len, at.tile);
+    const bool last = s == end_s && tile == end_tile;
+    if (s > end_s || (s == end_s && tile > end_tile) || (last && off >= end_off)) return false;
     g.st = st;
-    g.s = at.s;
-    g.tile = at.tile;
-    g.kb0 = at.off;
-    g.kb1 = last ? end.off : all;
+    g.s = s;
+    g.tile = tile;
+    g.kb0 = off;
+    g.kb1 = last ? end_off : all;
     g.all = all;
-    at.off = 0;
-    ++at.tile;
+    off = 0;
+    all = -1;
+    ++tile;
     return true;
   }
 };
@@ -228,7 +270,7 @@ struct Walk {
 template <int BN>
 struct BlockPos {
   int grp, sub;
-  __device__ BlockPos(const PagedK& p, int kb) : grp(kb / p.blocks), sub(kb % p.blocks) {}
+  __device__ BlockPos(const PagedK& p, int kb) : grp(p.by_blocks(kb)), sub(kb - grp * p.blocks) {}
   __device__ int token(const PagedK& p) const { return grp * p.group + sub * BN; }
   __device__ int rows(const PagedK& p) const { return min(BN, p.group - sub * BN); }
   __device__ void step(const PagedK& p) {
@@ -263,6 +305,10 @@ inline PagedK paged_params(const PagedAttnArgs& a, int bn, int dv) {
   k.blocks = (k.group + bn - 1) / bn;
   k.per_group = divides ? bn / a.page_tokens : 1;
   k.box_rows = divides ? a.page_tokens : bn;
+  k.by_heads = div_by(k.heads);
+  k.by_group = div_by(k.group);
+  k.by_blocks = div_by(k.blocks);
+  k.by_mask = div_by(k.block > 0 ? k.block : 1);
   k.scale_log2 = a.scale_log2;
   k.status = a.status;
   return k;

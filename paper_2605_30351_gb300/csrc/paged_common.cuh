@@ -33,13 +33,4 @@ __device__ __forceinline__ void check_q_start(const int* q_start, int seqs, int 
   }
 }
 
-// Keys that the token at place a (it may be negative) of a stream of `held`
-// tokens sees.
-__device__ __forceinline__ int visible_keys(int a, int held, int block) {
-  if (a < 0) return 0;
-  if (block == 0) return held;
-  const long long end = static_cast<long long>(a / block + 1) * block;
-  return end < held ? static_cast<int>(end) : held;
-}
-
 }  // namespace vmla

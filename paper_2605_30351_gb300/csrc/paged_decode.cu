@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     auto keys_of = [&](int r) {
       return r < n_rows
-                 ? visible_keys(g.st.len - g.st.n + (row0 + r) / p.heads, g.st.len, p.block)
+                 ? keys_seen(p, g.st.len - g.st.n + p.by_heads(row0 + r), g.st.len)
                  : 0;
     };
     const int keys_a = keys_of(ra), keys_b = keys_of(rb);
