@@ -278,37 +278,51 @@ __global__ void __launch_bounds__(kCopy)
 // then the free places below n, then the pages that move.
 __global__ void __launch_bounds__(kMeta) pack_plan_kernel(const Pool p, int* plan) {
   grid_dep_sync();
-  __shared__ int sums[32];
+  __shared__ long long sums[32];
   int* where = plan + 2;
   int* holes = where + p.pages;
   int* movers = holes + p.pages;
+  // kRun consecutive pages a thread: one prefix sum for 8,192 pages and pass, of
+  // the pages in use (low half) and of those past n (high half) together
+  constexpr int kRun = 8;
+  auto used_at = [&](int first) {  // a bit for each of the thread's pages in use
+    unsigned m = 0;
+#pragma unroll
+    for (int k = 0; k < kRun; ++k)
+      if (first + k < p.pages && p.refs[first + k] > 0) m |= 1u << k;
+    return m;
+  };
   int n = 0;
-  for (int p0 = 0; p0 < p.pages; p0 += kMeta) {
-    const int pg = p0 + threadIdx.x;
-    int total;
-    block_scan<int>(pg < p.pages && p.refs[pg] > 0, sums, total);
-    n += total;
+  for (int p0 = 0; p0 < p.pages; p0 += kMeta * kRun) {
+    long long total;
+    block_scan(static_cast<long long>(__popc(used_at(p0 + threadIdx.x * kRun))), sums, total);
+    n += static_cast<int>(total);
   }
   int live = 0, moved = 0;
-  for (int p0 = 0; p0 < p.pages; p0 += kMeta) {
-    const int pg = p0 + threadIdx.x;
-    const int used = pg < p.pages && p.refs[pg] > 0;
-    int total, past;
-    const int before = live + block_scan(used, sums, total);
-    const int rank = moved + block_scan<int>(used && pg >= n, sums, past);
-    if (pg < p.pages) {
-      if (!used) {
+  for (int p0 = 0; p0 < p.pages; p0 += kMeta * kRun) {
+    const int first = p0 + threadIdx.x * kRun;
+    const unsigned used = used_at(first);
+    const int below = n <= first ? 0 : min(kRun, n - first);  // of the thread's pages
+    const unsigned past = used & (0xffu << below);
+    long long total;
+    const long long at = block_scan(
+        static_cast<long long>(__popc(used)) + (static_cast<long long>(__popc(past)) << 32), sums,
+        total);
+    int before = live + static_cast<int>(at & 0xffffffff);
+    int rank = moved + static_cast<int>(at >> 32);
+    for (int k = 0; k < kRun && first + k < p.pages; ++k) {
+      const int pg = first + k;
+      if (!(used >> k & 1)) {
         where[pg] = -1;
         if (pg < n) holes[pg - before] = pg;
-      } else if (pg < n) {
-        where[pg] = pg;
-      } else {
-        where[pg] = -2 - rank;
-        movers[rank] = pg;
+        continue;
       }
+      ++before;
+      where[pg] = pg < n ? pg : -2 - rank;
+      if (pg >= n) movers[rank++] = pg;
     }
-    live += total;
-    moved += past;
+    live += static_cast<int>(total & 0xffffffff);
+    moved += static_cast<int>(total >> 32);
   }
   if (threadIdx.x == 0) {
     plan[0] = n;
