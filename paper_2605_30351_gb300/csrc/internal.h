@@ -1,6 +1,7 @@
 // Host-side interface between the C ABI (api.cu) and the kernel files.
 #pragma once
 
+#include <atomic>
 #include <initializer_list>
 
 #include <cuda.h>
@@ -225,6 +226,19 @@ bool encode_map_2d_bf16(CUtensorMap* map, const void* base, unsigned long long d
                         unsigned b1, CUtensorMapSwizzle swizzle);
 
 void set_last_cuda_error(cudaError_t e);
+
+// A number found once per device (resident CTAs of a kernel instance, 0 = not yet);
+// the current device's cell, or null with the CUDA error recorded.
+struct PerDevice {
+  std::atomic<int> v[64] = {};
+  std::atomic<int>* cell() {
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && dev >= 0 && dev < 64) return &v[dev];
+    set_last_cuda_error(e != cudaSuccess ? e : cudaErrorInvalidDevice);
+    return nullptr;
+  }
+};
 
 // Argument checks shared by the entry points: MLA_OK if every non-null pointer
 // is device memory of the current device, and the status word's address there

@@ -915,7 +915,10 @@ int launch_paged(const PagedAttnArgs& a) {
     return MLA_ERR_CUDA;
   auto kern = paged_attn_kernel<DC, DR, CL>;
   // resident CTAs of this instance (one per SM, whole clusters), asked once
-  static int resident = 0;
+  static PerDevice known;
+  std::atomic<int>* cell = known.cell();
+  if (!cell) return MLA_ERR_CUDA;
+  int resident = cell->load();
   if (resident == 0) {
     cudaError_t e =
         cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmemBytes);
@@ -934,12 +937,14 @@ int launch_paged(const PagedAttnArgs& a) {
       oc.numAttrs = 1;
       e = cudaOccupancyMaxActiveClusters(&n, kern, &oc);
     }
-    if (e != cudaSuccess || n < 1) {
+    if (e == cudaSuccess && n < 1) e = cudaErrorLaunchOutOfResources;
+    if (e != cudaSuccess) {
       (void)cudaGetLastError();
       set_last_cuda_error(e);
       return MLA_ERR_CUDA;
     }
     resident = n * CL < kMaxCtas ? n * CL : kMaxCtas / CL * CL;
+    cell->store(resident);
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(resident);

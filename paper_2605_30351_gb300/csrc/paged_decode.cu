@@ -391,7 +391,10 @@ int launch_decode(const PagedAttnArgs& a) {
   using S = DecodeShape<DC, DR>;
   const PagedK k = paged_params(a, kBN, DC);
   auto kern = paged_decode_kernel<DC, DR>;
-  static int ctas = 0;  // one per SM, asked once
+  static PerDevice known;  // one CTA per SM, asked once
+  std::atomic<int>* cell = known.cell();
+  if (!cell) return MLA_ERR_CUDA;
+  int ctas = cell->load();
   if (ctas == 0) {
     int dev = 0, sms = 0;
     cudaError_t e =
@@ -399,12 +402,14 @@ int launch_decode(const PagedAttnArgs& a) {
     if (e == cudaSuccess) e = cudaGetDevice(&dev);
     if (e == cudaSuccess)
       e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess || sms < 1) {
+    if (e == cudaSuccess && sms < 1) e = cudaErrorInvalidDevice;
+    if (e != cudaSuccess) {
       (void)cudaGetLastError();
       set_last_cuda_error(e);
       return MLA_ERR_CUDA;
     }
     ctas = sms < kMaxCtas ? sms : kMaxCtas;
+    cell->store(ctas);
   }
   const int rc = launch_pdl(kern, dim3(ctas), kThreads, S::kSmemBytes, a.stream,
                             static_cast<const uint8_t*>(a.c), static_cast<const uint8_t*>(a.kr),

@@ -106,6 +106,7 @@ __global__ void __launch_bounds__(kMeta) resize_kernel(const Pool p, const int* 
         record_status(p.status, MLA_ERR_RANGE);
       row[j] = -1;
     }
+    __syncwarp();  // every lane has read the length
     if (lane == 0) p.lens[s] = want_len;
   }
   __syncthreads();
@@ -168,6 +169,7 @@ __global__ void __launch_bounds__(kMeta) resize_kernel(const Pool p, const int* 
       if (lane == 0) record_status(p.status, MLA_ERR_RANGE);
       continue;
     }
+    __syncwarp();  // every lane has read the length
     const int have = pages_of(len, p.page_tokens);
     int* row = p.table + static_cast<size_t>(s) * p.max_pages;
     for (int j = cow + lane; j < v; j += 32) {
