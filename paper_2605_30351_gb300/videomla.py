@@ -506,6 +506,7 @@ class PagedCache:
         seqs, max_pages = table.shape
         bf, i32 = torch.bfloat16, torch.int32
         self.c, self.kr, self.table, self.lens, self.refs = c, kr, table, lens, refs
+        self.seqs, self.d_c, self.d_r = seqs, d_c, kr.shape[3]
         self.struct = mla_paged_cache(
             c=_dev(c, bf, c.shape, "c"),
             kr=_dev(kr, bf, (layers, pages, tokens, kr.shape[3]), "kr"),
@@ -534,7 +535,7 @@ def mla_pages_resize(cache, new_lens, stream=None):
     back or added, a shared last page that grows is copied first."""
     _check("mla_pages_resize",
            load().mla_pages_resize(cache.ref,
-                                   _ptr(new_lens, torch.int32, (cache.struct.seqs,), "new_lens"),
+                                   _ptr(new_lens, torch.int32, (cache.seqs,), "new_lens"),
                                    _stream_ptr(stream)))
 
 
@@ -569,14 +570,13 @@ def mla_pages_compact(cache, new_table, new_refs, stream=None):
 def mla_paged_append(cache, layer, c_new, kr_new, q_start, pos, rope, stream=None):
     """Write new tokens, the streams' newest, into their pages of one layer:
     c_new [total, d_c] as is, kr_new [total, d_r] rotated at pos."""
-    st = cache.struct
     bf, i32 = torch.bfloat16, torch.int32
     total = c_new.shape[0] if isinstance(c_new, torch.Tensor) and c_new.dim() == 2 else 0
     _check("mla_paged_append",
            load().mla_paged_append(
-               cache.ref, int(layer), _ptr(c_new, bf, (total, st.d_c), "c_new"),
-               _ptr(kr_new, bf, (total, st.d_r), "kr_new"), total,
-               _ptr(q_start, i32, (st.seqs + 1,), "q_start"),
+               cache.ref, layer, _ptr(c_new, bf, (total, cache.d_c), "c_new"),
+               _ptr(kr_new, bf, (total, cache.d_r), "kr_new"), total,
+               _ptr(q_start, i32, (cache.seqs + 1,), "q_start"),
                _ptr(pos, i32, (total, rope.axes), "pos"), rope.ref, _stream_ptr(stream)))
 
 
@@ -590,19 +590,17 @@ def mla_paged_attention(cache, layer, q_c, q_r, q_start, head_dim, causal_block,
     [total, heads, d_r] rotated; rows of stream s from q_start[s]) over the
     pages of one layer. causal_block 0: every held token is seen; b: those
     before the end of the token's own block of b."""
-    st = cache.struct
     bf = torch.bfloat16
     if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()):
         raise TypeError("workspace must be a contiguous CUDA tensor")
-    total, heads = q_c.shape[:2]
+    total, heads, _ = q_c.shape
     _check("mla_paged_attention",
            load().mla_paged_attention(
-               cache.ref, int(layer), _ptr(q_c, bf, (total, heads, st.d_c), "q_c"),
-               _ptr(q_r, bf, (total, heads, st.d_r), "q_r"), total, heads,
-               _ptr(q_start, torch.int32, (st.seqs + 1,), "q_start"), int(head_dim),
-               int(causal_block), workspace.data_ptr(),
-               workspace.numel() * workspace.element_size(),
-               _ptr(o, bf, (total, heads, st.d_c), "o"), _stream_ptr(stream)))
+               cache.ref, layer, _ptr(q_c, bf, (total, heads, cache.d_c), "q_c"),
+               _ptr(q_r, bf, (total, heads, cache.d_r), "q_r"), total, heads,
+               _ptr(q_start, torch.int32, (cache.seqs + 1,), "q_start"), head_dim,
+               causal_block, workspace.data_ptr(), workspace.nbytes,
+               _ptr(o, bf, (total, heads, cache.d_c), "o"), _stream_ptr(stream)))
 
 
 def mla_selftest_bounded_wait(limit_ns, stream=None):
