@@ -2,8 +2,11 @@
 // key rotated on the way (Sec. 3.2).
 //
 // One warp per token: it finds the token's stream in q_start with a 32-way
-// search, then moves the row of d_c + d_r values in 16-byte pieces. Bound by
-// latency for a decoding step and by memory for chunks.
+// search (one load where there are up to 32 streams), then moves the row of d_c +
+// d_r values in 16-byte pieces that were fetched meanwhile. Bound by latency: q_start
+// and lens, then the page table, then the store follow one another. Measured: 64
+// streams' tokens 2.5 us, 18,720 tokens 7.3 us (19.4 MB; two rounds of warps, whose
+// 64 registers leave 32 of them on an SM; held to 32 registers 9.9 us).
 #include "internal.h"
 #include "paged_common.cuh"
 #include "ptx_sm103.cuh"
