@@ -44,7 +44,7 @@
 // to 5,001 keys (16 heads, d_c = 128, d_r = 64) 48.3 us: 27 blocks a CTA take about
 // 31 of them, bound by the softmax's latency and the MMAs together (tensor pipe 47 %
 // active), the rest is the start, the join and cut tiles. 5 drafted tokens of 16
-// streams (16 heads, d_c = 512, d_r = 64) 51 us: two stages of 74 KB are all that
+// streams (16 heads, d_c = 512, d_r = 64) 44.4 us: two stages of 74 KB are all that
 // fits beside Q and the score MMAs of 64 keys run at half rate, so the 10 us that
 // reading the cache takes are not approached.
 #include <cmath>
@@ -653,9 +653,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 // Joins the partial rows of tiles that several shares cut: o = sum_k 2^(m_k - M)
 // O_k over the same of l_k, in the shares' order. Every block finds the list of
 // work for itself: tiles that some CTA begins and does not end. A warp takes 32 rows
-// x 16 columns, a lane per row; one row of a tile that lies row after row; and
-// where many shares cut the tile (long streams) a block takes one row, each of its
-// warps every 16th partial row.
+// x 16 columns, a lane per row; or one row of a tile that lies row after row. Where
+// many shares cut it a block takes the row, each of its warps every 16th partial
+// row, unless there are many such rows.
 template <int DC, int DV, int CL>
 __global__ void __launch_bounds__(kJoinThreads, 1)
     paged_join_kernel(const float* part_o, const float2* part_ml, const int4* part_desc,
@@ -790,9 +790,9 @@ __global__ void __launch_bounds__(kJoinThreads, 1)
     return o + (static_cast<size_t>(desc[i].x) + row) * DC + (kSplit > 1 ? i % CL : 0) * DV;
   };
 
-  // More rows of much-cut tiles than two per block: a warp each after all (16 rows
-  // at once for a chain of a few steps beat one row at once for a short one: 16
-  // streams of 5 tokens at d_c = 512 50.7 -> 48 us)
+  // More rows than two per block: a warp each (16 rows at once in a chain of a few
+  // steps beat one row at once in a short one: 16 streams of 5 tokens at d_c = 512
+  // 50.9 -> 46.8 us)
   const int warp_items = items[ctas] & 0xffff, rows_left = items[ctas] >> 16;
   const bool spread = rows_left > 2 * static_cast<int>(gridDim.x);
   const int warp_count = warp_items + (spread ? rows_left : 0);

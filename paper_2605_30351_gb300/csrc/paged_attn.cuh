@@ -45,7 +45,7 @@ struct PagedK {
   __nv_bfloat16* o;
   float* part_o;
   float2* part_ml;
-  int4* part_desc;  // first row in o, rows, kPart*, 1 = row after row, 2 = and many shares
+  int4* part_desc;  // first row in o, rows, kPart*, 1 or 2 = row after row
   int total, heads, seqs, pages, page_tokens, max_pages, block;
   // Key blocks never straddle a group of `group` tokens: BN tokens (per_group
   // whole pages) where the pages divide a block, else one page.
@@ -57,10 +57,14 @@ struct PagedK {
 };
 
 // Partial rows lie as [4 columns][128 rows], which a warp (a lane per row) writes in
-// full lines, except those of short tiles (up to 32 rows) and of tiles that many
-// shares cut: they lie row after row, as the join reads them.
+// full lines, except those of short tiles (up to 32 rows) and of tiles that more than
+// four shares cut: they lie row after row, as the join reads them, a warp or
+// (part_desc.w = 2: tiles of more than four shares, and all of paged_decode.cu) a
+// block for each row. Two or eight shares instead of four: 100 new tokens of 9 ragged
+// streams 28.9 or 25.9 us (25.9), 5 drafted tokens of 16 streams at d_c = 512 43.6 or
+// 46.8 us (44.4).
 constexpr int kFewRows = 32;
-constexpr int kManyShares = 8;
+constexpr int kManyShares = 4;
 
 // part_desc.z: the slot holds a partial tile, that ends its tile; the CTA's share
 // is empty (a chain of partial tiles passes over it)

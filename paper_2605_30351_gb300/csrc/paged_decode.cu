@@ -382,11 +382,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (!whole && threadIdx.x < n_rows)
       p.part_ml[slot * kBM + threadIdx.x] = total_of(threadIdx.x);
-    if (!whole && threadIdx.x == 0) {
-      const bool many = static_cast<long long>(g.all) * kBN > kManyShares * share;
+    if (!whole && threadIdx.x == 0)
       p.part_desc[slot] = make_int4(static_cast<int>(grow), n_rows,
-                                    kPartHeld | (g.kb1 == g.all ? kPartEnds : 0), many ? 2 : 1);
-    }
+                                    kPartHeld | (g.kb1 == g.all ? kPartEnds : 0), 2);
     __syncthreads();  // sQ, the sums and the buffers are the next segment's
   }
   if (!any && threadIdx.x == 0)
