@@ -35,7 +35,10 @@
 //              lose to exchanging maxima, registers and power.
 // Pairs (CL = 2): two consecutive row tiles walk the same key blocks; each CTA
 // fetches half of the boxes and multicasts them to both. At d_c = 512 the two
-// CTAs of a pair share one row tile instead and hold 256 columns of O each.
+// CTAs of a pair share one row tile instead: each fetches 256 columns of c (the first
+// k too), holds Q's and O's columns that go with them, and sends the other its part
+// of the scores, which both add up (fp32; the same sum in both). 5 drafted tokens of
+// 16 streams took 44.4 us with all scores computed in both CTAs, 33.5 us so.
 //
 // Measured (12 heads, d_c = 192, d_r = 32): a chunk of 4,680 tokens on 32,760 keys
 // 765 - 812 us in short runs (1.53 TFLOP: 1,885 - 2,000 TFLOP/s, 1.0 - 1.06 of the
@@ -44,9 +47,10 @@
 // to 5,001 keys (16 heads, d_c = 128, d_r = 64) 48.3 us: 27 blocks a CTA take about
 // 31 of them, bound by the softmax's latency and the MMAs together (tensor pipe 47 %
 // active), the rest is the start, the join and cut tiles. 5 drafted tokens of 16
-// streams (16 heads, d_c = 512, d_r = 64) 44.4 us: two stages of 74 KB are all that
-// fits beside Q and the score MMAs of 64 keys run at half rate, so the 10 us that
-// reading the cache takes are not approached.
+// streams (16 heads, d_c = 512, d_r = 64) 33.5 us, on 32,000 keys each 77 us
+// (3.5 TB/s): 1.2 us for a block of 64 keys in turn through score MMAs (64 keys a
+// step run at half rate), the exchange and the softmax, and 15 us of start, first
+// copies and join.
 #include <cmath>
 
 #include "internal.h"
@@ -65,21 +69,22 @@ constexpr int kJoinCols = 16;  // columns of a warp's join item of 32 rows
 template <int DC, int DR>
 struct PagedShape {
   // Keys per block: 64 only where 128 do not fit. A score MMA of 64 keys takes about
-  // as long as one of 128 (at d_c = 512: 71 clocks for each step of 16 values).
+  // as long as one of 128 (71 clocks for each step of 16 values).
   static constexpr int BN = DC > 256 ? 64 : 128;
   static constexpr int DV = DC > 256 ? 256 : DC;   // output columns per CTA
-  static constexpr int DK = DC + DR;
+  static constexpr int DK = DV + DR;               // c columns of its scores: the same
   static constexpr int kSplit = DC / DV;           // CTAs that share a row tile
   static constexpr int kTileBytes = BN * DK * 2;   // one stage
   static constexpr int kCBox = BN * 128;           // [BN rows x 64 columns] of c
-  static constexpr int kKrOff = DC * BN * 2;       // the d_r columns of a stage
-  static constexpr int kBoxes = DC / 64 + 1;       // boxes per page
+  static constexpr int kKrOff = DV * BN * 2;       // the d_r columns of a stage
+  static constexpr int kBoxes = DV / 64 + 1;       // boxes per page
   static constexpr int kQStages = kBM / BN;        // stages that Q takes
   // TMEM columns: S, P (bf16, two a column), O, and Q as far as it fits; the rest
   // of Q stays in shared memory. Where everything fits (d_c up to 128) S has two
   // buffers and P takes the place of the scores it came from, so that the next
   // block's scores are there before this one's weights are: with little MMA work a
-  // block the softmax sets the pace.
+  // block the softmax sets the pace. (d_c = 512 with q_r in shared memory would fit
+  // too: 34.8 us for 33.5.)
   static constexpr int kBufs = 2 * BN + DV + DK / 2 <= 512 ? 2 : 1;
   static constexpr int kTmemS = 0;
   static constexpr int kTmemP = kBufs == 2 ? 0 : BN;
@@ -87,16 +92,20 @@ struct PagedShape {
   static constexpr int kTmemQ = kTmemO + DV;
   static constexpr bool kQrTmem = kTmemQ + DK / 2 <= 512;
   static constexpr int kQcFit = (512 - kTmemQ) * 2 / 64 * 64;
-  static constexpr int kQcTmem = kQcFit < DC ? kQcFit : DC;
-  static constexpr int kQcSmem = DC - kQcTmem;
+  static constexpr int kQcTmem = kQcFit < DV ? kQcFit : DV;
+  static constexpr int kQcSmem = DV - kQcTmem;
   static constexpr int kQKrOff = kQcSmem * kBM * 2;
   static constexpr int kQBytes = kQrTmem ? 0 : kQKrOff + kBM * DR * 2;
+  // a block's partial scores from the peer, fp32 as [64 / 4][128 rows][4 keys]; two of it
+  static constexpr int kXBytes = kSplit > 1 ? BN * kBM * 4 : 0;
   static constexpr int kBarBytes = 512;  // barriers and small words
   static constexpr int kSmemCap = 232448;
-  static constexpr int kFit = (kSmemCap - 1024 - kBarBytes - kQBytes) / kTileBytes;
+  static constexpr int kFit =
+      (kSmemCap - 1024 - kBarBytes - kQBytes - 2 * kXBytes) / kTileBytes;
   static constexpr int kMaxStages = BN == 128 ? 4 : 6;
   static constexpr int kStages = kFit > kMaxStages ? kMaxStages : kFit;
-  static constexpr int kSmemBytes = 1024 + kQBytes + kTileBytes * kStages + kBarBytes;
+  static constexpr int kSmemBytes =
+      1024 + kQBytes + kTileBytes * kStages + 2 * kXBytes + kBarBytes;
   static constexpr uint32_t kTmemCols = 512;
   static constexpr uint32_t kKrSw = DR == 32 ? kSw64 : kSw128;
   static constexpr uint32_t kKrRow = DR * 2;
@@ -118,13 +127,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   using S = PagedShape<DC, DR>;
   constexpr int BN = S::BN, DV = S::DV, NST = S::kStages, QST = S::kQStages, NB = S::kBufs;
   constexpr int TR = kBM * CL / S::kSplit;  // rows of a CTA's, or a pair's, tile
+  constexpr int MC = S::kSplit == 1 ? CL : 1;  // CTAs that share a stage's boxes
   constexpr uint16_t kPair = static_cast<uint16_t>((1u << CL) - 1u);
   static_assert(S::kSplit == 1 || CL == S::kSplit, "split tiles take a pair");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = align_smem_1024(smem_raw);
   uint8_t* sQ = smem;
   uint8_t* sKV = smem + S::kQBytes;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(sKV + NST * S::kTileBytes);
+  uint8_t* sX = sKV + NST * S::kTileBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sX + 2 * S::kXBytes);
   uint64_t* q_ready = bars;
   uint64_t* kv_full = bars + 1;
   uint64_t* kv_empty = kv_full + NST;
@@ -133,7 +144,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* p_full = s_full + NB;          // so that a waiter one block behind still
   uint64_t* pv_done = p_full + NB;         // finds the phase it waits for
   uint64_t* mma_drain = pv_done + NB;      // [2]: one per issuing thread
-  long long* scratch = reinterpret_cast<long long*>(mma_drain + 2);  // [8]
+  uint64_t* x_full = mma_drain + 2;        // [2][4]: a warp's scores from the peer
+  long long* scratch = reinterpret_cast<long long*>(x_full + 8);  // [8]
   Place* ends = reinterpret_cast<Place*>(scratch + 8);               // [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ends + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -146,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(q_ready, kBM);
     for (int s = 0; s < NST; ++s) {
       mbar_init(&kv_full[s], 1);
-      mbar_init(&kv_empty[s], CL);
+      mbar_init(&kv_empty[s], MC);
     }
     mbar_init(s_free, kBM);
     for (int i = 0; i < NB; ++i) {
@@ -156,6 +168,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(&mma_drain[0], 1);
     mbar_init(&mma_drain[1], 1);
+    if (S::kSplit > 1)
+      for (int i = 0; i < 8; ++i) mbar_init(&x_full[i], 1);
     *abort_flag = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tm_c);
@@ -176,6 +190,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   grid_dep_sync();
   const int crank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int first_row = S::kSplit == 1 ? crank * kBM : 0;  // of the pair's tile
+  const int vpart = S::kSplit > 1 ? crank : 0;              // of c's columns
+  const bool has_r = vpart == 0;  // the first of a split tile's CTAs adds q_r . k
   if (blockIdx.x == 0) {
     check_q_start(p.q_start, p.seqs, p.total, p.status);
     for (int s = threadIdx.x; s < p.seqs; s += kThreads) {
@@ -201,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto acquire = [&]() {  // stage sc is free
         bool free = true;
         if (sc >= NST) {
-          if constexpr (CL == 1)
+          if constexpr (MC == 1)
             free = mbar_wait(&kv_empty[sc % NST], ((sc / NST) - 1) & 1, wc);
           else  // the peer's threads arrive on it too
             free = mbar_wait_cluster(&kv_empty[sc % NST], ((sc / NST) - 1) & 1, wc);
@@ -231,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint64_t* full = &kv_full[sc % NST];
           if (lane == 0) {
             if (boxes)
-              mbar_arrive_expect_tx(full, boxes * 32 * S::DK * 2);
+              mbar_arrive_expect_tx(full, boxes * 32 * (has_r ? S::DK : DV) * 2);
             else
               mbar_arrive(full);
           }
@@ -239,9 +255,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int bx = lane; bx < boxes * S::kBoxes; bx += 32) {
             const int i = bx / S::kBoxes, cb = bx - i * S::kBoxes;
             const int r = g.st.q0 * p.heads + r0 + 32 * i;
-            if (cb < DC / 64)
-              tma_load_2d(st + cb * S::kCBox + i * 32 * 128, &tm_qc, full, cb * 64, r);
-            else
+            if (cb < DV / 64)
+              tma_load_2d(st + cb * S::kCBox + i * 32 * 128, &tm_qc, full, vpart * DV + cb * 64,
+                          r);
+            else if (has_r)
               tma_load_2d(st + S::kKrOff + i * 32 * S::kKrRow, &tm_qr, full, 0, r);
           }
         }
@@ -256,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint64_t* full = &kv_full[sc % NST];
           if (lane == 0) {
             if (boxes)
-              mbar_arrive_expect_tx(full, boxes * p.box_rows * S::DK * 2);
+              mbar_arrive_expect_tx(full, boxes * p.box_rows * (has_r ? S::DK : DV) * 2);
             else
               mbar_arrive(full);
           }
@@ -264,18 +281,19 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int b0 = 0; b0 < boxes * S::kBoxes; b0 += 32) {
             const int bx = b0 + lane, i = bx / S::kBoxes, cb = bx - i * S::kBoxes;
             const int page = __shfl_sync(0xffffffffu, page_now, i & 31);
-            if (i >= boxes || (CL > 1 && (bx & 1) != crank)) continue;
+            if (i >= boxes || (MC > 1 && (bx & 1) != crank)) continue;
             int r = p.pages * p.page_tokens;  // past the pool: zeros
             if (page >= 0 && page < p.pages)
               r = page * p.page_tokens + sub * BN;
             else
               record_status(p.status, MLA_ERR_RANGE);
-            const bool is_c = cb < DC / 64;
+            const bool is_c = cb < DV / 64;
+            if (!is_c && !has_r) continue;
             uint8_t* dst = is_c ? kv + cb * S::kCBox + i * p.box_rows * 128
                                 : kv + S::kKrOff + i * p.box_rows * static_cast<int>(S::kKrRow);
             const CUtensorMap* map = is_c ? &tm_c : &tm_kr;
-            const int x = is_c ? cb * 64 : 0;
-            if constexpr (CL == 1)
+            const int x = is_c ? vpart * DV + cb * 64 : 0;
+            if constexpr (MC == 1)
               tma_load_2d(dst, map, full, x, r);
             else
               tma_load_2d_mc(dst, map, full, x, r, kPair);
@@ -299,8 +317,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         // Q has left its stages: give them back, to both CTAs of a pair
         for (int q = 0; q < QST; ++q, ++sc)
-          if (lane < CL) {
-            if constexpr (CL == 1)
+          if (lane < MC) {
+            if constexpr (MC == 1)
               mbar_arrive(&kv_empty[sc % NST]);
             else
               mbar_arrive_cluster(dsmem_addr(smem_u32(&kv_empty[sc % NST]), lane));
@@ -314,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ok) break;
           if (valid < BN) {
             const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-            for (int cb = 0; cb < DC / 64; ++cb)
+            for (int cb = 0; cb < DV / 64; ++cb)
               for (int i = valid * 8 + lane; i < BN * 8; i += 32)
                 *reinterpret_cast<uint4*>(kv + cb * S::kCBox + i * 16) = zero;
             fence_proxy_async_smem();
@@ -332,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t ka = smem_u32(kv);
             const uint32_t d = tmem + S::kTmemS + (it % NB) * BN;
 #pragma unroll
-            for (int cb = 0; cb < DC / 64; ++cb)
+            for (int cb = 0; cb < DV / 64; ++cb)
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 const uint64_t bd = sdesc(ka + cb * S::kCBox + k * 32, 16, 1024, kSw128);
@@ -344,10 +362,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                           bd, S::kIdescQK, acc);
               }
 #pragma unroll
-            for (int k = 0; k < DR / 16; ++k) {
+            for (int k = 0; k < (has_r ? DR / 16 : 0); ++k) {
               const uint64_t bd = sdesc(ka + S::kKrOff + k * 32, 16, S::kKrSbo, S::kKrSw);
               if constexpr (S::kQrTmem)
-                umma_ts(d, tmem + S::kTmemQ + DC / 2 + k * 8, bd, S::kIdescQK, 1u);
+                umma_ts(d, tmem + S::kTmemQ + DV / 2 + k * 8, bd, S::kIdescQK, 1u);
               else
                 umma_ss(d, sdesc(qa + S::kQKrOff + k * 32, 16, S::kKrSbo, S::kKrSw), bd,
                         S::kIdescQK, 1u);
@@ -365,7 +383,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == 2) {
       // ---------------------------------------------------------- PV issuer
       if (lane == 0) {
-        const int vpart = S::kSplit > 1 ? crank : 0;
         while (ok && walk.next(g)) {
           sc += QST;
           for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, ++sc) {
@@ -373,13 +390,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!ok) break;
             tc_fence_after();
             const int st = sc % NST;
-            const uint32_t va = smem_u32(sKV) + st * S::kTileBytes + vpart * (DV / 64) * S::kCBox;
+            const uint32_t va = smem_u32(sKV) + st * S::kTileBytes;
 #pragma unroll
             for (int s = 0; s < BN / 16; ++s)
               umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + (it % NB) * BN + s * 8,
                       sdesc(va + s * 2048, S::kCBox, 1024, kSw128), S::kIdescPV,
                       (kb > g.kb0 || s > 0) ? 1u : 0u);
-            if constexpr (CL == 1)
+            if constexpr (MC == 1)
               umma_commit(&kv_empty[st]);
             else
               umma_commit_mc(&kv_empty[st], kPair);
@@ -398,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int quarter = warp & 3;  // TMEM lane quarter this warp may access
     const int r = quarter * 32 + lane;
     const uint32_t t_lane = static_cast<uint32_t>(quarter * 32) << 16;
-    const int vpart = S::kSplit > 1 ? crank : 0;
+    int xc = 0;  // blocks exchanged with the peer
     struct Row {
       int tile0, lrow, keys;  // the CTA's first row, this thread's, the keys it sees
       size_t grow;            // its place in q and o
@@ -497,6 +514,36 @@ __global__ void __launch_bounds__(kThreads, 1)
         float sv[BN];
 #pragma unroll
         for (int c = 0; c < BN; ++c) sv[c] = __uint_as_float(sr[c]);
+        if constexpr (S::kSplit > 1) {
+          // The scores over all of c are this CTA's and the peer's: each sends its own
+          // (row by row, warp by warp) and adds what it gets. A buffer is written again
+          // two blocks later: by then the peer's scores of the block between are here,
+          // and it sent them after it had read these. Plain stores with a released
+          // arrival took 0.5 us a block more; sending a block ahead of its softmax,
+          // which spills registers, 0.15 us.
+          const uint32_t off = (xc & 1) * S::kXBytes + r * 16;
+          const uint32_t to = dsmem_addr(smem_u32(sX) + off, crank ^ 1);
+          uint64_t* full = &x_full[(xc & 1) * 4 + quarter];
+          const uint32_t bar = dsmem_addr(smem_u32(full), crank ^ 1);
+#pragma unroll
+          for (int c = 0; c < BN / 4; ++c)
+            st_async_v4(to + c * kBM * 16, bar, sv[4 * c], sv[4 * c + 1], sv[4 * c + 2],
+                        sv[4 * c + 3]);
+          if (lane == 0) mbar_arrive_expect_tx(full, 32 * BN * 4);
+          if (!mbar_wait_cluster(full, (xc >> 1) & 1, wc)) {
+            ok = false;
+            break;
+          }
+          ++xc;
+#pragma unroll
+          for (int c = 0; c < BN / 4; ++c) {
+            const float4 v = *reinterpret_cast<const float4*>(sX + off + c * kBM * 16);
+            sv[4 * c] += v.x;
+            sv[4 * c + 1] += v.y;
+            sv[4 * c + 2] += v.z;
+            sv[4 * c + 3] += v.w;
+          }
+        }
         const int valid = min(pos.rows(p), w.keys - pos.token(p));
         if (valid < BN) {
 #pragma unroll

@@ -106,8 +106,10 @@ __device__ __forceinline__ int tile_blocks(const PagedK& p, int n, int len, int 
 // Cost of a stream's row tiles in keys, as a straight line from the first to the
 // last tile's keys (exact for a whole chunk and token by token, and within a
 // mask block for others) plus kTileCost for loading Q and writing O: prefix sums
-// in closed form, so a share's ends are found without walking the tiles.
-constexpr int kTileCost = 512;
+// in closed form, so a share's ends are found without walking the tiles. Four blocks:
+// with two or eight the ragged and the drafted tokens' calls are 2 - 8 % slower.
+template <int BN>
+constexpr int kTileCost = 4 * BN;
 
 struct Cost {
   long long first, slope;  // slope in 1/256 keys per tile
@@ -117,21 +119,21 @@ struct Cost {
   }
 };
 
-template <int TR>
+template <int BN, int TR>
 __device__ __forceinline__ Cost cost_of(const PagedK& p, const Stream& st) {
   Cost c{0, 0, 0};
   if (st.n == 0) return c;
   const int rows = st.n * p.heads;
   c.tiles = (rows + TR - 1) / TR;
   const int k1 = keys_seen(p, st.len - 1, st.len);
-  c.first = k1 + kTileCost;
+  c.first = k1 + kTileCost<BN>;
   if (c.tiles > 1) {
     const int k0 = keys_seen(p, st.len - st.n + p.by_heads(TR - 1), st.len);
     if (c.tiles <= 4096) {  // the products stay below 2^63
-      c.first = k0 + kTileCost;
+      c.first = k0 + kTileCost<BN>;
       c.slope = static_cast<long long>(__fdividef((k1 - k0) * 256.f, c.tiles - 1.f));
     } else {
-      c.first = (static_cast<long long>(k0) + k1) / 2 + kTileCost;
+      c.first = (static_cast<long long>(k0) + k1) / 2 + kTileCost<BN>;
     }
   }
   return c;
@@ -162,7 +164,7 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
     for (int k = 0; k < per; ++k)
       if (s0 + k < p.seqs) {
         st = stream_at(p, s0 + k);
-        c = cost_of<TR>(p, st);
+        c = cost_of<BN, TR>(p, st);
         mine += c.before(c.tiles);
       }
   long long x = mine;
@@ -194,7 +196,7 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
       if (per > 1)
         for (; s < p.seqs; ++s) {
           st = stream_at(p, s);
-          c = cost_of<TR>(p, st);
+          c = cost_of<BN, TR>(p, st);
           const long long all = c.before(c.tiles);
           if (rem < all) break;
           rem -= all;

@@ -166,6 +166,17 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster) {
                : "memory");
 }
 
+// Four floats to shared memory of any CTA of the cluster; the mbarrier `bar` of the
+// same CTA counts their 16 bytes (both as shared::cluster addresses, dsmem_addr).
+__device__ __forceinline__ void st_async_v4(uint32_t addr, uint32_t bar, float x, float y, float z,
+                                            float w) {
+  asm volatile(
+      "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%2, %3, %4, %5},"
+      " [%1];" ::"r"(addr),
+      "r"(bar), "f"(x), "f"(y), "f"(z), "f"(w)
+      : "memory");
+}
+
 // Drain wait used on the abort path: ignores the abort flag, still bounded.
 __device__ __forceinline__ void mbar_wait_drain(uint64_t* bar, uint32_t parity, int* status) {
   const uint64_t t0 = globaltimer_ns();
