@@ -18,8 +18,8 @@
 // The warps' O, maxima and sums are added up in shared memory at the end of a
 // segment. Shares, partial rows and their join are those of paged_attn.cu.
 //
-// Measured at d_c = 192, d_r = 32, 12 heads: one token on 777 keys 9.6 us and on
-// 32,760 keys 13.5 us (latency: the share search, the first keys, the join); 64
+// Measured at d_c = 192, d_r = 32, 12 heads: one token on 777 keys 9.4 us and on
+// 32,760 keys 13.4 us (latency: the share search, the first keys, the join); 64
 // streams of up to 32,760 keys 78.3 us (416 MB, 5.3 TB/s; 76 us of it this kernel,
 // DRAM at 68 % of its peak over the kernel's start and end). The tensor-memory path
 // on the same calls: 13.3, 18.0 and 79.4 us, and with pages of 16 tokens, whose
