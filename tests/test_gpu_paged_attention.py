@@ -385,3 +385,42 @@ def test_one_token_bad_pages_count_as_zeros():
         assert torch.isfinite(o).all() and torch.equal(o[1], ref[1])
         p.cache.table[0, 1] = keep
     assert torch.equal(p.run(1), ref)
+
+
+# At d_c = 512 two CTAs score 256 columns of c each (one of them k too) and add up what
+# they send one another.
+
+@pytest.mark.parametrize("part", ["first", "second", "k", "cancel"])
+@pytest.mark.parametrize("d_r", [32, 64])
+def test_wide_scores_from_either_half(part, d_r):
+    """Scores that come from one CTA's columns alone, or cancel between the two."""
+    p = Problem([700, 130, 65], [9, 1, 65], heads=3, d_c=512, d_r=d_r, page=32, seed=5, gain=6.0)
+    q_c, q_r = p.q_c, p.q_r
+    if part != "first":
+        q_c[..., :256] = 0
+    if part not in ("second", "cancel"):
+        q_c[..., 256:] = 0
+    if part != "k":
+        q_r.zero_()
+    if part == "cancel":
+        q_c[..., :256] = -q_c[..., 256:]
+        p.cache.c[..., 256:] = p.cache.c[..., :256]
+    run_check(p, 1, tokens=9)
+
+
+@pytest.mark.parametrize("rows", [1, 31, 32, 33, 80, 96, 97, 128, 129, 300])
+@pytest.mark.parametrize("lens", [63, 64, 65, 200])
+def test_wide_row_counts(rows, lens):
+    """Warps without a row send nothing; tiles of one block and of several."""
+    n = min(rows, lens)
+    p = Problem([lens, lens + 1], [n, 1], heads=1 if rows <= lens else 5, d_c=512, d_r=64,
+                page=16, seed=rows)
+    run_check(p, 1, tokens=8)
+
+
+def test_wide_many_blocks_same_bits():
+    """Both exchange buffers many times over, and the same bits from call to call."""
+    p = Problem([30000, 9000, 1, 17000], [3, 40, 1, 2], heads=16, d_c=512, d_r=64, seed=3)
+    o = run_check(p, 1, tokens=3)
+    for _ in range(5):
+        assert torch.equal(p.run(), o)
