@@ -11,13 +11,18 @@ constexpr int kBM = 128;       // rows of a partial tile's slot
 constexpr int kMaxCtas = 152;  // the workspace holds two slots for each
 
 // Workspace of a call whose CTAs hold dv output columns: partial rows (fp32), their
-// (maximum, sum), and a descriptor per slot.
+// (maximum, sum), and a descriptor per slot. Partial rows are stored 32 bytes at a
+// time, while the caller's workspace starts on any 16-byte boundary: the layout
+// starts at the next 32-byte one, so a workspace has 16 bytes to spare.
 struct PartLayout {
   unsigned long long ml, desc, total;
   explicit PartLayout(int dv)
       : ml(2ull * kMaxCtas * kBM * dv * 4),
         desc(ml + 2ull * kMaxCtas * kBM * 8),
-        total(desc + 2ull * kMaxCtas * 16) {}
+        total(desc + 2ull * kMaxCtas * 16 + 16) {}
+  static char* base(void* workspace) {
+    return reinterpret_cast<char*>((reinterpret_cast<unsigned long long>(workspace) + 31) & ~31ull);
+  }
 };
 
 // What a short call pays for is the code that it runs for the first time, about 15
@@ -291,7 +296,7 @@ struct BlockPos {
 inline PagedK paged_params(const PagedAttnArgs& a, int bn, int dv) {
   const bool divides = bn % a.page_tokens == 0;
   const PartLayout at(dv);
-  char* ws = static_cast<char*>(a.workspace);
+  char* ws = PartLayout::base(a.workspace);
   PagedK k;
   k.q_start = a.q_start;
   k.table = a.table;
