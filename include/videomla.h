@@ -542,7 +542,9 @@ unsigned long long mla_paged_workspace_bytes(const mla_paged_cache* cache);
  *          token by token, a chunk's length is bidirectional inside a chunk (App. D.4)
  *  o       bf16 [total][heads][d_c]; a row that sees no key (a < 0, lens[s] = 0) is 0
  * Rows past a stream's length and free pages may hold anything, NaN included. A NaN or
- * infinity in a key that a mask hides from some of the new tokens may reach those too.
+ * infinity in a key that a row sees gives what the formula gives; a row whose scores are
+ * all -inf is 0 times c. In a key that a mask hides from some of the new tokens it may
+ * reach those too.
  * q_start not ascending within 0..total, a length past max_pages * page_tokens and a
  * table entry that names no page are recorded as MLA_ERR_RANGE: the stream's rows are
  * not written, or the page counts as zeros. total = 0 is MLA_OK.

@@ -144,9 +144,11 @@ def visible(place, held, block):
     return held if block == 0 else min(held, (place // block + 1) * block)
 
 
-def attend(q_c, q_r, c, kr, head_dim, block):
+def attend(q_c, q_r, c, kr, head_dim, block, v=None):
     """Newest tokens of one stream: q_c [n, H, d_c], q_r [n, H, d_r] rotated, c
-    [held, d_c], kr [held, d_r]; a row that sees nothing is 0. float64."""
+    [held, d_c], kr [held, d_r]; a row that sees nothing is 0. float64. The weights
+    multiply c, or v: |c| gives the size that rounding errors go by."""
+    v = c if v is None else v
     n, held = q_c.shape[0], c.shape[0]
     out = np.zeros(q_c.shape)
     for i in range(n):
@@ -155,5 +157,5 @@ def attend(q_c, q_r, c, kr, head_dim, block):
             continue
         s = (q_c[i] @ c[:k].T + q_r[i] @ kr[:k].T) / math.sqrt(head_dim)
         w = np.exp(s - s.max(-1, keepdims=True))
-        out[i] = (w / w.sum(-1, keepdims=True)) @ c[:k]
+        out[i] = (w / w.sum(-1, keepdims=True)) @ v[:k]
     return out

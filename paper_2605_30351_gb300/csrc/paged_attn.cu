@@ -563,12 +563,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                                fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7])));
         const float m_blk = mx * p.scale_log2;
         // The running maximum moves only when a block exceeds it by more than
-        // 2^8 (weights up to 256 are harmless in bf16 and fp32). A row that has
-        // seen no key yet has none; its weights are exp2(-inf) = 0.
+        // 2^8 (weights up to 256 are harmless in bf16 and fp32). A row that sees
+        // no key of the first block sees none of the segment (it sees a prefix) and
+        // has none; its weights are exp2(-inf) = 0.
         float alpha = 1.f;
         bool need = false;
         if (kb == g.kb0) {
-          m_run = m_blk;
+          m_run = valid > 0 ? fmaxf(m_blk, kLowest) : -INFINITY;
         } else if (m_blk > m_run + kRescaleLog2) {
           need = true;
           alpha = ex2_approx(m_run - m_blk);
@@ -785,6 +786,7 @@ __global__ void __launch_bounds__(kJoinThreads, 1)
       const int k = base + lane * step;
       float2 ml = make_float2(-INFINITY, 0.f);
       if (k < n && holds(i, k)) ml = part_ml[slot_of(i, k) * kBM + row];
+      const unsigned none = __ballot_sync(0xffffffffu, ml.x == -INFINITY);
       float mx = ml.x;
 #pragma unroll
       for (int s = 16; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
@@ -821,7 +823,7 @@ __global__ void __launch_bounds__(kJoinThreads, 1)
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const float wt = __shfl_sync(0xffffffffu, w, t0 + t);
-          if (wt == 0.f) continue;  // an empty share's slot may hold anything
+          if (none >> (t0 + t) & 1) continue;  // an empty share's slot may hold anything
 #pragma unroll
           for (int c = 0; c < kV; ++c) {
             acc[c].x += wt * v[t][c].x;
@@ -899,7 +901,7 @@ __global__ void __launch_bounds__(kJoinThreads, 1)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float b = ex2_approx(ml[k].x - ref);
-        if (b != 0.f) {
+        if (ml[k].x != -INFINITY) {
           l += ml[k].y * b;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -947,7 +949,7 @@ __global__ void __launch_bounds__(kJoinThreads, 1)
         sum += wt * row_l[w];
         v += wt * row_o[w][threadIdx.x];
       }
-      out_row(i, row)[threadIdx.x] = __float2bfloat16_rn(sum == 0.f ? 0.f : v / sum);
+      out_row(i, row)[threadIdx.x] = __float2bfloat16_rn(sum == 0.f ? v * 0.f : v / sum);
     }
     __syncthreads();  // the rows in shared memory are the next item's
   }

@@ -75,6 +75,12 @@ constexpr int kManyShares = 4;
 // is empty (a chain of partial tiles passes over it)
 constexpr int kPartHeld = 1, kPartEnds = 2, kPartEmpty = 4;
 
+// The maximum of a partial row is -inf only where the row sees none of the part's keys,
+// and the join passes over those (their values are whatever 0 times a hidden key's is).
+// Where every key seen scores -inf or NaN it is the lowest finite number, so that a NaN
+// sum or value gets into the row whatever its weight.
+constexpr float kLowest = -3.402823466e38f;
+
 struct Stream {
   int q0, n, len;
 };

@@ -380,8 +380,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                                      32 * c + out_c) = sum;
       }
     }
-    if (!whole && threadIdx.x < n_rows)
-      p.part_ml[slot * kBM + threadIdx.x] = total_of(threadIdx.x);
+    if (!whole && threadIdx.x < n_rows) {
+      float2 t = total_of(threadIdx.x);
+      if (keys_of(threadIdx.x) > BlockPos<kBN>(p, g.kb0).token(p)) t.x = fmaxf(t.x, kLowest);
+      p.part_ml[slot * kBM + threadIdx.x] = t;
+    }
     if (!whole && threadIdx.x == 0)
       p.part_desc[slot] = make_int4(static_cast<int>(grow), n_rows,
                                     kPartHeld | (g.kb1 == g.all ? kPartEnds : 0), 2);

@@ -1,11 +1,13 @@
 """Attention over the paged latent cache where its inputs lie at an edge of what the
 entry point accepts."""
 
+import numpy as np
 import pytest
 import torch
 
+from oracle import paged_oracle as O
 from paper_2605_30351_gb300 import videomla as V
-from test_gpu_paged_attention import Problem
+from test_gpu_paged_attention import REL, Problem
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +43,76 @@ def test_workspace_at_any_16_byte_boundary(d_c, d_r, lens, new, heads):
         p.workspace = arena[off:off + need]
         assert torch.equal(p.run(1), ref), off
         assert (arena[:off] == 0xA5).all() and (arena[off + need:] == 0xA5).all(), off
+
+
+# A key that is not finite, the last one of each stream: the newest token sees it, and
+# alone in its block of 64 or 128 keys. Whether a share of the work begins with that
+# block, ends before it or holds the whole tile depends on the sizes; the answer must
+# not. What the earlier tokens get is left open.
+LEN = 513
+PLACES = [
+    # streams, new tokens of each, heads
+    (60, 4, 12),      # tiles of 48 rows, cut by two or three shares
+    (60, 30, 12),     # two tiles and more a stream
+    (400, 4, 12),     # most tiles whole
+    (3, 4, 12),       # tiles cut by many shares
+    (3, 2, 12),       # short tiles
+    (60, 1, 12),      # tiles of 16 rows
+    (3, 1, 12),
+]
+
+
+def with_key(where, value, streams, new, heads, d_c, seed=0):
+    """A problem whose streams' last keys hold `value` in one column of c or k."""
+    p = Problem([LEN] * streams, [new] * streams, heads=heads, d_c=d_c, page=64, seed=seed)
+    last = p.cache.table[:, (LEN - 1) // 64].long()
+    t = p.cache.c if where == "c" else p.cache.kr
+    t[p.layer, last, (LEN - 1) % 64, 5] = value
+    return p
+
+
+def newest(p):
+    """(stream, its newest token's row)."""
+    return list(enumerate(np.cumsum(p.new) - 1))
+
+
+def host(*tensors):
+    return (t.double().cpu().numpy() for t in tensors)
+
+
+@pytest.mark.parametrize("d_c", [64, 128, 192, 256, 512])
+@pytest.mark.parametrize("streams,new,heads", PLACES)
+@pytest.mark.parametrize("where", ["c", "k"])
+def test_nan_in_a_visible_key(where, streams, new, heads, d_c):
+    """Its score is NaN, so every weight and every value of the rows is."""
+    p = with_key(where, float("nan"), streams, new, heads, d_c)
+    o = p.run(1)
+    bad = [s for s, i in newest(p) if not torch.isnan(o[i]).all()]
+    assert not bad, bad
+
+
+@pytest.mark.parametrize("d_c", [64, 128, 192, 256, 512])
+@pytest.mark.parametrize("streams,new,heads", PLACES)
+@pytest.mark.parametrize("where", ["c", "k"])
+def test_infinity_in_a_visible_key(where, streams, new, heads, d_c):
+    """Where the query's value there is positive, the score is inf and all weights are
+    inf - inf: NaN. Where it is negative the score is -inf and the weight 0: the row is
+    that of the other keys (the tolerance of test_gpu_paged_attention), but for the
+    column of c that holds the infinity, 0 * inf."""
+    p = with_key(where, float("inf"), streams, new, heads, d_c, seed=1)
+    o, q_c, q_r, table, c_all, kr_all = host(p.run(1), p.q_c, p.q_r, p.cache.table,
+                                             p.cache.c[p.layer], p.cache.kr[p.layer])
+    a = np.arange(LEN - 1)
+    for s, i in newest(p):
+        q = (q_c if where == "c" else q_r)[i, :, 5]
+        assert (q != 0).all()
+        at = table[s].astype(int)[a // 64], a % 64
+        args = q_c[i:i + 1], q_r[i:i + 1], c_all[at], kr_all[at], p.head_dim, 0
+        ref, size = O.attend(*args)[0], O.attend(*args, np.abs(c_all[at]))[0]
+        for h in range(heads):
+            if q[h] > 0:
+                assert np.isnan(o[i, h]).all(), (s, h)
+                continue
+            cols = np.arange(d_c) != 5 if where == "c" else np.ones(d_c, bool)
+            assert np.isnan(o[i, h, ~cols]).all(), (s, h)
+            assert (np.abs(o[i, h] - ref[h]) <= REL * size[h])[cols].all(), (s, h)
