@@ -44,15 +44,15 @@ __global__ void __launch_bounds__(kThreads) paged_append_kernel(const AppendK p)
     const uint4* src = p.c_new + static_cast<size_t>(t) * c16;
     const __nv_bfloat16* x = p.kr_new + static_cast<size_t>(t) * p.d_r;
     uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (lane < c16) v = __ldg(src + lane);
+    if (lane < c16) v = src[lane];
     auto angle = [&](int i) {
       const int axis = p.axes == 1 || i < p.pairs_t ? 0 : (i < p.pairs_t + p.pairs_h ? 1 : 2);
-      int co = __ldg(p.pos + static_cast<size_t>(t) * p.axes + axis);
+      int co = p.pos[static_cast<size_t>(t) * p.axes + axis];
       if (co < 0 || co >= p.rope_len) {
         record_status(p.status, MLA_ERR_RANGE);
         co = 0;
       }
-      return __ldg(p.rope + static_cast<size_t>(co) * m + i);
+      return p.rope[static_cast<size_t>(co) * m + i];
     };
     float2 cs = make_float2(0.f, 0.f);
     float a = 0.f, b = 0.f;
@@ -63,24 +63,24 @@ __global__ void __launch_bounds__(kThreads) paged_append_kernel(const AppendK p)
     }
     int s, q0, q1, len;
     if (p.seqs <= 32) {  // every stream's numbers in one load, a lane per stream
-      const int q = lane <= p.seqs ? __ldg(p.q_start + min(lane, p.seqs)) : 0;
-      const int n = lane < p.seqs ? __ldg(p.lens + lane) : 0;
+      const int q = lane <= p.seqs ? p.q_start[min(lane, p.seqs)] : 0;
+      const int n = lane < p.seqs ? p.lens[lane] : 0;
       const unsigned le = __ballot_sync(0xffffffffu, lane < p.seqs && q <= t);
       s = le ? 31 - __clz(le) : 0;
       q0 = __shfl_sync(0xffffffffu, q, s);
-      q1 = s == 31 ? __ldg(p.q_start + 32) : __shfl_sync(0xffffffffu, q, (s + 1) & 31);
+      q1 = s == 31 ? p.q_start[32] : __shfl_sync(0xffffffffu, q, (s + 1) & 31);
       len = __shfl_sync(0xffffffffu, n, s);
     } else {
       s = stream_of(p.q_start, p.seqs, t, lane);
-      q0 = __ldg(p.q_start + s);
-      q1 = __ldg(p.q_start + s + 1);
-      len = __ldg(p.lens + s);
+      q0 = p.q_start[s];
+      q1 = p.q_start[s + 1];
+      len = p.lens[s];
     }
     const long long place = static_cast<long long>(len) - (q1 - q0) + (t - q0);
     const long long j = place / p.page_tokens;
     int page = -1;
     if (t >= q0 && t < q1 && q1 <= p.total && place >= 0 && j < p.max_pages)
-      page = __ldg(p.table + static_cast<size_t>(s) * p.max_pages + j);
+      page = p.table[static_cast<size_t>(s) * p.max_pages + j];
     if (page < 0 || page >= p.pages) {
       if (lane == 0) record_status(p.status, MLA_ERR_RANGE);
       continue;
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kThreads) paged_append_kernel(const AppendK p)
     const size_t row = static_cast<size_t>(page) * p.page_tokens + (place - j * p.page_tokens);
     uint4* dst = p.c + row * c16;
     if (lane < c16) dst[lane] = v;
-    for (int i = lane + 32; i < c16; i += 32) dst[i] = __ldg(src + i);
+    for (int i = lane + 32; i < c16; i += 32) dst[i] = src[i];
     __nv_bfloat16* y = p.kr + row * p.d_r;
     for (int i = lane; i < m; i += 32) {
       const int ia = HALF ? i : 2 * i, ib = HALF ? i + m : 2 * i + 1;

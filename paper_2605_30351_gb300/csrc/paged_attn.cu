@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (blockIdx.x == 0) {
     check_q_start(p.q_start, p.seqs, p.total, p.status);
     for (int s = threadIdx.x; s < p.seqs; s += kThreads) {
-      const int len = __ldg(p.lens + s);
+      const int len = p.lens[s];
       if (len < 0 || len > static_cast<long long>(p.max_pages) * p.page_tokens)
         record_status(p.status, MLA_ERR_RANGE);
     }
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                   : (max(valid, 0) + p.page_tokens - 1) >> page_shift;
         };
         auto look_up = [&](const BlockPos<BN>& at) {
-          return lane < boxes_at(at) ? __ldg(table + at.grp * p.per_group + lane) : -1;
+          return lane < boxes_at(at) ? table[at.grp * p.per_group + lane] : -1;
         };
         int page_ahead = look_up(pos);
         for (int q = 0; q < QST; ++q, ++sc) {

@@ -86,7 +86,7 @@ struct Stream {
 };
 
 __device__ __forceinline__ Stream stream_at(const PagedK& p, int s) {
-  Stream t{__ldg(p.q_start + s), __ldg(p.q_start + s + 1), __ldg(p.lens + s)};
+  Stream t{p.q_start[s], p.q_start[s + 1], p.lens[s]};
   const int q1 = t.n;
   t.n = q1 - t.q0;
   if (t.q0 < 0 || q1 < t.q0 || q1 > p.total || t.len < 0 ||

@@ -1,4 +1,9 @@
 // Device helpers of the paged-cache kernels.
+//
+// These kernels start while the previous one of the stream still runs, and that one may
+// write any of their inputs (lengths, tables, latents, queries): they read them with
+// plain loads after grid_dep_sync, never through the non-coherent path, which asks for
+// data that nothing writes while the kernel is there.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -13,7 +18,7 @@ __device__ __forceinline__ int stream_of(const int* q_start, int seqs, int t, in
   while (n > 1) {
     const int step = (n + 31) / 32;
     const int at = lane * step;
-    const bool le = at < n && __ldg(q_start + lo + at) <= t;
+    const bool le = at < n && q_start[lo + at] <= t;
     const unsigned m = __ballot_sync(0xffffffffu, le);
     const int k = m ? 31 - __clz(m) : 0;
     lo += k * step;
@@ -26,8 +31,8 @@ __device__ __forceinline__ int stream_of(const int* q_start, int seqs, int t, in
 __device__ __forceinline__ void check_q_start(const int* q_start, int seqs, int total,
                                               int* status) {
   for (int s = threadIdx.x; s <= seqs; s += blockDim.x) {
-    const int v = __ldg(q_start + s);
-    const int next = s < seqs ? __ldg(q_start + s + 1) : total;
+    const int v = q_start[s];
+    const int next = s < seqs ? q_start[s + 1] : total;
     if (v > next || (s == 0 && v != 0) || (s == seqs && v != total))
       record_status(status, MLA_ERR_RANGE);
   }

@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (blockIdx.x == 0) {
     check_q_start(p.q_start, p.seqs, p.total, p.status);
     for (int s = threadIdx.x; s < p.seqs; s += kThreads) {
-      const int len = __ldg(p.lens + s);
+      const int len = p.lens[s];
       if (len < 0 || len > static_cast<long long>(p.max_pages) * p.page_tokens)
         record_status(p.status, MLA_ERR_RANGE);
     }
@@ -138,8 +138,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint4 v = make_uint4(0u, 0u, 0u, 0u);
       if (r < n_rows)
         v = pc < kPc
-                ? __ldg(reinterpret_cast<const uint4*>(q_c + (grow + r) * DC) + pc)
-                : __ldg(reinterpret_cast<const uint4*>(q_r + (grow + r) * DR) + (pc - kPc));
+                ? reinterpret_cast<const uint4*>(q_c + (grow + r) * DC)[pc]
+                : reinterpret_cast<const uint4*>(q_r + (grow + r) * DR)[pc - kPc];
       *reinterpret_cast<uint4*>(sQ + r * S::kQStride + pc * 16) = v;
     }
     auto keys_of = [&](int r) {
@@ -162,8 +162,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto look_up = [&](int i) {
       if (i < n_blocks && held(ahead) > 0) {
         const int at = ahead.grp * p.per_group + page_at;
-        page_a = __ldg(table + at);
-        page_b = page_step && held(ahead) > 8 ? __ldg(table + at + 1) : page_a;
+        page_a = table[at];
+        page_b = page_step && held(ahead) > 8 ? table[at + 1] : page_a;
       }
     };
     auto fetch = [&](int i) {

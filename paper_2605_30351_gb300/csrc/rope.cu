@@ -45,15 +45,16 @@ __device__ __forceinline__ void from_f(float v, float& o) { o = v; }
 __device__ __forceinline__ void from_f(float v, __half& o) { o = __float2half_rn(v); }
 __device__ __forceinline__ void from_f(float v, __nv_bfloat16& o) { o = __float2bfloat16_rn(v); }
 
-// (cos, +-sin) of pair i of a token
+// (cos, +-sin) of pair i of a token. Plain loads: a previous kernel that still runs when
+// this one starts may have written the positions.
 __device__ __forceinline__ float2 pair_cs(const RopeK& p, long long t, int i) {
   const int axis = p.axes == 1 || i < p.pairs_t ? 0 : (i < p.pairs_t + p.pairs_h ? 1 : 2);
-  int c = __ldg(p.pos + t * p.axes + axis);
+  int c = p.pos[t * p.axes + axis];
   if (c < 0 || c >= p.table_len) {
     record_status(p.status, MLA_ERR_RANGE);
     c = 0;
   }
-  float2 cs = __ldg(p.table + static_cast<size_t>(c) * p.pairs + i);
+  float2 cs = p.table[static_cast<size_t>(c) * p.pairs + i];
   cs.y *= p.sign;
   return cs;
 }
