@@ -201,11 +201,11 @@ __global__ void __launch_bounds__(kMeta) resize_kernel(const Pool p, const int* 
 
 // n 16-byte pieces by the block: kFlight loads of a thread before its first store,
 // so that a unit of a page and layer (28 KB at 64 tokens of 224 values) is mostly in
-// flight at once.
+// flight at once. Counted in 64 bits: a page of wide rows may hold 2^31 pieces.
 constexpr int kFlight = 4;
 
-__device__ __forceinline__ void copy_pieces(const uint4* src, uint4* dst, int n) {
-  for (int i0 = threadIdx.x; i0 < n; i0 += kCopy * kFlight) {
+__device__ __forceinline__ void copy_pieces(const uint4* src, uint4* dst, long long n) {
+  for (long long i0 = threadIdx.x; i0 < n; i0 += kCopy * kFlight) {
     uint4 v[kFlight];
 #pragma unroll
     for (int k = 0; k < kFlight; ++k)
@@ -220,8 +220,8 @@ __device__ __forceinline__ void copy_pieces(const uint4* src, uint4* dst, int n)
 __device__ __forceinline__ void copy_rows(const Pool& p, int from, int to, int rows, int layer) {
   const size_t base = static_cast<size_t>(layer) * p.pages;
   const size_t a = (base + from) * p.page_tokens, b = (base + to) * p.page_tokens;
-  copy_pieces(p.c + a * p.c16, p.c + b * p.c16, rows * p.c16);
-  copy_pieces(p.kr + a * p.k16, p.kr + b * p.k16, rows * p.k16);
+  copy_pieces(p.c + a * p.c16, p.c + b * p.c16, static_cast<long long>(rows) * p.c16);
+  copy_pieces(p.kr + a * p.k16, p.kr + b * p.k16, static_cast<long long>(rows) * p.k16);
 }
 
 __global__ void __launch_bounds__(kCopy) copy_plan_kernel(const Pool p, const int* plan) {
