@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   if (threadIdx.x < 2) p.part_desc[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
-  const long long share = find_share<kBN, kRows>(p, blockIdx.x, gridDim.x, scratch, ends);
+  find_share<kBN, kRows>(p, blockIdx.x, gridDim.x, scratch, ends);
   Walk<kBN, kRows> walk(p, ends);
   Segment g;
   const int ra = lane >> 2, rb = ra + 8;  // the lane's two rows

@@ -116,3 +116,31 @@ def test_infinity_in_a_visible_key(where, streams, new, heads, d_c):
             cols = np.arange(d_c) != 5 if where == "c" else np.ones(d_c, bool)
             assert np.isnan(o[i, h, ~cols]).all(), (s, h)
             assert (np.abs(o[i, h] - ref[h]) <= REL * size[h])[cols].all(), (s, h)
+
+
+@pytest.mark.parametrize("streams,new,heads,d_c", [
+    (97, 3, 12, 192),      # one stream more than threads that look for a share's end
+    (300, 5, 4, 128),
+    (1000, 2, 9, 64),
+    (150, 1, 2, 512),
+    (100, 90, 3, 192),     # two row tiles a stream: CTA pairs
+])
+def test_many_streams_in_tiles_of_128_rows(streams, new, heads, d_c):
+    """More streams than the share search has threads; idle and empty ones among
+    them. All of them against the oracle's attention."""
+    rng = np.random.default_rng(streams)
+    lens = rng.integers(new, 200, streams)
+    n = np.where(np.arange(streams) % 7 == 3, 0, new)
+    lens[5::50] = 0
+    n[5::50] = 0
+    p = Problem(lens.tolist(), n.tolist(), heads=heads, d_c=d_c, page=16, seed=streams)
+    o, q_c, q_r, table, c_all, kr_all = host(p.run(1), p.q_c, p.q_r, p.cache.table,
+                                             p.cache.c[p.layer], p.cache.kr[p.layer])
+    end = np.cumsum(n)
+    for s in np.flatnonzero(n):
+        a = np.arange(lens[s])
+        at = table[s].astype(int)[a // 16], a % 16
+        i = slice(end[s] - n[s], end[s])
+        args = q_c[i], q_r[i], c_all[at], kr_all[at], p.head_dim, 1
+        ref, size = O.attend(*args), O.attend(*args, np.abs(c_all[at]))
+        assert (np.abs(o[i] - ref) <= REL * size).all(), s
