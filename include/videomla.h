@@ -447,6 +447,13 @@ int mla_rope_apply(const mla_rope* rope, const void* x, const int* pos, void* y,
  * Sizes: page_tokens >= 8; d_c and d_r multiples of 8; at most 65,536 streams;
  * pages * page_tokens and max_pages * page_tokens below 2^31 - 2^16; all buffers
  * start on 16-byte boundaries.
+ * A stream keeps its tokens from the first one on: lengths change at the end only, so
+ * a window that slides (the ring above) has no counterpart here, and a stream holds at
+ * most max_pages * page_tokens tokens.
+ * What costs time: attention is fastest with 8, 16, 32, 64 or 128 tokens a page (others
+ * take a whole key block, 128 or at d_c = 512 64 keys, for what is left of a page), and
+ * every call looks at all seqs slots, idle ones too, so a pool should have about as
+ * many slots as streams that run.
  */
 typedef struct mla_paged_cache {
   void* c;
@@ -548,6 +555,8 @@ unsigned long long mla_paged_workspace_bytes(const mla_paged_cache* cache);
  * q_start not ascending within 0..total, a length past max_pages * page_tokens and a
  * table entry that names no page are recorded as MLA_ERR_RANGE: the stream's rows are
  * not written, or the page counts as zeros. total = 0 is MLA_OK.
+ * Scores, softmax statistics and sums are fp32; the weights are rounded to bf16 before
+ * they multiply c, and o once more at the end.
  * The workspace (16-byte aligned) is scratch of the call; calls that overlap on the
  * GPU need one each. MLA_ERR_UNSUPPORTED unless d_c is 64, 128, 192, 256 or 512 and
  * d_r 32 or 64. total * heads is at most 2^30.

@@ -4,9 +4,10 @@
 // One warp per token: it finds the token's stream in q_start with a 32-way
 // search (one load where there are up to 32 streams), then moves the row of d_c +
 // d_r values in 16-byte pieces that were fetched meanwhile. Bound by latency: q_start
-// and lens, then the page table, then the store follow one another. Measured: 64
-// streams' tokens 2.5 us, 18,720 tokens 7.3 us (19.4 MB; two rounds of warps, whose
-// 64 registers leave 32 of them on an SM; held to 32 registers 9.9 us).
+// and lens, then the page table, then the store follow one another, for each token
+// anew. Measured on the GPU (in a CUDA graph): 64 streams' tokens 2.6 us, 18,720 tokens
+// 7.5 us (19.4 MB; the warps, of 48 and 62 registers, take two rounds; held to 32
+// registers 9.9 us, to 64 7.6 us). A call from Python takes 7 us at the least: the host.
 #include "internal.h"
 #include "paged_common.cuh"
 #include "ptx_sm103.cuh"

@@ -4,9 +4,11 @@
 // Every (token, head) row of a stream scores the same latents, so a stream's
 // rows stack along M and a key tile is read once per 128 of them:
 //     S = [q_c | q_r] . [c | k]^T      K = d_c + d_r
-//     P = exp2(S * log2(e)/sqrt(d_h) - m)   running maximum and sum in fp32;
-//                                      P is rounded to bf16 (the type of c, as
-//                                      the MMA takes both operands of one type)
+//     P = exp2(S * log2(e)/sqrt(d_h) - m)   running maximum and sum in fp32, the sum
+//                                      over unrounded weights; P is rounded to
+//                                      bf16 (the type of c, as the MMA takes both
+//                                      operands of one type): the results' errors are
+//                                      1.0 to 1.3 times those of fp32 weights
 //     O += P . c                       N = d_c, c read again from the same tile
 //
 // Work is split evenly whatever the streams look like: all (row tile, key block)
@@ -40,14 +42,19 @@
 // of the scores, which both add up (fp32; the same sum in both). 5 drafted tokens of
 // 16 streams took 44.4 us with all scores computed in both CTAs, 33.5 us so.
 //
-// Measured (12 heads, d_c = 192, d_r = 32): a chunk of 4,680 tokens on 32,760 keys
-// 765 - 812 us in short runs (1.53 TFLOP: 1,885 - 2,000 TFLOP/s, 1.0 - 1.06 of the
+// Pages that do not divide a block (24, 48 or 100 tokens) take one block each, copied as a
+// box of BN rows: 2 x 500 tokens on 8,000 keys 316, 151 and 80 us, with pages of 16, 32, 64
+// or 128 tokens 59 - 61 us.
+//
+// Measured on the GPU (12 heads, d_c = 192, d_r = 32): a chunk of 4,680 tokens on 32,760 keys
+// 765 - 834 us in short runs (1.53 TFLOP: 1,835 - 2,000 TFLOP/s, 0.97 - 1.06 of the
 // measured cuBLAS burst rate) and 850 us in long ones, which hold the GPU at its
-// power limit; bound by the tensor pipe. 9 ragged prompts of up to 333 tokens on up
-// to 5,001 keys (16 heads, d_c = 128, d_r = 64) 48.3 us: 27 blocks a CTA take about
-// 31 of them, bound by the softmax's latency and the MMAs together (tensor pipe 47 %
-// active), the rest is the start, the join and cut tiles. 5 drafted tokens of 16
-// streams (16 heads, d_c = 512, d_r = 64) 33.5 us, on 32,000 keys each 77 us
+// power limit; bound by the tensor pipe; at d_c = 256 and 512 1,415 and 4,786 us. 9 ragged
+// prompts of up to 333 tokens on up to 5,001 keys (16 heads, d_c = 128, d_r = 64) 48 - 54
+// us: 27 blocks a CTA take about 31 of them, bound by the softmax's latency and the MMAs
+// together (tensor pipe 47 % active), the rest is the start, the join and cut tiles. 5
+// drafted tokens of 16 streams (16 heads, d_c = 512, d_r = 64) 33.4 us, on 32,000 keys each
+// 77 us
 // (3.5 TB/s): 1.2 us for a block of 64 keys in turn through score MMAs (64 keys a
 // step run at half rate), the exchange and the softmax, and 15 us of start, first
 // copies and join.
@@ -1036,8 +1043,10 @@ int launch_paged(const PagedAttnArgs& a) {
   return launch_join<DC, S::DV, CL>(k, resident, a);
 }
 
-// Streams of two row tiles and more on average: CTA pairs, which read each key
-// tile from L2 once for 256 rows. Shorter ones would leave half a pair idle.
+// Two row tiles and more a slot of the pool on average: CTA pairs, which read each key
+// tile from L2 once for 256 rows. Shorter ones would leave half a pair idle (ragged
+// prompts 51 us with pairs, 60 without). Idle slots count as short streams here too: a
+// 4,680-token chunk on 32,760 keys 820 us in a pool of 4 slots, 891 of 256.
 template <int DC, int DR>
 int pick(const PagedAttnArgs& a) {
   if constexpr (PagedShape<DC, DR>::kSplit == 2) {
@@ -1086,8 +1095,12 @@ int launch_paged_join(const PagedK& k, int ctas, const PagedAttnArgs& a) {
 }
 
 int launch_paged_attention(const PagedAttnArgs& a) {
-  // Up to 16 rows a stream on average, as one token of 8 to 16 heads: the kernel of
-  // 16-row tiles
+  // Up to 16 rows a slot of the pool on average, as one token of 8 to 16 heads of every
+  // stream: the kernel of 16-row tiles (13.3 -> 11.2 us for one token when it was added).
+  // The host knows the slots and the rows, not which streams have them: a few streams'
+  // chunks in a pool of many idle slots come here too and are slower than in a small pool
+  // (333 tokens on 5,001 keys, 12 heads: 29 us in a pool of 4 slots, 34 of 64, 105 of 256,
+  // 187 of 1,024).
   if (a.d_c <= 256 && static_cast<long long>(a.total) * a.heads <= 16ll * a.seqs)
     return launch_paged_decode(a);
   return a.d_r == 32 ? pick_dc<32>(a) : pick_dc<64>(a);

@@ -159,8 +159,10 @@ struct Place {
 // The shares' ends: place of share id's first block and of the one after its
 // last. Every thread of the block calls it; scratch: 8 long longs and out: two
 // Places in shared memory. Three warps look for each end, all streams among their
-// 96 threads: one search's latency, not two, is part of every call. Returns the
-// cost of a share.
+// 96 threads: one search's latency, not two, is part of every call. With more slots
+// than that, idle ones included, a thread walks several of them in turn: one token of
+// 16 streams on 2,000 keys takes 13.9 us with 16 slots, 21 with 96, 115 with 1,024 and
+// 908 with 8,192. Returns the cost of a share.
 template <int BN, int TR>
 __device__ __forceinline__ long long find_share(const PagedK& p, int id, int groups,
                                                 long long* scratch, Place* out) {

@@ -2,7 +2,8 @@
 // a decoding step, where a stream has up to 16 (token, head) rows.
 //
 // Each key is read once for 16 rows, so the step is bound by reading the cache (at
-// d_c = 192, d_r = 32: 448 bytes and 26 kFLOP a key). The tensor-memory path pads
+// d_c = 192, d_r = 32: 448 bytes and 13.3 kFLOP a key, 30 FLOP a byte where the card does
+// 280 a byte at its measured rates, mma.sync a fraction of that). The tensor-memory path pads
 // 16 rows to 128 and passes every block through four warps in turn (scores,
 // softmax, weights, output); here each of eight warps takes 16 keys of a block of
 // 128 through all steps by itself, with mma.sync tiles of 16 rows, and waits for no
@@ -14,14 +15,21 @@
 //                                          at d_c = 256, where O fills them)
 //     P = exp2(S * log2(e)/sqrt(d_h) - m)  the warp's own running maximum and sum
 //     O += P C                             P's accumulator layout is the next A
-//                                          operand's; C read transposed (ldmatrix)
+//                                          operand's; C read transposed (ldmatrix).
+//                                          P is rounded to bf16, the type of C, as the
+//                                          mma takes both operands of one type; its sum
+//                                          is that of the unrounded weights, in fp32
 // The warps' O, maxima and sums are added up in shared memory at the end of a
 // segment. Shares, partial rows and their join are those of paged_attn.cu.
 //
-// Measured at d_c = 192, d_r = 32, 12 heads: one token on 777 keys 9.4 us and on
+// Pages that do not divide a block of 128 keys are blocks of their own: with 24 tokens a
+// page two warps of eight have keys, and the last of them half a tile (64 streams on 8,000
+// keys 140 us, with 16 or 32 tokens a page 53 and 50).
+//
+// Measured on the GPU at d_c = 192, d_r = 32, 12 heads: one token on 777 keys 9.2 us and on
 // 32,760 keys 13.4 us (latency: the share search, the first keys, the join); 64
-// streams of up to 32,760 keys 78.3 us (416 MB, 5.3 TB/s; 76 us of it this kernel,
-// DRAM at 68 % of its peak over the kernel's start and end). The tensor-memory path
+// streams of up to 32,760 keys 78.0 us (416 MB, 5.3 TB/s; 76 us of it this kernel,
+// DRAM at 70 % of its peak over the kernel's start and end). The tensor-memory path
 // on the same calls: 13.3, 18.0 and 79.4 us, and with pages of 16 tokens, whose
 // copies are 2 KB boxes there, 102 us instead of 84.5.
 #include <cmath>

@@ -8,9 +8,10 @@
 // bytes a (token, pair) are shared by all heads of a token. A thread takes one
 // 16-byte piece (half layout: the two pieces that pair up) of kHeads heads of a
 // token: its cosines and sines are fetched once for all of them, and kHeads
-// loads are in flight at once. Measured: 18,720 tokens x 12 heads x 128 channels of
-// bf16, the last 32 of them turned, 20.4 us (117.6 MB, 5.77 TB/s of a measured copy
-// rate of 6.77); 9,999 x 16 x 128 fp32, half layout, inverse, 29.3 us (5.68 TB/s).
+// loads are in flight at once. Measured on the GPU: 18,720 tokens x 12 heads x 128
+// channels of bf16, the last 32 of them turned, 20.7 us (117.6 MB, 5.67 TB/s of a
+// measured copy rate of 6.77); 9,999 x 16 x 128 fp32, half layout, inverse, 29.2 us
+// (5.69 TB/s).
 // Two heads a thread (22.1 and 29.5 us) or registers held to 48 for more warps (28.0
 // and 39.1 us) were slower. Tensors whose rows or rotated part do not lie on
 // 16-byte boundaries take the kernel that moves single values.
