@@ -566,6 +566,106 @@ int mla_paged_attention(const mla_paged_cache* cache, int layer, const void* q_c
                         int head_dim, int causal_block, void* workspace,
                         unsigned long long workspace_bytes, void* o, void* stream);
 
+/* --------------------------------------------------------------------------
+ * Streams whose window slides: the long-rollout cache (App. D.4, D.5) in pages.
+ *
+ * A stream keeps its first tokens, the sinks, for good, and a window of its newest
+ * ones; the pages between them are given back and the stream's page list closes up,
+ * so a stream may go on for ever in a short list. All of it is the paged cache above:
+ * mla_pages_resize, mla_paged_append and the other calls work on the tokens that are
+ * held.
+ * ------------------------------------------------------------------------ */
+
+/*
+ *  window   tokens that a token sees besides the sinks, its own block included
+ *           (>= 1; as in App. D.4 the newest frames count the current chunk's)
+ *  sinks    first tokens of a stream that every later token sees (>= 0)
+ *  dropped  int32 [seqs], device memory, 4-byte aligned: tokens that mla_pages_slide
+ *           gave back, per stream. NULL: none of any stream
+ * The sinks' pages are those of a stream's first sinks tokens, in whole pages; they are
+ * never given back. The token at place p of the held ones has the index p in its stream
+ * if p lies in the sinks' pages, else p + dropped. Indices stay below 2^31 - 2^16.
+ * A stream keeps its numbers in every call: window may change, sinks not once tokens were
+ * given back.
+ */
+typedef struct mla_paged_window {
+  int window;
+  int sinks;
+  int* dropped;
+} mla_paged_window;
+
+/*
+ * The places of a step's rows: n_new int32 [seqs] new tokens of each stream (0: none).
+ *     q_start[0] = 0,  q_start[s + 1] = q_start[s] + n_new[s]             int32 [seqs + 1]
+ *     new_lens[s] = lens[s] + n_new[s], or -1 where n_new[s] = 0          int32 [seqs]
+ * which mla_pages_resize takes next. A stream that holds no token starts anew: its
+ * dropped becomes 0. A negative count is recorded as MLA_ERR_RANGE and counts as 0;
+ * sums past 2^31 - 1 are recorded and stay there.
+ */
+int mla_paged_window_plan(const mla_paged_cache* cache, const mla_paged_window* window,
+                          const int* n_new, int* q_start, int* new_lens, void* stream);
+
+/*
+ * Coordinates and rows of a step's tokens (after mla_pages_resize): token i of the total
+ * has the index g in its stream (its place among the newest q_start[s+1] - q_start[s]).
+ *     pos[i]       (t, h, w) = (g / T, g % T / frame_width, g % T % frame_width) with T =
+ *                  tokens_per_frame, or (t) alone: int32 [total][axes], axes 1 or 3
+ *     pos_sink[i]  the same with t counted as App. D.5 does, sinks and window held next to
+ *                  each other: t - floor(k / T), k = max(0, e - window - sinks) the tokens
+ *                  between the sinks and the first one that the window holds, e the end of
+ *                  what token i sees (see mla_paged_window_attention). NULL: not wanted
+ *     rows[i]      its row of the pool, page * page_tokens + place in the page. NULL: not
+ *                  wanted
+ * T and frame_width are at least 1, frame_width at most T. A token without a page has the
+ * row -1 (MLA_ERR_RANGE); tokens that are no stream's (a q_start that does not ascend
+ * from 0 to total, recorded too) are not written. A token at a negative place has the
+ * coordinates 0. total = 0 is MLA_OK.
+ */
+int mla_paged_window_positions(const mla_paged_cache* cache, const mla_paged_window* window,
+                               const int* q_start, int total, int causal_block,
+                               int tokens_per_frame, int frame_width, int axes, int* pos,
+                               int* pos_sink, int* rows, void* stream);
+
+/*
+ * mla_paged_attention with a window: the token of index g sees, with e = the end of its
+ * block of causal_block tokens (g / b + 1) * b, at most the stream's end, or with b = 0
+ * the stream's end, the held tokens of the indices
+ *     j < min(sinks, e)   and   max(sinks, e - window) <= j < e.
+ *  q_r_sink  bf16 [total][heads][d_r]: the queries that score the sinks, rotated at
+ *            pos_sink (App. D.5: the sinks move along in front of the window); NULL: q_r
+ *            scores them too
+ * and everything else as there: layout, types, rounding, workspace, rows that see nothing,
+ * what is recorded. Tokens that were given back are not seen, and where some were, nor are
+ * tokens of the sinks' last page behind the sinks. New tokens of such a stream lie behind
+ * the sinks' pages (else its rows are not written, MLA_ERR_RANGE). A key that the masks
+ * hide from all new tokens of a call reaches none of them, NaN included.
+ */
+int mla_paged_window_attention(const mla_paged_cache* cache, const mla_paged_window* window,
+                               int layer, const void* q_c, const void* q_r,
+                               const void* q_r_sink, int total, int heads, const int* q_start,
+                               int head_dim, int causal_block, void* workspace,
+                               unsigned long long workspace_bytes, void* o, void* stream);
+
+/*
+ * Give back the pages between the sinks and the window: keep int32 [seqs] newest tokens
+ * of each stream to keep (-1 = leave the stream alone). The whole pages that lie between
+ * the sinks' pages and the newest keep[s] tokens leave the stream's list, which closes up:
+ *     lens[s] -= n,  dropped[s] += n,  n a multiple of page_tokens.
+ * What the next step's first token sees of a window w is kept with keep = w - 1 (token by
+ * token; w - b with blocks of b tokens that a step fills). A page whose last stream this
+ * was is free afterwards; a page that branches share stays theirs. A page number outside
+ * the pool is recorded as MLA_ERR_RANGE and leaves the list; a stream whose indices would
+ * pass 2^31 - 2^16 is recorded and left alone, as is one whose length its table cannot
+ * hold or whose dropped is negative. dropped must not be NULL.
+ */
+int mla_pages_slide(mla_paged_cache* cache, const mla_paged_window* window, const int* keep,
+                    void* stream);
+
+/* mla_pages_fork for streams whose window slides: dropped[dst[i]] becomes dropped[src[i]]
+ * too. dropped must not be NULL. */
+int mla_pages_window_fork(mla_paged_cache* cache, const mla_paged_window* window,
+                          const int* src, const int* dst, int n, void* stream);
+
 /*
  * Self-test of the bounded device waits that guard every mbarrier wait in the
  * tensor-core kernels (a device wait never hangs: after its limit it records

@@ -159,3 +159,71 @@ def attend(q_c, q_r, c, kr, head_dim, block, v=None):
         w = np.exp(s - s.max(-1, keepdims=True))
         out[i] = (w / w.sum(-1, keepdims=True)) @ v[:k]
     return out
+
+
+# ------------------------------------------------- streams whose window slides
+def front(sinks, page):
+    """Places of the pages that hold a stream's sinks."""
+    return -(-sinks // page) * page
+
+
+def window_sees(place, held, gone, block, window, sinks, page):
+    """(places of the sinks, places of the window) that the token at `place` sees, of a
+    stream that holds `held` tokens and gave `gone` back behind the sinks' pages."""
+    j = np.arange(held)
+    index = np.where(j < front(sinks, page), j, j + gone)
+    if place < 0:
+        return j[:0], j[:0]
+    g, total = place + gone, held + gone
+    end = total if block == 0 else min(total, (g // block + 1) * block)
+    near = (index >= max(sinks, end - window)) & (index < end)
+    if gone:
+        near &= j >= front(sinks, page)
+    return j[(j < sinks) & (index < end)], j[near & (j >= sinks)]
+
+
+def attend_window(q_c, q_r, q_sink, c, kr, places, head_dim):
+    """One token: q_c [H, d_c], q_r and q_sink [H, d_r] over the keys at places =
+    (sinks, window): (output, the same with |c|), which rounding errors go by."""
+    a, b = places
+    if len(a) + len(b) == 0:
+        return np.zeros(q_c.shape), np.zeros(q_c.shape)
+    s = np.concatenate((q_c @ c[a].T + q_sink @ kr[a].T, q_c @ c[b].T + q_r @ kr[b].T), -1)
+    s = s / math.sqrt(head_dim)
+    w = np.exp(s - s.max(-1, keepdims=True))
+    w /= w.sum(-1, keepdims=True)
+    v = np.concatenate((c[a], c[b]))
+    return w @ v, w @ np.abs(v)
+
+
+def slide(pages, gone, keep, sinks):
+    """Pages (above) and gone [seqs] after the pages between sinks and window went."""
+    P, first = pages.P, front(sinks, pages.P) // pages.P
+    for s, k in enumerate(keep):
+        if k < 0:
+            continue
+        row = [int(v) for v in pages.table[s]]
+        n = max(0, (int(pages.lens[s]) - int(k)) // P - first) if pages.lens[s] > k else 0
+        for v in row[first:first + n]:
+            pages.refs[v] -= 1
+        row = row[:first] + row[first + n:] + [-1] * n if n else row
+        pages.table[s] = row
+        pages.lens[s] -= n * P
+        gone[s] += n * P
+
+
+def window_positions(held, gone, new, block, window, sinks, frame, width):
+    """[(t, h, w)], [(t beside the sinks, h, w)] of the newest `new` tokens."""
+    out, beside, total = [], [], held + gone
+    for i in range(new):
+        if held - new + i < 0:
+            out.append((0, 0, 0))
+            beside.append((0, 0, 0))
+            continue
+        g = total - new + i
+        end = total if block == 0 else min(total, (g // block + 1) * block)
+        k = max(0, end - window - sinks)
+        t, r = divmod(g, frame)
+        out.append((t, r // width, r % width))
+        beside.append((t - k // frame, r // width, r % width))
+    return out, beside

@@ -184,6 +184,25 @@ struct PagedAttnArgs {
   float scale_log2;     // log2(e) / sqrt(head_dim)
   int* status;
   cudaStream_t stream;
+  // a window that slides (mla_paged_window_attention)
+  const void* q_sink = nullptr;   // bf16 [total][heads][d_r], or none: q_r
+  const int* dropped = nullptr;   // int32 [seqs], or none: zeros
+  int window = 0, sinks = 0;
+};
+
+// Rows of a step's tokens and their coordinates.
+struct PagedPositionsArgs {
+  const int* q_start;   // int32 [seqs + 1]
+  const int* table;     // int32 [seqs][max_pages]
+  const int* lens;      // int32 [seqs]
+  const int* dropped;   // int32 [seqs] or nullptr
+  int* pos;             // int32 [total][axes]
+  int* pos_sink;        // int32 [total][axes] or nullptr
+  int* rows;            // int32 [total] or nullptr
+  int total, seqs, pages, page_tokens, max_pages, window, sinks, causal_block;
+  int tokens_per_frame, frame_width, axes;
+  int* status;
+  cudaStream_t stream;
 };
 
 // Each launcher returns MLA_OK, MLA_ERR_UNSUPPORTED or MLA_ERR_CUDA.
@@ -204,6 +223,14 @@ int launch_pages_resize(const mla_paged_cache& c, const int* new_lens, int* stat
                         cudaStream_t stream);
 int launch_pages_fork(const mla_paged_cache& c, const int* src, const int* dst, int n,
                       int* status, cudaStream_t stream);
+int launch_pages_window_fork(const mla_paged_cache& c, int* dropped, const int* src,
+                             const int* dst, int n, int* status, cudaStream_t stream);
+int launch_pages_slide(const mla_paged_cache& c, const mla_paged_window& w, const int* keep,
+                       int* status, cudaStream_t stream);
+int launch_paged_window_plan(const mla_paged_cache& c, int* dropped, const int* n_new,
+                             int* q_start, int* new_lens, int* status, cudaStream_t stream);
+int launch_paged_positions(const PagedPositionsArgs& a);
+int launch_paged_window_attention(const PagedAttnArgs& a);
 int launch_pages_copy(const mla_paged_cache& c, const int* src, const int* dst, int n,
                       int* status, cudaStream_t stream);
 int launch_pages_compact(const mla_paged_cache& c, int* new_table, int* new_refs, int* status,
@@ -246,6 +273,8 @@ struct PerDevice {
 int check_resident(std::initializer_list<const void*> ptrs);
 int* device_status_ptr();
 int check_rope(const mla_rope* r);
+// Indices of a stream's tokens stay below this.
+constexpr long long kMostTokens = (1ll << 31) - (1 << 16);
 inline bool aligned_to(const void* p, unsigned n) {
   return (reinterpret_cast<unsigned long long>(p) & (n - 1)) == 0;
 }

@@ -33,6 +33,60 @@ int check_cache(const mla_paged_cache* c, bool plan) {
   return check_resident({c->c, c->kr, c->table, c->lens, c->refs, plan ? c->plan : nullptr});
 }
 
+// The window's own rules; dropped may be missing unless the call writes it.
+int check_window(const mla_paged_window* w, bool dropped) {
+  if (!w || w->window < 1 || w->sinks < 0 || (dropped && !w->dropped) ||
+      !aligned_to(w->dropped, 4))
+    return MLA_ERR_ARG;
+  return MLA_OK;
+}
+
+// What both attention calls check, and the arguments without the window's.
+int attention_args(const mla_paged_cache* cache, int layer, const void* q_c, const void* q_r,
+                   int total, int heads, const int* q_start, int head_dim, int causal_block,
+                   void* workspace, unsigned long long workspace_bytes, void* o, void* stream,
+                   PagedAttnArgs& a) {
+  int rc = check_sizes(cache);
+  if (rc != MLA_OK) return rc;
+  if (layer < 0 || layer >= cache->layers || total < 0 || heads < 1 || head_dim < 1 ||
+      causal_block < 0 || static_cast<long long>(total) * heads > (1ll << 30))
+    return MLA_ERR_ARG;
+  const unsigned long long need = paged_attention_workspace(cache->d_c, cache->d_r);
+  if (need == 0) return MLA_ERR_UNSUPPORTED;
+  a.total = total;
+  if (total == 0) return check_cache(cache, false);
+  if (!q_c || !q_r || !q_start || !workspace || !o || !aligned_to(q_c, 16) ||
+      !aligned_to(q_r, 16) || !aligned_to(q_start, 4) || !aligned_to(workspace, 16) ||
+      !aligned_to(o, 16) || workspace_bytes < need)
+    return MLA_ERR_ARG;
+  rc = check_cache(cache, false);
+  if (rc == MLA_OK) rc = check_resident({q_c, q_r, q_start, workspace, o});
+  if (rc != MLA_OK) return rc;
+  const size_t rows = static_cast<size_t>(cache->pages) * cache->page_tokens * layer;
+  a.q_c = q_c;
+  a.q_r = q_r;
+  a.q_start = q_start;
+  a.c = static_cast<char*>(cache->c) + rows * cache->d_c * 2;
+  a.kr = static_cast<char*>(cache->kr) + rows * cache->d_r * 2;
+  a.table = cache->table;
+  a.lens = cache->lens;
+  a.workspace = workspace;
+  a.o = o;
+  a.heads = heads;
+  a.seqs = cache->seqs;
+  a.pages = cache->pages;
+  a.page_tokens = cache->page_tokens;
+  a.max_pages = cache->max_pages;
+  a.d_c = cache->d_c;
+  a.d_r = cache->d_r;
+  a.causal_block = causal_block;
+  a.scale_log2 =
+      static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(head_dim)));
+  a.status = device_status_ptr();
+  a.stream = static_cast<cudaStream_t>(stream);
+  return a.status ? MLA_OK : MLA_ERR_CUDA;
+}
+
 }  // namespace
 }  // namespace vmla
 
@@ -144,47 +198,116 @@ int mla_paged_attention(const mla_paged_cache* cache, int layer, const void* q_c
                         int total, int heads, const int* q_start, int head_dim, int causal_block,
                         void* workspace, unsigned long long workspace_bytes, void* o,
                         void* stream) {
-  int rc = check_sizes(cache);
+  PagedAttnArgs a;
+  const int rc = attention_args(cache, layer, q_c, q_r, total, heads, q_start, head_dim,
+                                causal_block, workspace, workspace_bytes, o, stream, a);
+  if (rc != MLA_OK || total == 0) return rc;
+  return launch_paged_attention(a);
+}
+
+int mla_paged_window_attention(const mla_paged_cache* cache, const mla_paged_window* window,
+                               int layer, const void* q_c, const void* q_r,
+                               const void* q_r_sink, int total, int heads, const int* q_start,
+                               int head_dim, int causal_block, void* workspace,
+                               unsigned long long workspace_bytes, void* o, void* stream) {
+  int rc = check_window(window, false);
+  if (rc == MLA_OK && !aligned_to(q_r_sink, 16)) rc = MLA_ERR_ARG;
   if (rc != MLA_OK) return rc;
-  if (layer < 0 || layer >= cache->layers || total < 0 || heads < 1 || head_dim < 1 ||
-      causal_block < 0 || static_cast<long long>(total) * heads > (1ll << 30))
+  PagedAttnArgs a;
+  rc = attention_args(cache, layer, q_c, q_r, total, heads, q_start, head_dim, causal_block,
+                      workspace, workspace_bytes, o, stream, a);
+  if (rc == MLA_OK) rc = check_resident({q_r_sink, window->dropped});
+  if (rc != MLA_OK || total == 0) return rc;
+  a.q_sink = q_r_sink;
+  a.dropped = window->dropped;
+  a.window = window->window;
+  a.sinks = window->sinks;
+  return launch_paged_window_attention(a);
+}
+
+int mla_paged_window_plan(const mla_paged_cache* cache, const mla_paged_window* window,
+                          const int* n_new, int* q_start, int* new_lens, void* stream) {
+  if (!n_new || !q_start || !new_lens || !aligned_to(n_new, 4) || !aligned_to(q_start, 4) ||
+      !aligned_to(new_lens, 4))
     return MLA_ERR_ARG;
-  const unsigned long long need = paged_attention_workspace(cache->d_c, cache->d_r);
-  if (need == 0) return MLA_ERR_UNSUPPORTED;
+  int rc = check_window(window, false);
+  if (rc == MLA_OK) rc = check_cache(cache, false);
+  if (rc == MLA_OK) rc = check_resident({n_new, q_start, new_lens, window->dropped});
+  if (rc != MLA_OK) return rc;
+  int* status = device_status_ptr();
+  if (!status) return MLA_ERR_CUDA;
+  return launch_paged_window_plan(*cache, window->dropped, n_new, q_start, new_lens, status,
+                                  static_cast<cudaStream_t>(stream));
+}
+
+int mla_paged_window_positions(const mla_paged_cache* cache, const mla_paged_window* window,
+                               const int* q_start, int total, int causal_block,
+                               int tokens_per_frame, int frame_width, int axes, int* pos,
+                               int* pos_sink, int* rows, void* stream) {
+  int rc = check_window(window, false);
+  if (rc == MLA_OK) rc = check_sizes(cache);
+  if (rc != MLA_OK) return rc;
+  if (total < 0 || causal_block < 0 || tokens_per_frame < 1 || frame_width < 1 ||
+      frame_width > tokens_per_frame || (axes != 1 && axes != 3))
+    return MLA_ERR_ARG;
   if (total == 0) return check_cache(cache, false);
-  if (!q_c || !q_r || !q_start || !workspace || !o || !aligned_to(q_c, 16) ||
-      !aligned_to(q_r, 16) || !aligned_to(q_start, 4) || !aligned_to(workspace, 16) ||
-      !aligned_to(o, 16) || workspace_bytes < need)
+  if (!q_start || !pos || !aligned_to(q_start, 4) || !aligned_to(pos, 4) ||
+      !aligned_to(pos_sink, 4) || !aligned_to(rows, 4))
     return MLA_ERR_ARG;
   rc = check_cache(cache, false);
-  if (rc == MLA_OK) rc = check_resident({q_c, q_r, q_start, workspace, o});
+  if (rc == MLA_OK) rc = check_resident({q_start, pos, pos_sink, rows, window->dropped});
   if (rc != MLA_OK) return rc;
-  const size_t rows = static_cast<size_t>(cache->pages) * cache->page_tokens * layer;
-  PagedAttnArgs a;
-  a.q_c = q_c;
-  a.q_r = q_r;
+  PagedPositionsArgs a;
   a.q_start = q_start;
-  a.c = static_cast<char*>(cache->c) + rows * cache->d_c * 2;
-  a.kr = static_cast<char*>(cache->kr) + rows * cache->d_r * 2;
   a.table = cache->table;
   a.lens = cache->lens;
-  a.workspace = workspace;
-  a.o = o;
+  a.dropped = window->dropped;
+  a.pos = pos;
+  a.pos_sink = pos_sink;
+  a.rows = rows;
   a.total = total;
-  a.heads = heads;
   a.seqs = cache->seqs;
   a.pages = cache->pages;
   a.page_tokens = cache->page_tokens;
   a.max_pages = cache->max_pages;
-  a.d_c = cache->d_c;
-  a.d_r = cache->d_r;
+  a.window = window->window;
+  a.sinks = window->sinks;
   a.causal_block = causal_block;
-  a.scale_log2 =
-      static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(head_dim)));
+  a.tokens_per_frame = tokens_per_frame;
+  a.frame_width = frame_width;
+  a.axes = axes;
   a.status = device_status_ptr();
   a.stream = static_cast<cudaStream_t>(stream);
   if (!a.status) return MLA_ERR_CUDA;
-  return launch_paged_attention(a);
+  return launch_paged_positions(a);
+}
+
+int mla_pages_slide(mla_paged_cache* cache, const mla_paged_window* window, const int* keep,
+                    void* stream) {
+  if (!keep || !aligned_to(keep, 4)) return MLA_ERR_ARG;
+  int rc = check_window(window, true);
+  if (rc == MLA_OK) rc = check_cache(cache, false);
+  if (rc == MLA_OK) rc = check_resident({keep, window->dropped});
+  if (rc != MLA_OK) return rc;
+  int* status = device_status_ptr();
+  if (!status) return MLA_ERR_CUDA;
+  return launch_pages_slide(*cache, *window, keep, status, static_cast<cudaStream_t>(stream));
+}
+
+int mla_pages_window_fork(mla_paged_cache* cache, const mla_paged_window* window,
+                          const int* src, const int* dst, int n, void* stream) {
+  if (n < 0 || (n > 0 && (!src || !dst)) || !aligned_to(src, 4) || !aligned_to(dst, 4))
+    return MLA_ERR_ARG;
+  int rc = check_window(window, true);
+  if (rc == MLA_OK) rc = check_sizes(cache);
+  if (rc == MLA_OK && n > cache->seqs) rc = MLA_ERR_ARG;
+  if (rc == MLA_OK) rc = check_cache(cache, false);
+  if (rc == MLA_OK) rc = check_resident({src, dst, window->dropped});
+  if (rc != MLA_OK || n == 0) return rc;
+  int* status = device_status_ptr();
+  if (!status) return MLA_ERR_CUDA;
+  return launch_pages_window_fork(*cache, window->dropped, src, dst, n, status,
+                                  static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

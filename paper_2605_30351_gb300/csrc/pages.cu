@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kCopy)
 }
 
 __global__ void __launch_bounds__(kCopy)
-    fork_kernel(const Pool p, const int* src, const int* dst, int n) {
+    fork_kernel(const Pool p, int* dropped, const int* src, const int* dst, int n) {
   grid_dep_sync();
   const int i = blockIdx.x;
   const int s = src[i], d = dst[i];
@@ -278,7 +278,55 @@ __global__ void __launch_bounds__(kCopy)
     else
       record_status(p.status, MLA_ERR_RANGE);
   }
-  if (threadIdx.x == 0) p.lens[d] = len;
+  if (threadIdx.x == 0) {
+    p.lens[d] = len;
+    if (dropped) dropped[d] = dropped[s];
+  }
+}
+
+// Pages between a stream's sinks and its newest tokens leave its list (a block per
+// stream): their references go first, then the entries behind them move up, kCopy at
+// a time, every entry read before the place it moves to, which lies ahead of it, is
+// written. Bound by latency: lens, then the table, then the references.
+__global__ void __launch_bounds__(kCopy)
+    slide_kernel(const Pool p, int* dropped, const int* keep, int front) {
+  grid_dep_sync();
+  const int s = blockIdx.x;
+  const int kept = keep[s], len = p.lens[s], gone = dropped[s];
+  const long long cap = static_cast<long long>(p.max_pages) * p.page_tokens;
+  if (kept < 0) return;
+  if (len < 0 || len > cap || gone < 0) {
+    if (threadIdx.x == 0) record_status(p.status, MLA_ERR_RANGE);
+    return;
+  }
+  const int n = (len > kept ? len - kept : 0) / p.page_tokens - front;
+  if (n <= 0) return;
+  if (static_cast<long long>(gone) + len >= kMostTokens) {
+    if (threadIdx.x == 0) record_status(p.status, MLA_ERR_RANGE);
+    return;
+  }
+  const int have = pages_of(len, p.page_tokens), left = have - n;
+  int* row = p.table + static_cast<size_t>(s) * p.max_pages;
+  for (int j = front + threadIdx.x; j < front + n; j += kCopy) {
+    const int pg = row[j];
+    if (pg >= 0 && pg < p.pages)
+      atomicSub(p.refs + pg, 1);
+    else
+      record_status(p.status, MLA_ERR_RANGE);
+  }
+  __syncthreads();  // also: every thread has read the stream's numbers
+  for (int j0 = front; j0 < left; j0 += kCopy) {
+    const int j = j0 + threadIdx.x;
+    const int v = j < left ? row[j + n] : 0;
+    __syncthreads();
+    if (j < left) row[j] = v;
+  }
+  __syncthreads();  // the last entries have moved
+  for (int j = left + threadIdx.x; j < have; j += kCopy) row[j] = -1;
+  if (threadIdx.x == 0) {
+    p.lens[s] = len - n * p.page_tokens;
+    dropped[s] = gone + n * p.page_tokens;
+  }
 }
 
 // Packing. plan: [0] pages in use n, [1] pages that move m; then per page where
@@ -406,7 +454,20 @@ int launch_pages_resize(const mla_paged_cache& c, const int* new_lens, int* stat
 
 int launch_pages_fork(const mla_paged_cache& c, const int* src, const int* dst, int n,
                       int* status, cudaStream_t stream) {
-  return launch_pdl(fork_kernel, dim3(n), kCopy, 0, stream, pool_of(c, status), src, dst, n);
+  return launch_pages_window_fork(c, nullptr, src, dst, n, status, stream);
+}
+
+int launch_pages_window_fork(const mla_paged_cache& c, int* dropped, const int* src,
+                             const int* dst, int n, int* status, cudaStream_t stream) {
+  return launch_pdl(fork_kernel, dim3(n), kCopy, 0, stream, pool_of(c, status), dropped, src, dst,
+                    n);
+}
+
+int launch_pages_slide(const mla_paged_cache& c, const mla_paged_window& w, const int* keep,
+                       int* status, cudaStream_t stream) {
+  const long long front = (static_cast<long long>(w.sinks) + c.page_tokens - 1) / c.page_tokens;
+  return launch_pdl(slide_kernel, dim3(c.seqs), kCopy, 0, stream, pool_of(c, status), w.dropped,
+                    keep, static_cast<int>(front));
 }
 
 int launch_pages_copy(const mla_paged_cache& c, const int* src, const int* dst, int n,

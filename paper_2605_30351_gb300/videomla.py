@@ -45,7 +45,8 @@ EXPORTS = ("mla_rope_table_bytes", "mla_rope_table_fill", "mla_config_check",
            "mla_rope_scaled_table_fill", "mla_rope_apply", "mla_paged_check",
            "mla_pages_plan_bytes", "mla_pages_resize", "mla_pages_fork", "mla_pages_copy",
            "mla_pages_compact", "mla_paged_append", "mla_paged_workspace_bytes",
-           "mla_paged_attention",
+           "mla_paged_attention", "mla_paged_window_plan", "mla_paged_window_positions",
+           "mla_paged_window_attention", "mla_pages_slide", "mla_pages_window_fork",
            "mla_selftest_bounded_wait", "mla_status_string", "mla_last_cuda_error", "mla_device_status",
            "mla_debug_rescale_count", "mla_version")
 
@@ -87,6 +88,10 @@ class mla_paged_cache(ctypes.Structure):
         ("seqs", ctypes.c_int), ("max_pages", ctypes.c_int), ("d_c", ctypes.c_int),
         ("d_r", ctypes.c_int),
     ]
+
+
+class mla_paged_window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int), ("sinks", ctypes.c_int), ("dropped", ctypes.c_void_p)]
 
 
 class MlaError(RuntimeError):
@@ -152,7 +157,16 @@ def load():
     lib.mla_paged_workspace_bytes.restype = ctypes.c_ulonglong
     lib.mla_paged_attention.argtypes = [P(mla_paged_cache), I, VP, VP, I, I, VP, I, I, VP,
                                         ctypes.c_ulonglong, VP, VP]
-    for name in ("mla_paged_attention", "mla_rope_scaled_table_fill", "mla_rope_apply", "mla_paged_check",
+    PC, PW = P(mla_paged_cache), P(mla_paged_window)
+    lib.mla_paged_window_plan.argtypes = [PC, PW, VP, VP, VP, VP]
+    lib.mla_paged_window_positions.argtypes = [PC, PW, VP, I, I, I, I, I, VP, VP, VP, VP]
+    lib.mla_paged_window_attention.argtypes = [PC, PW, I, VP, VP, VP, I, I, VP, I, I, VP,
+                                               ctypes.c_ulonglong, VP, VP]
+    lib.mla_pages_slide.argtypes = [PC, PW, VP, VP]
+    lib.mla_pages_window_fork.argtypes = [PC, PW, VP, VP, I, VP]
+    for name in ("mla_paged_window_plan", "mla_paged_window_positions",
+                 "mla_paged_window_attention", "mla_pages_slide", "mla_pages_window_fork",
+                 "mla_paged_attention", "mla_rope_scaled_table_fill", "mla_rope_apply", "mla_paged_check",
                  "mla_pages_resize", "mla_pages_fork", "mla_pages_copy", "mla_pages_compact",
                  "mla_paged_append"):
         getattr(lib, name).restype = I
@@ -601,6 +615,90 @@ def mla_paged_attention(cache, layer, q_c, q_r, q_start, head_dim, causal_block,
                _ptr(q_start, torch.int32, (cache.seqs + 1,), "q_start"), head_dim,
                causal_block, workspace.data_ptr(), workspace.nbytes,
                _ptr(o, bf, (total, heads, cache.d_c), "o"), _stream_ptr(stream)))
+
+
+class PagedWindow:
+    """The window of a paged cache's streams + the C struct: every token sees the
+    first `sinks` tokens and the newest `window` ones; dropped int32 [seqs] counts
+    the tokens that mla_pages_slide gave back (None: nothing is given back)."""
+
+    def __init__(self, window, sinks=0, dropped=None):
+        self.window, self.sinks, self.dropped = int(window), int(sinks), dropped
+        self.seqs = None if dropped is None else dropped.shape[0]
+        self.struct = mla_paged_window(
+            window=self.window, sinks=self.sinks,
+            dropped=None if dropped is None
+            else _dev(dropped, torch.int32, (self.seqs,), "dropped"))
+        self.ref = ctypes.byref(self.struct)
+
+
+def _window_ref(cache, window):
+    if window.seqs is not None and window.seqs != cache.seqs:
+        raise ValueError(f"dropped must have shape {(cache.seqs,)}, got {(window.seqs,)}")
+    return window.ref
+
+
+def mla_paged_window_plan(cache, window, n_new, q_start, new_lens, stream=None):
+    """n_new [seqs] tokens of a step to q_start [seqs + 1] and the lengths for
+    mla_pages_resize (-1: no new tokens); streams that hold nothing start anew."""
+    i32, seqs = torch.int32, cache.seqs
+    _check("mla_paged_window_plan",
+           load().mla_paged_window_plan(
+               cache.ref, _window_ref(cache, window), _ptr(n_new, i32, (seqs,), "n_new"),
+               _ptr(q_start, i32, (seqs + 1,), "q_start"),
+               _ptr(new_lens, i32, (seqs,), "new_lens"), _stream_ptr(stream)))
+
+
+def mla_paged_window_positions(cache, window, q_start, causal_block, tokens_per_frame,
+                               frame_width, pos, pos_sink=None, rows=None, stream=None):
+    """Coordinates of a step's tokens: pos [total, 1 or 3], pos_sink (the same with
+    sinks and window held next to each other) and their rows [total] of the pool."""
+    i32 = torch.int32
+    total, axes = pos.shape
+    _check("mla_paged_window_positions",
+           load().mla_paged_window_positions(
+               cache.ref, _window_ref(cache, window),
+               _ptr(q_start, i32, (cache.seqs + 1,), "q_start"), total, causal_block,
+               tokens_per_frame, frame_width, axes, _ptr(pos, i32, (total, axes), "pos"),
+               None if pos_sink is None else _ptr(pos_sink, i32, (total, axes), "pos_sink"),
+               None if rows is None else _ptr(rows, i32, (total,), "rows"),
+               _stream_ptr(stream)))
+
+
+def mla_paged_window_attention(cache, window, layer, q_c, q_r, q_r_sink, q_start, head_dim,
+                               causal_block, workspace, o, stream=None):
+    """mla_paged_attention over each stream's sinks and window. q_r_sink (or None:
+    q_r) scores the sinks."""
+    bf = torch.bfloat16
+    if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    total, heads, _ = q_c.shape
+    _check("mla_paged_window_attention",
+           load().mla_paged_window_attention(
+               cache.ref, _window_ref(cache, window), layer,
+               _ptr(q_c, bf, (total, heads, cache.d_c), "q_c"),
+               _ptr(q_r, bf, (total, heads, cache.d_r), "q_r"),
+               None if q_r_sink is None
+               else _ptr(q_r_sink, bf, (total, heads, cache.d_r), "q_r_sink"), total, heads,
+               _ptr(q_start, torch.int32, (cache.seqs + 1,), "q_start"), head_dim,
+               causal_block, workspace.data_ptr(), workspace.nbytes,
+               _ptr(o, bf, (total, heads, cache.d_c), "o"), _stream_ptr(stream)))
+
+
+def mla_pages_slide(cache, window, keep, stream=None):
+    """Give back the pages between the sinks' and the newest keep [seqs] tokens
+    (-1: leave the stream alone); the streams' page lists close up."""
+    _check("mla_pages_slide",
+           load().mla_pages_slide(cache.ref, _window_ref(cache, window),
+                                  _ptr(keep, torch.int32, (cache.seqs,), "keep"),
+                                  _stream_ptr(stream)))
+
+
+def mla_pages_window_fork(cache, window, src, dst, stream=None):
+    """mla_pages_fork; the branches take their parents' dropped too."""
+    _check("mla_pages_window_fork",
+           load().mla_pages_window_fork(cache.ref, _window_ref(cache, window),
+                                        *_pairs_of(src, dst), _stream_ptr(stream)))
 
 
 def mla_selftest_bounded_wait(limit_ns, stream=None):
