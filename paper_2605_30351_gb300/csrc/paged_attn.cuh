@@ -59,6 +59,11 @@ struct PagedK {
   Div by_heads, by_group, by_blocks, by_mask;  // by_mask: by `block`
   float scale_log2;
   int* status;
+  // a window that slides: tokens given back by stream (or none), the window, the sinks and
+  // the places of their whole pages; q_r of its own for the sinks
+  const int* dropped;
+  int window, sinks, front;
+  bool turned;
 };
 
 // Partial rows lie as [4 columns][128 rows], which a warp (a lane per row) writes in
@@ -82,36 +87,93 @@ constexpr int kPartHeld = 1, kPartEnds = 2, kPartEmpty = 4;
 constexpr float kLowest = -3.402823466e38f;
 
 struct Stream {
-  int q0, n, len;
+  int q0, n, len, gone;
 };
 
+// WIN: the stream's window slides, here and below.
+template <bool WIN>
+__device__ __forceinline__ bool stream_held(const PagedK& p, int n, int len, int gone) {
+  if (len < 0 || len > static_cast<long long>(p.max_pages) * p.page_tokens) return false;
+  if constexpr (WIN)  // indices below the limit, and new tokens behind the sinks' pages
+    return gone >= 0 && static_cast<long long>(len) + gone < kMostTokens &&
+           (gone == 0 || static_cast<long long>(len) - n >= p.front);
+  return true;
+}
+
+template <bool WIN>
 __device__ __forceinline__ Stream stream_at(const PagedK& p, int s) {
-  Stream t{p.q_start[s], p.q_start[s + 1], p.lens[s]};
+  Stream t{p.q_start[s], p.q_start[s + 1], p.lens[s], 0};
+  if constexpr (WIN)
+    if (p.dropped) t.gone = p.dropped[s];
   const int q1 = t.n;
   t.n = q1 - t.q0;
-  if (t.q0 < 0 || q1 < t.q0 || q1 > p.total || t.len < 0 ||
-      t.len > static_cast<long long>(p.max_pages) * p.page_tokens)
-    t.n = 0;
+  if (t.q0 < 0 || q1 < t.q0 || q1 > p.total || !stream_held<WIN>(p, t.n, t.len, t.gone)) t.n = 0;
   return t;
 }
 
-// Keys that the token at place a (it may be negative) of a stream of `held` tokens
-// sees.
-__device__ __forceinline__ int keys_seen(const PagedK& p, int a, int held) {
-  if (a < 0) return 0;
-  if (p.block == 0) return held;
-  const long long end = static_cast<long long>(p.by_mask(a) + 1) * p.block;
-  return end < held ? static_cast<int>(end) : held;
+// Record lengths that the table cannot hold (and what else stream_held asks for, of
+// streams with new tokens); one block calls it.
+template <bool WIN>
+__device__ __forceinline__ void check_streams(const PagedK& p) {
+  for (int s = threadIdx.x; s < p.seqs; s += blockDim.x) {
+    int n = 0, gone = 0;
+    if constexpr (WIN) {
+      n = p.q_start[s + 1] - p.q_start[s];
+      if (p.dropped && n > 0) gone = p.dropped[s];
+    }
+    if (!stream_held<WIN>(p, n, p.lens[s], gone)) record_status(p.status, MLA_ERR_RANGE);
+  }
 }
 
-// Key blocks of row tile `tile` (TR rows) of a stream: what its last row, which
-// sees most, needs; at least one, so that rows that see nothing are written.
-template <int BN, int TR>
-__device__ __forceinline__ int tile_blocks(const PagedK& p, int n, int len, int tile) {
-  const int last = min(n * p.heads, (tile + 1) * TR) - 1;
-  const int keys = keys_seen(p, len - n + p.by_heads(last), len);
+// Where the keys end that the token at place a (it may be negative) of a stream sees:
+// blocks of the mask count from the stream's start.
+template <bool WIN>
+__device__ __forceinline__ int keys_seen(const PagedK& p, int a, const Stream& st) {
+  if (a < 0) return 0;
+  if (p.block == 0) return st.len;
+  const int gone = WIN ? st.gone : 0;
+  const long long end = static_cast<long long>(p.by_mask(a + gone) + 1) * p.block - gone;
+  return end < st.len ? static_cast<int>(end) : st.len;
+}
+
+// The first key behind the sinks that a token sees whose keys end there.
+__device__ __forceinline__ int first_key(const PagedK& p, int keys, int gone) {
+  return max(gone > 0 ? p.front : p.sinks, keys - p.window);
+}
+
+// Key blocks before place `keys`, the one it lies in included.
+template <int BN>
+__device__ __forceinline__ int blocks_to(const PagedK& p, int keys) {
   const int whole = p.by_group(keys), rest = keys - whole * p.group;
-  return max(1, whole * p.blocks + (rest + BN - 1) / BN);
+  return whole * p.blocks + (rest + BN - 1) / BN;
+}
+
+// The key blocks of row tile `tile` (TR rows) of a stream: what its last row, which sees
+// most, needs; at least one, so that rows that see nothing are written. With a window
+// they are two runs, which the tile counts through: the sinks' blocks 0 .. sb - 1, then
+// those from the first key of the tile's first row on, wb, wb + 1, ... Where the sinks
+// have queries of their own, a block that holds sinks and window keys is in both runs,
+// once for each; else in the first.
+struct Span {
+  int sb, wb, all;
+};
+
+template <int BN, int TR, bool WIN>
+__device__ __forceinline__ Span tile_span(const PagedK& p, const Stream& st, int tile) {
+  const int last = min(st.n * p.heads, (tile + 1) * TR) - 1;
+  const int keys = keys_seen<WIN>(p, st.len - st.n + p.by_heads(last), st);
+  if constexpr (!WIN) return Span{0, 0, max(1, blocks_to<BN>(p, keys))};
+  const int low = first_key(p, keys_seen<WIN>(p, st.len - st.n + p.by_heads(tile * TR), st), st.gone);
+  Span v{blocks_to<BN>(p, min(p.sinks, keys)), 0, 0};
+  int n = 0;
+  if (keys > low) {
+    const int grp = p.by_group(low);
+    v.wb = grp * p.blocks + (low - grp * p.group) / BN;
+    if (!p.turned) v.wb = max(v.wb, v.sb);
+    n = max(0, blocks_to<BN>(p, keys) - v.wb);
+  }
+  v.all = max(1, v.sb + n);
+  return v;
 }
 
 // Cost of a stream's row tiles in keys, as a straight line from the first to the
@@ -122,6 +184,7 @@ __device__ __forceinline__ int tile_blocks(const PagedK& p, int n, int len, int 
 template <int BN>
 constexpr int kTileCost = 4 * BN;
 
+template <bool WIN>
 struct Cost {
   long long first, slope;  // slope in 1/256 keys per tile
   int tiles;
@@ -130,21 +193,54 @@ struct Cost {
   }
 };
 
-template <int BN, int TR>
-__device__ __forceinline__ Cost cost_of(const PagedK& p, const Stream& st) {
-  Cost c{0, 0, 0};
+// With a window the line ends where sinks and window are full, at tile `knee`; from
+// there on all tiles cost the same.
+template <>
+struct Cost<true> {
+  long long first, slope, flat;
+  int tiles, knee;
+  __device__ long long before(int t) const {
+    const int k = min(t, knee);
+    return k * first + ((slope * (static_cast<long long>(k) * (k - 1) / 2)) >> 8) +
+           (t - k) * flat;
+  }
+};
+
+template <int BN, int TR, bool WIN>
+__device__ __forceinline__ Cost<WIN> cost_of(const PagedK& p, const Stream& st) {
+  Cost<WIN> c{};
   if (st.n == 0) return c;
   const int rows = st.n * p.heads;
   c.tiles = (rows + TR - 1) / TR;
-  const int k1 = keys_seen(p, st.len - 1, st.len);
-  c.first = k1 + kTileCost<BN>;
-  if (c.tiles > 1) {
-    const int k0 = keys_seen(p, st.len - st.n + p.by_heads(TR - 1), st.len);
-    if (c.tiles <= 4096) {  // the products stay below 2^63
-      c.first = k0 + kTileCost<BN>;
-      c.slope = static_cast<long long>(__fdividef((k1 - k0) * 256.f, c.tiles - 1.f));
-    } else {
-      c.first = (static_cast<long long>(k0) + k1) / 2 + kTileCost<BN>;
+  const int k1 = keys_seen<WIN>(p, st.len - 1, st);
+  if constexpr (WIN) {
+    // what a row sees of k keys is min(k - off, cap): the keys of the sinks' pages that a
+    // stream which gave pages back does not see are off
+    const int off = st.gone > 0 ? p.front - p.sinks : 0;
+    const long long cap = static_cast<long long>(p.sinks) + p.window;
+    const int v1 = k1 - off;
+    const int v0 = c.tiles > 1
+                       ? keys_seen<WIN>(p, st.len - st.n + p.by_heads(TR - 1), st) - off
+                       : v1;
+    c.flat = min(cap, static_cast<long long>(v1)) + kTileCost<BN>;
+    if (v0 >= c.flat - kTileCost<BN>) return c;  // all tiles alike: the knee is at 0
+    // products below 2^63: slope < 2^39 / tiles, of at most 2^23 tiles
+    c.first = v0 + kTileCost<BN>;
+    c.slope = static_cast<long long>(__fdividef((v1 - v0) * 256.f, c.tiles - 1.f));
+    c.knee = c.tiles;
+    if (v1 > cap)
+      c.knee = min(c.tiles, 1 + static_cast<int>(__fdividef((cap - v0) * (c.tiles - 1.f),
+                                                           static_cast<float>(v1 - v0))));
+  } else {
+    c.first = k1 + kTileCost<BN>;
+    if (c.tiles > 1) {
+      const int k0 = keys_seen<WIN>(p, st.len - st.n + p.by_heads(TR - 1), st);
+      if (c.tiles <= 4096) {  // the products stay below 2^63
+        c.first = k0 + kTileCost<BN>;
+        c.slope = static_cast<long long>(__fdividef((k1 - k0) * 256.f, c.tiles - 1.f));
+      } else {
+        c.first = (static_cast<long long>(k0) + k1) / 2 + kTileCost<BN>;
+      }
     }
   }
   return c;
@@ -152,7 +248,7 @@ __device__ __forceinline__ Cost cost_of(const PagedK& p, const Stream& st) {
 
 struct Place {
   int s, tile, off;  // stream, row tile, key block
-  int all;           // the tile's key blocks
+  Span at;           // the tile's key blocks
   Stream st;
 };
 
@@ -163,7 +259,7 @@ struct Place {
 // than that, idle ones included, a thread walks several of them in turn: one token of
 // 16 streams on 2,000 keys takes 13.9 us with 16 slots, 21 with 96, 115 with 1,024 and
 // 908 with 8,192. Returns the cost of a share.
-template <int BN, int TR>
+template <int BN, int TR, bool WIN>
 __device__ __forceinline__ long long find_share(const PagedK& p, int id, int groups,
                                                 long long* scratch, Place* out) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -171,13 +267,13 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
   const int per = (p.seqs + 95) / 96;
   const int s0 = (threadIdx.x - e * 96) * per;
   long long mine = 0;
-  Stream st{0, 0, 0};
-  Cost c{0, 0, 0};
+  Stream st{0, 0, 0, 0};
+  Cost<WIN> c{};
   if (e < 2)
     for (int k = 0; k < per; ++k)
       if (s0 + k < p.seqs) {
-        st = stream_at(p, s0 + k);
-        c = cost_of<BN, TR>(p, st);
+        st = stream_at<WIN>(p, s0 + k);
+        c = cost_of<BN, TR, WIN>(p, st);
         mine += c.before(c.tiles);
       }
   long long x = mine;
@@ -208,8 +304,8 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
       int s = s0;
       if (per > 1)
         for (; s < p.seqs; ++s) {
-          st = stream_at(p, s);
-          c = cost_of<BN, TR>(p, st);
+          st = stream_at<WIN>(p, s);
+          c = cost_of<BN, TR, WIN>(p, st);
           const long long all = c.before(c.tiles);
           if (rem < all) break;
           rem -= all;
@@ -224,11 +320,11 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
             hi = mid - 1;
         }
         const long long at = c.before(lo);
-        const int blocks = tile_blocks<BN, TR>(p, st.n, st.len, lo);
+        const Span span = tile_span<BN, TR, WIN>(p, st, lo);
         const int off = static_cast<int>(
             static_cast<float>(rem - at) *
-            __fdividef(static_cast<float>(blocks), static_cast<float>(c.before(lo + 1) - at)));
-        out[e] = Place{s, lo, min(off, blocks - 1), blocks, st};
+            __fdividef(static_cast<float>(span.all), static_cast<float>(c.before(lo + 1) - at)));
+        out[e] = Place{s, lo, min(off, span.all - 1), span, st};
       }
     }
   }
@@ -241,34 +337,36 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
 struct Segment {
   Stream st;
   int s, tile;
-  int kb0, kb1, all;   // key blocks [kb0, kb1) of the tile's `all`
+  int kb0, kb1, all;   // key blocks [kb0, kb1) of the tile's `all`, counted as Span does
+  int sb, wb;
 };
 
-template <int BN, int TR>
+template <int BN, int TR, bool WIN>
 struct Walk {
   const PagedK& p;
   Stream st;
-  int s, tile, off, all;  // all < 0: not known yet
+  int s, tile, off;
+  Span span;  // all < 0: not known yet
   int end_s, end_tile, end_off;
   __device__ Walk(const PagedK& k, const Place* ends) : p(k) {
     st = ends[0].st;  // the first segment needs no arithmetic: the search had it all
     s = ends[0].s;
     tile = ends[0].tile;
     off = ends[0].off;
-    all = ends[0].all;
+    span = ends[0].at;
     end_s = ends[1].s;
     end_tile = ends[1].tile;
     end_off = ends[1].off;
   }
   __device__ bool next(Segment& g) {
     if (s >= p.seqs) return false;
-    if (all < 0) {
+    if (span.all < 0) {
       while (tile * TR >= st.n * p.heads) {  // a stream with new tokens
         if (++s >= p.seqs) return false;
-        st = stream_at(p, s);
+        st = stream_at<WIN>(p, s);
         tile = 0;
       }
-      all = tile_blocks<BN, TR>(p, st.n, st.len, tile);
+      span = tile_span<BN, TR, WIN>(p, st, tile);
     }
     const bool last = s == end_s && tile == end_tile;
     if (s > end_s || (s == end_s && tile > end_tile) || (last && off >= end_off)) return false;
@@ -276,16 +374,19 @@ struct Walk {
     g.s = s;
     g.tile = tile;
     g.kb0 = off;
-    g.kb1 = last ? end_off : all;
-    g.all = all;
+    g.kb1 = last ? end_off : span.all;
+    g.all = span.all;
+    g.sb = span.sb;
+    g.wb = span.wb;
     off = 0;
-    all = -1;
+    span.all = -1;
     ++tile;
     return true;
   }
 };
 
-// Place of key block kb: its first token, and the rows of its group from there.
+// Place of key block kb of the pool's: its first token, and the rows of its group from
+// there. The blocks of a segment follow one another from first_block on.
 template <int BN>
 struct BlockPos {
   int grp, sub;
@@ -299,6 +400,38 @@ struct BlockPos {
     }
   }
 };
+
+template <bool WIN>
+__device__ __forceinline__ int first_block(const Segment& g) {
+  return WIN && g.kb0 >= g.sb ? g.wb + (g.kb0 - g.sb) : g.kb0;
+}
+
+// From the tile's block kb to the next.
+template <int BN, bool WIN>
+__device__ __forceinline__ void next_block(const PagedK& p, const Segment& g, int kb,
+                                           BlockPos<BN>& pos) {
+  if (WIN && kb + 1 == g.sb)
+    pos = BlockPos<BN>(p, g.wb);
+  else
+    pos.step(p);
+}
+
+// Whether the masks hide the key at place j from all rows of a tile, whose first row's keys
+// end at first_end and whose last row's at last_end, in one of its blocks: such a key may be
+// NaN, and must not be multiplied by weights of 0. (Where a window is shorter than a block of
+// the mask, keys before each block's window are hidden too.)
+__device__ __forceinline__ bool tile_hides(const PagedK& p, const Stream& st, bool sink_block,
+                                           int first_end, int last_end, int j) {
+  if (j >= last_end) return true;
+  if (sink_block && j < p.sinks) return false;
+  if (sink_block && p.turned) return true;
+  int end = first_end;
+  if (p.block > p.window) {
+    const long long own = static_cast<long long>(p.by_mask(j + st.gone) + 1) * p.block - st.gone;
+    end = max(end, static_cast<int>(min(own, static_cast<long long>(st.len))));
+  }
+  return j < first_key(p, end, st.gone);
+}
 
 // Host side: the kernels' parameters for key blocks of bn tokens.
 inline PagedK paged_params(const PagedAttnArgs& a, int bn, int dv) {
@@ -330,10 +463,19 @@ inline PagedK paged_params(const PagedAttnArgs& a, int bn, int dv) {
   k.by_mask = div_by(k.block > 0 ? k.block : 1);
   k.scale_log2 = a.scale_log2;
   k.status = a.status;
+  k.dropped = a.dropped;
+  k.window = a.window;
+  k.sinks = a.sinks;
+  const long long front =
+      (static_cast<long long>(a.sinks) + a.page_tokens - 1) / a.page_tokens * a.page_tokens;
+  k.front = static_cast<int>(front < kMostTokens ? front : kMostTokens);
+  k.turned = a.q_sink != nullptr && a.sinks > 0;
   return k;
 }
 
-int launch_paged_join(const PagedK& k, int ctas, const PagedAttnArgs& a);
+// CTAs that shared the work, cl of them a pair.
+int launch_paged_join(const PagedK& k, int ctas, int cl, const PagedAttnArgs& a);
 int launch_paged_decode(const PagedAttnArgs& a);
+int launch_window_decode(const PagedAttnArgs& a);
 
 }  // namespace vmla
