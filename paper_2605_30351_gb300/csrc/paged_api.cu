@@ -21,8 +21,8 @@ int check_sizes(const mla_paged_cache* c) {
   return MLA_OK;
 }
 
-// The cache's own buffers, for an operation that needs the plan or not.
-int check_cache(const mla_paged_cache* c, bool plan) {
+// The cache's own buffers are there and aligned, for an operation that needs the plan or not.
+int check_buffers(const mla_paged_cache* c, bool plan) {
   const int rc = check_sizes(c);
   if (rc != MLA_OK) return rc;
   if (!c->c || !c->kr || !c->table || !c->lens || !c->refs || (plan && !c->plan))
@@ -30,6 +30,13 @@ int check_cache(const mla_paged_cache* c, bool plan) {
   if (!aligned_to(c->c, 16) || !aligned_to(c->kr, 16) || !aligned_to(c->table, 16) ||
       !aligned_to(c->lens, 16) || !aligned_to(c->refs, 16) || !aligned_to(c->plan, 16))
     return MLA_ERR_ARG;
+  return MLA_OK;
+}
+
+// They are this GPU's memory too.
+int check_cache(const mla_paged_cache* c, bool plan) {
+  const int rc = check_buffers(c, plan);
+  if (rc != MLA_OK) return rc;
   return check_resident({c->c, c->kr, c->table, c->lens, c->refs, plan ? c->plan : nullptr});
 }
 
@@ -231,8 +238,11 @@ int mla_paged_window_plan(const mla_paged_cache* cache, const mla_paged_window* 
       !aligned_to(new_lens, 4))
     return MLA_ERR_ARG;
   int rc = check_window(window, false);
-  if (rc == MLA_OK) rc = check_cache(cache, false);
-  if (rc == MLA_OK) rc = check_resident({n_new, q_start, new_lens, window->dropped});
+  // the metadata calls look up the addresses that they use only: a lookup is a noticeable
+  // part of so short a call
+  if (rc == MLA_OK) rc = check_buffers(cache, false);
+  if (rc == MLA_OK)
+    rc = check_resident({cache->lens, n_new, q_start, new_lens, window->dropped});
   if (rc != MLA_OK) return rc;
   int* status = device_status_ptr();
   if (!status) return MLA_ERR_CUDA;
@@ -254,8 +264,10 @@ int mla_paged_window_positions(const mla_paged_cache* cache, const mla_paged_win
   if (!q_start || !pos || !aligned_to(q_start, 4) || !aligned_to(pos, 4) ||
       !aligned_to(pos_sink, 4) || !aligned_to(rows, 4))
     return MLA_ERR_ARG;
-  rc = check_cache(cache, false);
-  if (rc == MLA_OK) rc = check_resident({q_start, pos, pos_sink, rows, window->dropped});
+  rc = check_buffers(cache, false);
+  if (rc == MLA_OK)
+    rc = check_resident(
+        {cache->table, cache->lens, q_start, pos, pos_sink, rows, window->dropped});
   if (rc != MLA_OK) return rc;
   PagedPositionsArgs a;
   a.q_start = q_start;
@@ -286,8 +298,9 @@ int mla_pages_slide(mla_paged_cache* cache, const mla_paged_window* window, cons
                     void* stream) {
   if (!keep || !aligned_to(keep, 4)) return MLA_ERR_ARG;
   int rc = check_window(window, true);
-  if (rc == MLA_OK) rc = check_cache(cache, false);
-  if (rc == MLA_OK) rc = check_resident({keep, window->dropped});
+  if (rc == MLA_OK) rc = check_buffers(cache, false);
+  if (rc == MLA_OK)
+    rc = check_resident({cache->table, cache->lens, cache->refs, keep, window->dropped});
   if (rc != MLA_OK) return rc;
   int* status = device_status_ptr();
   if (!status) return MLA_ERR_CUDA;
@@ -301,8 +314,9 @@ int mla_pages_window_fork(mla_paged_cache* cache, const mla_paged_window* window
   int rc = check_window(window, true);
   if (rc == MLA_OK) rc = check_sizes(cache);
   if (rc == MLA_OK && n > cache->seqs) rc = MLA_ERR_ARG;
-  if (rc == MLA_OK) rc = check_cache(cache, false);
-  if (rc == MLA_OK) rc = check_resident({src, dst, window->dropped});
+  if (rc == MLA_OK) rc = check_buffers(cache, false);
+  if (rc == MLA_OK)
+    rc = check_resident({cache->table, cache->lens, cache->refs, src, dst, window->dropped});
   if (rc != MLA_OK || n == 0) return rc;
   int* status = device_status_ptr();
   if (!status) return MLA_ERR_CUDA;

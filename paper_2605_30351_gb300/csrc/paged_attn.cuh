@@ -86,11 +86,17 @@ constexpr int kPartHeld = 1, kPartEnds = 2, kPartEmpty = 4;
 // sum or value gets into the row whatever its weight.
 constexpr float kLowest = -3.402823466e38f;
 
+// WIN: the stream's window slides, here and below.
+template <bool WIN>
 struct Stream {
+  int q0, n, len;
+  static constexpr int gone = 0;
+};
+template <>
+struct Stream<true> {
   int q0, n, len, gone;
 };
 
-// WIN: the stream's window slides, here and below.
 template <bool WIN>
 __device__ __forceinline__ bool stream_held(const PagedK& p, int n, int len, int gone) {
   if (len < 0 || len > static_cast<long long>(p.max_pages) * p.page_tokens) return false;
@@ -101,10 +107,9 @@ __device__ __forceinline__ bool stream_held(const PagedK& p, int n, int len, int
 }
 
 template <bool WIN>
-__device__ __forceinline__ Stream stream_at(const PagedK& p, int s) {
-  Stream t{p.q_start[s], p.q_start[s + 1], p.lens[s], 0};
-  if constexpr (WIN)
-    if (p.dropped) t.gone = p.dropped[s];
+__device__ __forceinline__ Stream<WIN> stream_at(const PagedK& p, int s) {
+  Stream<WIN> t{p.q_start[s], p.q_start[s + 1], p.lens[s]};
+  if constexpr (WIN) t.gone = p.dropped ? p.dropped[s] : 0;
   const int q1 = t.n;
   t.n = q1 - t.q0;
   if (t.q0 < 0 || q1 < t.q0 || q1 > p.total || !stream_held<WIN>(p, t.n, t.len, t.gone)) t.n = 0;
@@ -128,11 +133,10 @@ __device__ __forceinline__ void check_streams(const PagedK& p) {
 // Where the keys end that the token at place a (it may be negative) of a stream sees:
 // blocks of the mask count from the stream's start.
 template <bool WIN>
-__device__ __forceinline__ int keys_seen(const PagedK& p, int a, const Stream& st) {
+__device__ __forceinline__ int keys_seen(const PagedK& p, int a, const Stream<WIN>& st) {
   if (a < 0) return 0;
   if (p.block == 0) return st.len;
-  const int gone = WIN ? st.gone : 0;
-  const long long end = static_cast<long long>(p.by_mask(a + gone) + 1) * p.block - gone;
+  const long long end = static_cast<long long>(p.by_mask(a + st.gone) + 1) * p.block - st.gone;
   return end < st.len ? static_cast<int>(end) : st.len;
 }
 
@@ -154,26 +158,36 @@ __device__ __forceinline__ int blocks_to(const PagedK& p, int keys) {
 // those from the first key of the tile's first row on, wb, wb + 1, ... Where the sinks
 // have queries of their own, a block that holds sinks and window keys is in both runs,
 // once for each; else in the first.
+template <bool WIN>
 struct Span {
-  int sb, wb, all;
+  int all;
+  static constexpr int sb = 0, wb = 0;
+};
+template <>
+struct Span<true> {
+  int all, sb, wb;
 };
 
 template <int BN, int TR, bool WIN>
-__device__ __forceinline__ Span tile_span(const PagedK& p, const Stream& st, int tile) {
+__device__ __forceinline__ Span<WIN> tile_span(const PagedK& p, const Stream<WIN>& st, int tile) {
   const int last = min(st.n * p.heads, (tile + 1) * TR) - 1;
   const int keys = keys_seen<WIN>(p, st.len - st.n + p.by_heads(last), st);
-  if constexpr (!WIN) return Span{0, 0, max(1, blocks_to<BN>(p, keys))};
-  const int low = first_key(p, keys_seen<WIN>(p, st.len - st.n + p.by_heads(tile * TR), st), st.gone);
-  Span v{blocks_to<BN>(p, min(p.sinks, keys)), 0, 0};
-  int n = 0;
-  if (keys > low) {
-    const int grp = p.by_group(low);
-    v.wb = grp * p.blocks + (low - grp * p.group) / BN;
-    if (!p.turned) v.wb = max(v.wb, v.sb);
-    n = max(0, blocks_to<BN>(p, keys) - v.wb);
+  if constexpr (!WIN) {
+    return Span<WIN>{max(1, blocks_to<BN>(p, keys))};
+  } else {
+    const int low =
+        first_key(p, keys_seen<WIN>(p, st.len - st.n + p.by_heads(tile * TR), st), st.gone);
+    Span<WIN> v{0, blocks_to<BN>(p, min(p.sinks, keys)), 0};
+    int n = 0;
+    if (keys > low) {
+      const int grp = p.by_group(low);
+      v.wb = grp * p.blocks + (low - grp * p.group) / BN;
+      if (!p.turned) v.wb = max(v.wb, v.sb);
+      n = max(0, blocks_to<BN>(p, keys) - v.wb);
+    }
+    v.all = max(1, v.sb + n);
+    return v;
   }
-  v.all = max(1, v.sb + n);
-  return v;
 }
 
 // Cost of a stream's row tiles in keys, as a straight line from the first to the
@@ -207,7 +221,7 @@ struct Cost<true> {
 };
 
 template <int BN, int TR, bool WIN>
-__device__ __forceinline__ Cost<WIN> cost_of(const PagedK& p, const Stream& st) {
+__device__ __forceinline__ Cost<WIN> cost_of(const PagedK& p, const Stream<WIN>& st) {
   Cost<WIN> c{};
   if (st.n == 0) return c;
   const int rows = st.n * p.heads;
@@ -246,10 +260,11 @@ __device__ __forceinline__ Cost<WIN> cost_of(const PagedK& p, const Stream& st) 
   return c;
 }
 
+template <bool WIN>
 struct Place {
   int s, tile, off;  // stream, row tile, key block
-  Span at;           // the tile's key blocks
-  Stream st;
+  Span<WIN> at;      // the tile's key blocks
+  Stream<WIN> st;
 };
 
 // The shares' ends: place of share id's first block and of the one after its
@@ -261,13 +276,13 @@ struct Place {
 // 908 with 8,192. Returns the cost of a share.
 template <int BN, int TR, bool WIN>
 __device__ __forceinline__ long long find_share(const PagedK& p, int id, int groups,
-                                                long long* scratch, Place* out) {
+                                                long long* scratch, Place<WIN>* out) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int e = warp / 3;  // which end; the other warps only wait
   const int per = (p.seqs + 95) / 96;
   const int s0 = (threadIdx.x - e * 96) * per;
   long long mine = 0;
-  Stream st{0, 0, 0, 0};
+  Stream<WIN> st{};
   Cost<WIN> c{};
   if (e < 2)
     for (int k = 0; k < per; ++k)
@@ -320,11 +335,11 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
             hi = mid - 1;
         }
         const long long at = c.before(lo);
-        const Span span = tile_span<BN, TR, WIN>(p, st, lo);
+        const Span<WIN> span = tile_span<BN, TR, WIN>(p, st, lo);
         const int off = static_cast<int>(
             static_cast<float>(rem - at) *
             __fdividef(static_cast<float>(span.all), static_cast<float>(c.before(lo + 1) - at)));
-        out[e] = Place{s, lo, min(off, span.all - 1), span, st};
+        out[e] = Place<WIN>{s, lo, min(off, span.all - 1), span, st};
       }
     }
   }
@@ -334,21 +349,22 @@ __device__ __forceinline__ long long find_share(const PagedK& p, int id, int gro
 
 // Walks a share segment by segment: a segment is a run of key blocks of one row
 // tile. Every role of the CTA walks it for itself.
+template <bool WIN>
 struct Segment {
-  Stream st;
+  Stream<WIN> st;
   int s, tile;
-  int kb0, kb1, all;   // key blocks [kb0, kb1) of the tile's `all`, counted as Span does
-  int sb, wb;
+  int kb0, kb1;  // key blocks [kb0, kb1) of the tile's
+  Span<WIN> at;
 };
 
 template <int BN, int TR, bool WIN>
 struct Walk {
   const PagedK& p;
-  Stream st;
+  Stream<WIN> st;
   int s, tile, off;
-  Span span;  // all < 0: not known yet
+  Span<WIN> span;  // all < 0: not known yet
   int end_s, end_tile, end_off;
-  __device__ Walk(const PagedK& k, const Place* ends) : p(k) {
+  __device__ Walk(const PagedK& k, const Place<WIN>* ends) : p(k) {
     st = ends[0].st;  // the first segment needs no arithmetic: the search had it all
     s = ends[0].s;
     tile = ends[0].tile;
@@ -358,7 +374,7 @@ struct Walk {
     end_tile = ends[1].tile;
     end_off = ends[1].off;
   }
-  __device__ bool next(Segment& g) {
+  __device__ bool next(Segment<WIN>& g) {
     if (s >= p.seqs) return false;
     if (span.all < 0) {
       while (tile * TR >= st.n * p.heads) {  // a stream with new tokens
@@ -375,9 +391,7 @@ struct Walk {
     g.tile = tile;
     g.kb0 = off;
     g.kb1 = last ? end_off : span.all;
-    g.all = span.all;
-    g.sb = span.sb;
-    g.wb = span.wb;
+    g.at = span;
     off = 0;
     span.all = -1;
     ++tile;
@@ -402,16 +416,16 @@ struct BlockPos {
 };
 
 template <bool WIN>
-__device__ __forceinline__ int first_block(const Segment& g) {
-  return WIN && g.kb0 >= g.sb ? g.wb + (g.kb0 - g.sb) : g.kb0;
+__device__ __forceinline__ int first_block(const Segment<WIN>& g) {
+  return WIN && g.kb0 >= g.at.sb ? g.at.wb + (g.kb0 - g.at.sb) : g.kb0;
 }
 
 // From the tile's block kb to the next.
 template <int BN, bool WIN>
-__device__ __forceinline__ void next_block(const PagedK& p, const Segment& g, int kb,
+__device__ __forceinline__ void next_block(const PagedK& p, const Segment<WIN>& g, int kb,
                                            BlockPos<BN>& pos) {
-  if (WIN && kb + 1 == g.sb)
-    pos = BlockPos<BN>(p, g.wb);
+  if (WIN && kb + 1 == g.at.sb)
+    pos = BlockPos<BN>(p, g.at.wb);
   else
     pos.step(p);
 }
@@ -420,7 +434,7 @@ __device__ __forceinline__ void next_block(const PagedK& p, const Segment& g, in
 // end at first_end and whose last row's at last_end, in one of its blocks: such a key may be
 // NaN, and must not be multiplied by weights of 0. (Where a window is shorter than a block of
 // the mask, keys before each block's window are hidden too.)
-__device__ __forceinline__ bool tile_hides(const PagedK& p, const Stream& st, bool sink_block,
+__device__ __forceinline__ bool tile_hides(const PagedK& p, const Stream<true>& st, bool sink_block,
                                            int first_end, int last_end, int j) {
   if (j >= last_end) return true;
   if (sink_block && j < p.sinks) return false;

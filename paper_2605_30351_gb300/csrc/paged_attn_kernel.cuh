@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* mma_drain = pv_done + NB;      // [2]: one per issuing thread
   uint64_t* x_full = mma_drain + 2;        // [2][4]: a warp's scores from the peer
   long long* scratch = reinterpret_cast<long long*>(x_full + 8);  // [8]
-  Place* ends = reinterpret_cast<Place*>(scratch + 8);               // [2]
+  Place<WIN>* ends = reinterpret_cast<Place<WIN>*>(scratch + 8);               // [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ends + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -213,13 +213,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   const long long share =
       find_share<BN, TR, WIN>(p, blockIdx.x / CL, gridDim.x / CL, scratch, ends);
   Walk<BN, TR, WIN> walk(p, ends);
-  Segment g;
+  Segment<WIN> g;
   bool ok = true;
   int it = 0;  // key blocks so far: the phases of the per-block barriers
   auto phase = [](int block) { return static_cast<uint32_t>(block / NB) & 1u; };
   int sc = 0;  // ring stages so far, Q's included: the phases of kv_full, kv_empty
   // a segment with blocks of the sinks has a stage more in front: their own q_r
-  auto own_qr = [&](const Segment& sg) { return WIN && p.turned && sg.kb0 < sg.sb ? 1 : 0; };
+  auto own_qr = [&](const Segment<WIN>& sg) { return WIN && p.turned && sg.kb0 < sg.at.sb ? 1 : 0; };
 
   if (warp < 4) {
     if (warp == 0) {
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int rows = g.st.n * p.heads;
         // a lane per page of a block, looked up one block ahead of its copies
         const int* table = p.table + static_cast<size_t>(g.s) * p.max_pages;
-        BlockPos<BN> pos(p, first_block<WIN>(g));
+        BlockPos<BN> pos(p, first_block(g));
         auto boxes_at = [&](const BlockPos<BN>& at) {  // pages of a block that hold tokens
           const int valid = min(at.rows(p), g.st.len - at.token(p));
           return p.per_group == 1 ? (valid > 0 ? 1 : 0)
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         for (int kb = g.kb0; kb < g.kb1; ++kb, ++sc) {
           const int boxes = boxes_at(pos), sub = pos.sub, page_now = page_ahead;
-          next_block<BN, WIN>(p, g, kb, pos);
+          next_block<BN>(p, g, kb, pos);
           if (kb + 1 < g.kb1) page_ahead = look_up(pos);
           ok = acquire();
           if (!ok) break;
@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             else
               mbar_arrive_cluster(dsmem_addr(smem_u32(&kv_empty[sc % NST]), lane));
           }
-        BlockPos<BN> pos(p, first_block<WIN>(g));
+        BlockPos<BN> pos(p, first_block(g));
         int first_end = 0, last_end = 0;  // of the keys that the tile's rows see
         if constexpr (WIN) {
           const int a = g.st.len - g.st.n;
@@ -361,11 +361,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           last_end = keys_seen<WIN>(
               p, a + p.by_heads(min(g.st.n * p.heads, (g.tile + 1) * TR) - 1), g.st);
         }
-        for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, ++sc, next_block<BN, WIN>(p, g, kb - 1, pos)) {
+        for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, ++sc, next_block<BN>(p, g, kb - 1, pos)) {
           const int st = sc % NST;
           uint8_t* kv = sKV + st * S::kTileBytes;
           const int valid = max(0, min(pos.rows(p), g.st.len - pos.token(p)));
-          const bool sink_block = WIN && kb < g.sb;
+          const bool sink_block = WIN && kb < g.at.sb;
           ok = __all_sync(0xffffffffu, mbar_wait(&kv_full[st], (sc / NST) & 1, wc));
           if (!ok) break;
           if constexpr (WIN) {
@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // (row-major, two values a column) and shared memory (the swizzle the MMA
     // descriptors name). The score MMAs that read the previous Q are done: their
     // scores were awaited.
-    auto load_row = [&](const Segment& sg, Row& w) {
+    auto load_row = [&](const Segment<WIN>& sg, Row& w) {
       const int rows = sg.st.n * p.heads;
       w.tile0 = sg.tile * TR + first_row;
       w.lrow = w.tile0 + r;
@@ -579,8 +579,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (have) ok = load_row(g, w);
     while (ok && have) {
       float m_run = -INFINITY, l_run = 0.f;
-      BlockPos<BN> pos(p, first_block<WIN>(g));
-      for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, next_block<BN, WIN>(p, g, kb - 1, pos)) {
+      BlockPos<BN> pos(p, first_block(g));
+      for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, next_block<BN>(p, g, kb - 1, pos)) {
         if (!mbar_wait(&s_full[it % NB], phase(it), wc)) {
           ok = false;
           break;
@@ -641,12 +641,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         int valid = min(pos.rows(p), w.keys - pos.token(p));
-        bool sees = valid > 0;
+        bool sees = true;  // WIN: the row sees one of the block's keys
         if constexpr (WIN) {
           // the row sees the block's keys below `valid` that are sinks or in its window
           const int token = pos.token(p), low = w.low - token;
           int sinks = 0;
-          if (kb < g.sb) {
+          if (kb < g.at.sb) {
             sinks = p.sinks - token;
             if (p.turned) valid = min(valid, sinks);
           }
@@ -683,7 +683,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float alpha = 1.f;
         bool need = false;
         if (WIN ? m_run == -INFINITY : kb == g.kb0) {
-          m_run = sees ? fmaxf(m_blk, kLowest) : -INFINITY;
+          m_run = (WIN ? sees : valid > 0) ? fmaxf(m_blk, kLowest) : -INFINITY;
         } else if (m_blk > m_run + kRescaleLog2) {
           need = true;
           alpha = ex2_approx(m_run - m_blk);
@@ -746,10 +746,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       // The next segment's Q first, so that its scores are computed while this
       // one's O is written.
       const Row d = w;
-      const bool starts = g.kb0 == 0, stops = g.kb1 == g.all, whole = starts && stops;
+      const bool starts = g.kb0 == 0, stops = g.kb1 == g.at.all, whole = starts && stops;
       const int n_rows = max(0, min(kBM, g.st.n * p.heads - d.tile0));
       const int row0 = g.st.q0 * p.heads + d.tile0;
-      const bool many = static_cast<long long>(g.all) * BN > kManyShares * share;
+      const bool many = static_cast<long long>(g.at.all) * BN > kManyShares * share;
       const bool by_row = many || n_rows <= kFewRows;
       have = walk.next(g);
       if (have) ok = load_row(g, w);

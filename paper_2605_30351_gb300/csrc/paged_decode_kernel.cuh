@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   float* red = reinterpret_cast<float*>(sQ + S::kQBytes);  // [2][warps][16][kRedStride]
   float2* warp_ml = reinterpret_cast<float2*>(red + 2 * kWarps * kRows * kRedStride);
   long long* scratch = reinterpret_cast<long long*>(warp_ml + kWarps * kRows);  // [8]
-  Place* ends = reinterpret_cast<Place*>(scratch + 8);                          // [2]
+  Place<WIN>* ends = reinterpret_cast<Place<WIN>*>(scratch + 8);                          // [2]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   grid_dep_sync();
@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   if (threadIdx.x < 2) p.part_desc[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
   find_share<kBN, kRows, WIN>(p, blockIdx.x, gridDim.x, scratch, ends);
   Walk<kBN, kRows, WIN> walk(p, ends);
-  Segment g;
+  Segment<WIN> g;
   const int ra = lane >> 2, rb = ra + 8;  // the lane's two rows
   const int cq = 2 * (lane & 3);          // and the first of its two columns in a tile of 8
   // ldmatrix addresses: Q, keys (two tiles of 8 keys x 16 values), values transposed
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     const int rows = g.st.n * p.heads, row0 = g.tile * kRows;
     const int n_rows = min(kRows, rows - row0);
     const size_t grow = static_cast<size_t>(g.st.q0) * p.heads + row0;
-    const bool own_qr = WIN && p.turned && g.kb0 < g.sb;  // the sinks' queries are needed
+    const bool own_qr = WIN && p.turned && g.kb0 < g.at.sb;  // the sinks' queries are needed
     constexpr int kPc = DC / 8, kPr = DR / 8;  // 16-byte pieces of a row
     constexpr int kPq = WIN ? kPc + 2 * kPr : kPc + kPr;
     for (int i = threadIdx.x; i < kRows * kPq; i += kDecodeThreads) {
@@ -173,14 +173,14 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     // block ahead of that.
     const int n_blocks = g.kb1 - g.kb0;
     const int* table = p.table + static_cast<size_t>(g.s) * p.max_pages;
-    BlockPos<kBN> ahead(p, first_block<WIN>(g));
+    BlockPos<kBN> ahead(p, first_block(g));
     int page_a = -1, page_b = -1;
     // tokens among the warp's 16 keys of block i; with a window none where no row of the
     // tile sees one of them
     auto held = [&](const BlockPos<kBN>& at, int i) {
       const int token = at.token(p) + 16 * warp;
       if constexpr (WIN) {
-        const bool sink_block = g.kb0 + i < g.sb;
+        const bool sink_block = g.kb0 + i < g.at.sb;
         if (token >= last_end ||
             !((sink_block && token < p.sinks) ||
               (!(sink_block && p.turned) && token + 16 > first_low)))
@@ -202,8 +202,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         unsigned shown = 0xffffu;
         if constexpr (WIN) {
           const int token = ahead.token(p) + 16 * warp;
-          if (g.kb0 + i < g.sb || token < first_low || token + 16 > last_end || p.block > p.window)
-            shown = __ballot_sync(0xffffffffu, lane < 16 && !tile_hides(p, g.st, g.kb0 + i < g.sb, first_end,
+          if (g.kb0 + i < g.at.sb || token < first_low || token + 16 > last_end || p.block > p.window)
+            shown = __ballot_sync(0xffffffffu, lane < 16 && !tile_hides(p, g.st, g.kb0 + i < g.at.sb, first_end,
                                                                         last_end, token + lane));
         }
         if (page_a < 0 || page_a >= p.pages || page_b < 0 || page_b >= p.pages)
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
-      next_block<kBN, WIN>(p, g, g.kb0 + i, ahead);
+      next_block<kBN>(p, g, g.kb0 + i, ahead);
       look_up(i + 1);
     };
     look_up(0);
@@ -259,13 +259,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       for (int c = 0; c < 4; ++c) o[i][c] = 0.f;
     float m_a = -INFINITY, m_b = -INFINITY, l_a = 0.f, l_b = 0.f;
 
-    BlockPos<kBN> pos(p, first_block<WIN>(g));
+    BlockPos<kBN> pos(p, first_block(g));
 #pragma unroll 1
-    for (int i = 0; i < n_blocks; ++i, next_block<kBN, WIN>(p, g, g.kb0 + i - 1, pos)) {
+    for (int i = 0; i < n_blocks; ++i, next_block<kBN>(p, g, g.kb0 + i - 1, pos)) {
       fetch(i + NST - 1);
-      const bool sink_block = WIN && g.kb0 + i < g.sb;
+      const bool sink_block = WIN && g.kb0 + i < g.at.sb;
       if constexpr (WIN && S::kQRegs)
-        if (own_qr && g.kb0 + i == g.sb) {  // from the sinks to the window: the other q_r
+        if (own_qr && g.kb0 + i == g.at.sb) {  // from the sinks to the window: the other q_r
 #pragma unroll
           for (int k = DC / 16; k < kSteps; ++k) ldm4(q[k], q_at + k * 32);
         }
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       warp_ml[warp * kRows + rb] = make_float2(m_b, l_b);
     }
     __syncthreads();
-    const bool whole = g.kb0 == 0 && g.kb1 == g.all;
+    const bool whole = g.kb0 == 0 && g.kb1 == g.at.all;
     const int slot = 2 * blockIdx.x + (g.kb0 == 0 ? 1 : 0);
     // row r over all warps: maximum, sum
     auto total_of = [&](int r) {
@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     if (!whole && threadIdx.x < n_rows) {
       float2 t = total_of(threadIdx.x);
       const int keys = keys_of(threadIdx.x);
-      bool sees = keys > BlockPos<kBN>(p, first_block<WIN>(g)).token(p);
+      bool sees = keys > BlockPos<kBN>(p, first_block(g)).token(p);
       if constexpr (WIN) {  // a run of the sinks' blocks, a run of the window's
         const int low = first_key(p, keys, g.st.gone);
         auto tokens = [&](int kb, int& end) {
@@ -445,16 +445,16 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         };
         int from, to;
         sees = false;
-        if (g.kb0 < g.sb) {
-          tokens(min(g.kb1, g.sb) - 1, to);
+        if (g.kb0 < g.at.sb) {
+          tokens(min(g.kb1, g.at.sb) - 1, to);
           int end;
           from = tokens(g.kb0, end);
           sees = from < min(p.sinks, keys) || (!p.turned && max(from, low) < min(to, keys));
         }
-        if (g.kb1 > g.sb) {
-          tokens(g.wb + (g.kb1 - g.sb) - 1, to);
+        if (g.kb1 > g.at.sb) {
+          tokens(g.at.wb + (g.kb1 - g.at.sb) - 1, to);
           int end;
-          from = tokens(g.wb + max(0, g.kb0 - g.sb), end);
+          from = tokens(g.at.wb + max(0, g.kb0 - g.at.sb), end);
           sees = sees || max(from, low) < min(to, keys);
         }
       }
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     }
     if (!whole && threadIdx.x == 0)
       p.part_desc[slot] = make_int4(static_cast<int>(grow), n_rows,
-                                    kPartHeld | (g.kb1 == g.all ? kPartEnds : 0), 2);
+                                    kPartHeld | (g.kb1 == g.at.all ? kPartEnds : 0), 2);
     __syncthreads();  // sQ, the sums and the buffers are the next segment's
   }
   if (!any && threadIdx.x == 0)
