@@ -64,6 +64,10 @@ struct PagedK {
   const int* dropped;
   int window, sinks, front;
   bool turned;
+  // pages divide a key block (they are a power of two of tokens): blocks are runs of pages
+  // wherever these lie
+  bool compact;
+  int page_log;  // log2 of page_tokens where they do, else 0
 };
 
 // Partial rows lie as [4 columns][128 rows], which a warp (a lane per row) writes in
@@ -153,19 +157,25 @@ __device__ __forceinline__ int blocks_to(const PagedK& p, int keys) {
 }
 
 // The key blocks of row tile `tile` (TR rows) of a stream: what its last row, which sees
-// most, needs; at least one, so that rows that see nothing are written. With a window
-// they are two runs, which the tile counts through: the sinks' blocks 0 .. sb - 1, then
-// those from the first key of the tile's first row on, wb, wb + 1, ... Where the sinks
-// have queries of their own, a block that holds sinks and window keys is in both runs,
-// once for each; else in the first.
+// most, needs; at least one, so that rows that see nothing are written.
+//
+// With a window, what a tile needs is its sinks' pages and the pages from the first key of
+// its first row on. Where pages divide a block they follow one another without a gap: the
+// tile counts its tokens through, u < cut are the sinks' pages, from cut on the token u lies
+// at place u + shift (blocks of 9 ragged prompts, 16 tokens a page and a window of 1,024:
+// 9 a tile instead of 10). Sinks with queries of their own end at a multiple of 16 tokens, as
+// the columns of an MMA do, else of a block. Where pages do not divide a block (cut = shift =
+// 0) the blocks are two runs of the stream's: 0 .. sb - 1 with the sinks, then from wb on;
+// a block that holds sinks and window keys is in both runs where the sinks have queries of
+// their own, else in the first. sb: blocks that hold sinks, in both cases.
 template <bool WIN>
 struct Span {
   int all;
-  static constexpr int sb = 0, wb = 0;
+  static constexpr int sb = 0, wb = 0, cut = 0, shift = 0;
 };
 template <>
 struct Span<true> {
-  int all, sb, wb;
+  int all, sb, wb, cut, shift;
 };
 
 template <int BN, int TR, bool WIN>
@@ -177,15 +187,35 @@ __device__ __forceinline__ Span<WIN> tile_span(const PagedK& p, const Stream<WIN
   } else {
     const int low =
         first_key(p, keys_seen<WIN>(p, st.len - st.n + p.by_heads(tile * TR), st), st.gone);
-    Span<WIN> v{0, blocks_to<BN>(p, min(p.sinks, keys)), 0};
-    int n = 0;
-    if (keys > low) {
-      const int grp = p.by_group(low);
-      v.wb = grp * p.blocks + (low - grp * p.group) / BN;
-      if (!p.turned) v.wb = max(v.wb, v.sb);
-      n = max(0, blocks_to<BN>(p, keys) - v.wb);
+    const int sink_end = min(p.sinks, keys);
+    Span<WIN> v{0, 0, 0, 0, 0};
+    if (p.compact) {
+      const int sp = (sink_end + p.page_tokens - 1) >> p.page_log;
+      if (keys > low) {
+        int wp = low >> p.page_log;
+        if (!p.turned) wp = max(wp, sp);
+        v.cut = sp << p.page_log;
+        if (p.turned && v.cut % 16) v.cut = (v.cut + BN - 1) / BN * BN;
+        v.shift = (wp << p.page_log) - v.cut;
+        v.all = max(1, (keys - v.shift + BN - 1) / BN);
+        v.sb = (v.cut + BN - 1) / BN;
+      } else {  // sinks only
+        v.sb = (sink_end + BN - 1) / BN;
+        v.cut = v.sb * BN;
+        v.all = max(1, v.sb);
+      }
+      v.wb = v.sb;
+    } else {
+      v.sb = blocks_to<BN>(p, sink_end);
+      int n = 0;
+      if (keys > low) {
+        const int grp = p.by_group(low);
+        v.wb = grp * p.blocks + (low - grp * p.group) / BN;
+        if (!p.turned) v.wb = max(v.wb, v.sb);
+        n = max(0, blocks_to<BN>(p, keys) - v.wb);
+      }
+      v.all = max(1, v.sb + n);
     }
-    v.all = max(1, v.sb + n);
     return v;
   }
 }
@@ -430,21 +460,71 @@ __device__ __forceinline__ void next_block(const PagedK& p, const Segment<WIN>& 
     pos.step(p);
 }
 
-// Whether the masks hide the key at place j from all rows of a tile, whose first row's keys
-// end at first_end and whose last row's at last_end, in one of its blocks: such a key may be
-// NaN, and must not be multiplied by weights of 0. (Where a window is shorter than a block of
-// the mask, keys before each block's window are hidden too.)
-__device__ __forceinline__ bool tile_hides(const PagedK& p, const Stream<true>& st, bool sink_block,
-                                           int first_end, int last_end, int j) {
+// Page of a tile's count of them in the stream's list.
+template <bool WIN>
+__device__ __forceinline__ int page_index(const PagedK& p, const Span<WIN>& at, int page) {
+  return WIN && page >= at.cut >> p.page_log ? page + (at.shift >> p.page_log) : page;
+}
+
+// Where the tokens end that are there, as the tile counts them, in the block at `token`.
+template <bool WIN>
+__device__ __forceinline__ int held_to(const PagedK& p, const Segment<WIN>& g, int token) {
+  if constexpr (WIN)
+    if (token < g.at.cut && g.at.cut > p.front) return min(p.front, g.st.len);
+  return g.st.len - g.at.shift;
+}
+
+// What a row sees of a block, counted from its first token: the keys c < sinks, which are
+// sinks, and low <= c < valid.
+struct View {
+  int sinks, low, valid;
+};
+
+// Of a row whose keys end at `keys` and begin behind the sinks at `low`.
+__device__ __forceinline__ View view_of(const PagedK& p, const Segment<true>& g, int kb, int token,
+                                        int keys, int low) {
+  View v{0, low - g.at.shift - token, keys - g.at.shift - token};
+  if (kb < g.at.sb) {
+    v.sinks = min(p.sinks, keys) - token;
+    if (!p.compact && p.turned) v.valid = 0;
+    v.valid = max(v.valid, v.sinks);
+  }
+  return v;
+}
+
+// Whether the token u of the tile's count, in its block kb, is there as one of the sinks'
+// pages, which their own queries score.
+__device__ __forceinline__ bool among_sinks(const PagedK& p, const Segment<true>& g, int kb,
+                                            int u) {
+  return p.compact ? u < g.at.cut : kb < g.at.sb;
+}
+
+// Whether the masks hide that token from all rows of the tile, whose first row's keys end at
+// first_end and whose last row's at last_end: such a key may be NaN, and must not be
+// multiplied by weights of 0. (Where a window is shorter than a block of the mask, keys
+// before each block's window are hidden too.)
+__device__ __forceinline__ bool tile_hides(const PagedK& p, const Segment<true>& g, int kb, int u,
+                                           int first_end, int last_end) {
+  const bool sink = among_sinks(p, g, kb, u);
+  const int j = sink ? u : u + g.at.shift;
   if (j >= last_end) return true;
-  if (sink_block && j < p.sinks) return false;
-  if (sink_block && p.turned) return true;
+  if (sink && j < p.sinks) return false;
+  if (sink && p.turned) return true;
   int end = first_end;
   if (p.block > p.window) {
-    const long long own = static_cast<long long>(p.by_mask(j + st.gone) + 1) * p.block - st.gone;
-    end = max(end, static_cast<int>(min(own, static_cast<long long>(st.len))));
+    const long long own =
+        static_cast<long long>(p.by_mask(j + g.st.gone) + 1) * p.block - g.st.gone;
+    end = max(end, static_cast<int>(min(own, static_cast<long long>(g.st.len))));
   }
-  return j < first_key(p, end, st.gone);
+  return j < first_key(p, end, g.st.gone);
+}
+
+// Whether it may hide one of the block's.
+template <int BN>
+__device__ __forceinline__ bool tile_hides_some(const PagedK& p, const Segment<true>& g, int kb,
+                                                int token, int tile_low, int last_end) {
+  return token + BN > last_end - g.at.shift || p.block > p.window ||
+         (kb < g.at.sb ? token + BN > p.sinks : token < tile_low - g.at.shift);
 }
 
 // Host side: the kernels' parameters for key blocks of bn tokens.
@@ -484,6 +564,9 @@ inline PagedK paged_params(const PagedAttnArgs& a, int bn, int dv) {
       (static_cast<long long>(a.sinks) + a.page_tokens - 1) / a.page_tokens * a.page_tokens;
   k.front = static_cast<int>(front < kMostTokens ? front : kMostTokens);
   k.turned = a.q_sink != nullptr && a.sinks > 0;
+  k.compact = divides;
+  k.page_log = 0;
+  while (divides && (1 << k.page_log) < a.page_tokens) ++k.page_log;
   return k;
 }
 

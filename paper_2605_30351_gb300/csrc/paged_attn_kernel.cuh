@@ -241,12 +241,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int* table = p.table + static_cast<size_t>(g.s) * p.max_pages;
         BlockPos<BN> pos(p, first_block(g));
         auto boxes_at = [&](const BlockPos<BN>& at) {  // pages of a block that hold tokens
-          const int valid = min(at.rows(p), g.st.len - at.token(p));
+          const int valid = min(at.rows(p), held_to(p, g, at.token(p)) - at.token(p));
           return p.per_group == 1 ? (valid > 0 ? 1 : 0)
                                   : (max(valid, 0) + p.page_tokens - 1) >> page_shift;
         };
         auto look_up = [&](const BlockPos<BN>& at) {
-          return lane < boxes_at(at) ? table[at.grp * p.per_group + lane] : -1;
+          return lane < boxes_at(at) ? table[page_index(p, g.at, at.grp * p.per_group + lane)] : -1;
         };
         int page_ahead = look_up(pos);
         for (int q = 0; q < QST; ++q, ++sc) {
@@ -354,32 +354,32 @@ __global__ void __launch_bounds__(kThreads, 1)
               mbar_arrive_cluster(dsmem_addr(smem_u32(&kv_empty[sc % NST]), lane));
           }
         BlockPos<BN> pos(p, first_block(g));
-        int first_end = 0, last_end = 0;  // of the keys that the tile's rows see
+        // where the keys end that the tile's first and last row see; its first behind the sinks
+        int first_end = 0, last_end = 0, tile_low = 0;
         if constexpr (WIN) {
           const int a = g.st.len - g.st.n;
           first_end = keys_seen<WIN>(p, a + p.by_heads(g.tile * TR), g.st);
           last_end = keys_seen<WIN>(
               p, a + p.by_heads(min(g.st.n * p.heads, (g.tile + 1) * TR) - 1), g.st);
+          tile_low = first_key(p, first_end, g.st.gone);
         }
         for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, ++sc, next_block<BN>(p, g, kb - 1, pos)) {
           const int st = sc % NST;
           uint8_t* kv = sKV + st * S::kTileBytes;
-          const int valid = max(0, min(pos.rows(p), g.st.len - pos.token(p)));
-          const bool sink_block = WIN && kb < g.at.sb;
+          const int token = pos.token(p);
+          const int valid = max(0, min(pos.rows(p), held_to(p, g, token) - token));
           ok = __all_sync(0xffffffffu, mbar_wait(&kv_full[st], (sc / NST) & 1, wc));
           if (!ok) break;
           if constexpr (WIN) {
             const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-            const int token = pos.token(p);
             // nothing to clear in most blocks: all rows hold tokens that some row sees
-            if (valid < BN || token + BN > last_end || p.block > p.window ||
-                (sink_block ? token + BN > p.sinks : token < first_key(p, first_end, g.st.gone))) {
+            if (valid < BN || tile_hides_some<BN>(p, g, kb, token, tile_low, last_end)) {
 #pragma unroll 1
               for (int q = 0; q < BN / 32; ++q) {
                 const int i = q * 32 + lane;
                 const unsigned hid = __ballot_sync(
-                    0xffffffffu, i >= valid || tile_hides(p, g.st, sink_block, first_end, last_end,
-                                                          token + i));
+                    0xffffffffu,
+                    i >= valid || tile_hides(p, g, kb, token + i, first_end, last_end));
                 if (hid)
                   for (int cb = 0; cb < DV / 64; ++cb)
                     for (int j = lane; j < 32 * 8; j += 32)
@@ -421,20 +421,42 @@ __global__ void __launch_bounds__(kThreads, 1)
                   umma_ss(d, sdesc(qa + (cb - S::kQcTmem / 64) * 16384 + k * 32, 16, 1024, kSw128),
                           bd, S::kIdescQK, acc);
               }
+            // q_r . k of all columns; where sinks are among them, of the sinks' pages (the
+            // first columns) with their own q_r
+            int own = 0;
+            if constexpr (WIN)
+              if (p.turned && kb < g.at.sb) own = p.compact ? min(BN, g.at.cut - token) : BN;
+            if (own == 0) {
 #pragma unroll
-            for (int k = 0; k < (has_r ? DR / 16 : 0); ++k) {
-              const uint64_t bd = sdesc(ka + S::kKrOff + k * 32, 16, S::kKrSbo, S::kKrSw);
-              if (WIN && p.turned && sink_block) {
-                if constexpr (S::kQsTmem)
-                  umma_ts(d, tmem + S::kTmemQs + k * 8, bd, S::kIdescQK, 1u);
+              for (int k = 0; k < (has_r ? DR / 16 : 0); ++k) {
+                const uint64_t bd = sdesc(ka + S::kKrOff + k * 32, 16, S::kKrSbo, S::kKrSw);
+                if constexpr (S::kQrTmem)
+                  umma_ts(d, tmem + S::kTmemQ + DV / 2 + k * 8, bd, S::kIdescQK, 1u);
                 else
-                  umma_ss(d, sdesc(qa + S::kQsOff + k * 32, 16, S::kKrSbo, S::kKrSw), bd,
+                  umma_ss(d, sdesc(qa + S::kQKrOff + k * 32, 16, S::kKrSbo, S::kKrSw), bd,
                           S::kIdescQK, 1u);
-              } else if constexpr (S::kQrTmem)
-                umma_ts(d, tmem + S::kTmemQ + DV / 2 + k * 8, bd, S::kIdescQK, 1u);
-              else
-                umma_ss(d, sdesc(qa + S::kQKrOff + k * 32, 16, S::kKrSbo, S::kKrSw), bd,
-                        S::kIdescQK, 1u);
+              }
+            } else if (has_r) {
+              for (int c0 = 0; c0 < BN; c0 = own) {  // [0, own), then [own, BN)
+                const bool sinks = c0 == 0;
+                const int n = sinks ? own : BN - own;
+                const uint32_t idesc = idesc_bf16_f32(kBM, 0, false, false) |
+                                       (static_cast<uint32_t>(n >> 3) << 17);
+#pragma unroll
+                for (int k = 0; k < DR / 16; ++k) {
+                  const uint64_t bd =
+                      sdesc(ka + S::kKrOff + c0 * S::kKrRow + k * 32, 16, S::kKrSbo, S::kKrSw);
+                  if (sinks ? S::kQsTmem : S::kQrTmem)
+                    umma_ts(d + c0, tmem + (sinks ? S::kTmemQs : S::kTmemQ + DV / 2) + k * 8, bd,
+                            idesc, 1u);
+                  else
+                    umma_ss(d + c0,
+                            sdesc(qa + (sinks ? S::kQsOff : S::kQKrOff) + k * 32, 16, S::kKrSbo,
+                                  S::kKrSw),
+                            bd, idesc, 1u);
+                }
+                if (!sinks) break;
+              }
             }
             umma_commit(&s_full[it % NB]);
           }
@@ -643,18 +665,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         int valid = min(pos.rows(p), w.keys - pos.token(p));
         bool sees = true;  // WIN: the row sees one of the block's keys
         if constexpr (WIN) {
-          // the row sees the block's keys below `valid` that are sinks or in its window
-          const int token = pos.token(p), low = w.low - token;
-          int sinks = 0;
-          if (kb < g.at.sb) {
-            sinks = p.sinks - token;
-            if (p.turned) valid = min(valid, sinks);
-          }
-          sees = valid > 0 && (sinks > 0 || low < valid);
-          if (low > 0 && sinks < BN) {
+          const View v = view_of(p, g, kb, pos.token(p), w.keys, w.low);
+          valid = min(pos.rows(p), v.valid);
+          sees = v.sinks > 0 || max(v.low, 0) < valid;
+          if (v.low > 0 && v.sinks < BN) {
 #pragma unroll
             for (int c = 0; c < BN; ++c)
-              if (c < low && c >= sinks) sv[c] = -INFINITY;
+              if (c < v.low && c >= v.sinks) sv[c] = -INFINITY;
           }
         }
         if (valid < BN) {

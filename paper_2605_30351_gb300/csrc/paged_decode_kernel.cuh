@@ -180,19 +180,20 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     auto held = [&](const BlockPos<kBN>& at, int i) {
       const int token = at.token(p) + 16 * warp;
       if constexpr (WIN) {
-        const bool sink_block = g.kb0 + i < g.at.sb;
-        if (token >= last_end ||
-            !((sink_block && token < p.sinks) ||
-              (!(sink_block && p.turned) && token + 16 > first_low)))
+        const bool sinks = among_sinks(p, g, g.kb0 + i, token);
+        const int from = sinks ? token : token + g.at.shift;
+        if (from >= last_end ||
+            !((sinks && from < p.sinks) || (!(sinks && p.turned) && from + 16 > first_low)))
           return 0;
+        return min(at.rows(p) - 16 * warp, held_to(p, g, token) - token);
       }
       return min(at.rows(p) - 16 * warp, g.st.len - token);
     };
     auto look_up = [&](int i) {
       if (i < n_blocks && held(ahead, i) > 0) {
         const int at = ahead.grp * p.per_group + page_at;
-        page_a = table[at];
-        page_b = page_step && held(ahead, i) > 8 ? table[at + 1] : page_a;
+        page_a = table[page_index(p, g.at, at)];
+        page_b = page_step && held(ahead, i) > 8 ? table[page_index(p, g.at, at + 1)] : page_a;
       }
     };
     auto fetch = [&](int i) {
@@ -202,9 +203,10 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         unsigned shown = 0xffffu;
         if constexpr (WIN) {
           const int token = ahead.token(p) + 16 * warp;
-          if (g.kb0 + i < g.at.sb || token < first_low || token + 16 > last_end || p.block > p.window)
-            shown = __ballot_sync(0xffffffffu, lane < 16 && !tile_hides(p, g.st, g.kb0 + i < g.at.sb, first_end,
-                                                                        last_end, token + lane));
+          if (g.kb0 + i < g.at.sb || token + 16 > last_end - g.at.shift ||
+              token < first_low - g.at.shift || p.block > p.window)
+            shown = __ballot_sync(0xffffffffu, lane < 16 && !tile_hides(p, g, g.kb0 + i, token + lane,
+                                                                        first_end, last_end));
         }
         if (page_a < 0 || page_a >= p.pages || page_b < 0 || page_b >= p.pages)
           record_status(p.status, MLA_ERR_RANGE);
@@ -250,7 +252,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     if constexpr (S::kQRegs) {
 #pragma unroll
       for (int k = 0; k < kSteps; ++k)
-        ldm4(q[k], q_at + k * 32 + (WIN && k >= DC / 16 && own_qr ? DR * 2 : 0));
+        ldm4(q[k], q_at + k * 32);
     }
     float o[DC / 8][4];
 #pragma unroll
@@ -260,18 +262,23 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     float m_a = -INFINITY, m_b = -INFINITY, l_a = 0.f, l_b = 0.f;
 
     BlockPos<kBN> pos(p, first_block(g));
+    bool q_is_sinks = false;
 #pragma unroll 1
     for (int i = 0; i < n_blocks; ++i, next_block<kBN>(p, g, g.kb0 + i - 1, pos)) {
       fetch(i + NST - 1);
-      const bool sink_block = WIN && g.kb0 + i < g.at.sb;
-      if constexpr (WIN && S::kQRegs)
-        if (own_qr && g.kb0 + i == g.at.sb) {  // from the sinks to the window: the other q_r
+      const int token = pos.token(p) + 16 * warp, room = pos.rows(p) - 16 * warp;
+      bool sinks_q = false;  // the warp's keys are scored by the sinks' own q_r
+      if constexpr (WIN) {
+        sinks_q = own_qr && among_sinks(p, g, g.kb0 + i, token);
+        if (S::kQRegs && sinks_q != q_is_sinks) {
 #pragma unroll
-          for (int k = DC / 16; k < kSteps; ++k) ldm4(q[k], q_at + k * 32);
+          for (int k = DC / 16; k < kSteps; ++k)
+            ldm4(q[k], q_at + k * 32 + (sinks_q ? DR * 2 : 0));
+          q_is_sinks = sinks_q;
         }
+      }
       asm volatile("cp.async.wait_group %0;" ::"n"(NST - 1) : "memory");
       __syncwarp();
-      const int token = pos.token(p) + 16 * warp, room = pos.rows(p) - 16 * warp;
       if (held(pos, i) > 0) {
         const uint32_t ka = ring + (i % NST) * S::kTileBytes;
         float s[2][4];  // two tiles of 8 keys
@@ -294,28 +301,34 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
             mma16816(s[0], q[k], b[0], b[1]);
             mma16816(s[1], q[k], b[2], b[3]);
           } else {
-            ldm4(q[0], q_at + k * 32 + (k >= DC / 16 && sink_block && p.turned ? DR * 2 : 0));
+            ldm4(q[0], q_at + k * 32 + (k >= DC / 16 && sinks_q ? DR * 2 : 0));
             mma16816(s[0], q[0], b[0], b[1]);
             mma16816(s[1], q[0], b[2], b[3]);
           }
         }
-        int lim_a = min(room, keys_a - token), lim_b = min(room, keys_b - token), sinks = 0;
-        if (sink_block) {
-          sinks = p.sinks - token;
-          if (p.turned) {
-            lim_a = min(lim_a, sinks);
-            lim_b = min(lim_b, sinks);
-          }
+        if constexpr (WIN) {
+          const View a = view_of(p, g, g.kb0 + i, token, keys_a, low_a);
+          const View b = view_of(p, g, g.kb0 + i, token, keys_b, low_b);
+          const int lim_a = min(room, a.valid), lim_b = min(room, b.valid);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const int key = 8 * t + cq + c;
+              if (key >= lim_a || (key < a.low && key >= a.sinks)) s[t][c] = -INFINITY;
+              if (key >= lim_b || (key < b.low && key >= b.sinks)) s[t][2 + c] = -INFINITY;
+            }
+        } else {
+          const int lim_a = min(room, keys_a - token), lim_b = min(room, keys_b - token);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const int key = 8 * i + cq + c;
+              if (key >= lim_a) s[i][c] = -INFINITY;
+              if (key >= lim_b) s[i][2 + c] = -INFINITY;
+            }
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const int key = 8 * i + cq + c;
-            if (key >= lim_a || (WIN && key < low_a - token && key >= sinks)) s[i][c] = -INFINITY;
-            if (key >= lim_b || (WIN && key < low_b - token && key >= sinks))
-              s[i][2 + c] = -INFINITY;
-          }
         float x_a = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
         float x_b = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
 #pragma unroll
@@ -436,26 +449,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       float2 t = total_of(threadIdx.x);
       const int keys = keys_of(threadIdx.x);
       bool sees = keys > BlockPos<kBN>(p, first_block(g)).token(p);
-      if constexpr (WIN) {  // a run of the sinks' blocks, a run of the window's
+      if constexpr (WIN) {  // one of the segment's keys
         const int low = first_key(p, keys, g.st.gone);
-        auto tokens = [&](int kb, int& end) {
-          const BlockPos<kBN> at(p, kb);
-          end = at.token(p) + at.rows(p);
-          return at.token(p);
-        };
-        int from, to;
         sees = false;
-        if (g.kb0 < g.at.sb) {
-          tokens(min(g.kb1, g.at.sb) - 1, to);
-          int end;
-          from = tokens(g.kb0, end);
-          sees = from < min(p.sinks, keys) || (!p.turned && max(from, low) < min(to, keys));
-        }
-        if (g.kb1 > g.at.sb) {
-          tokens(g.at.wb + (g.kb1 - g.at.sb) - 1, to);
-          int end;
-          from = tokens(g.at.wb + max(0, g.kb0 - g.at.sb), end);
-          sees = sees || max(from, low) < min(to, keys);
+        BlockPos<kBN> at(p, first_block(g));
+        for (int kb = g.kb0; kb < g.kb1 && !sees; ++kb, next_block<kBN>(p, g, kb - 1, at)) {
+          const View v = view_of(p, g, kb, at.token(p), keys, low);
+          sees = v.sinks > 0 || max(v.low, 0) < min(at.rows(p), v.valid);
         }
       }
       if (sees) t.x = fmaxf(t.x, kLowest);
