@@ -429,6 +429,64 @@ struct Walk {
   }
 };
 
+// Whole tiles instead of a share, for team `id` of `teams`: the first tile of streams id, id +
+// teams, ... and the further tiles of all streams, dealt out in turn from the team after the
+// last stream's on, so that a stream of many rows does not wait for one team. Every warp of the
+// team's CTAs walks them for itself; most calls have no such tiles, and `more` says so.
+template <int BN, int TR>
+struct TeamWalk {
+  const PagedK& p;
+  int id, teams, s;
+  int base, before;  // streams from base on, and the further tiles of those before
+  long long next_more;
+  bool more;
+  __device__ TeamWalk(const PagedK& k, int i, int n, bool further)
+      : p(k), id(i), teams(n), s(i), base(0), before(0), more(further) {
+    next_more = (i + n - k.seqs % n) % n;
+  }
+  __device__ int further_of(int stream) const {
+    if (stream >= p.seqs) return 0;
+    const Stream<true> st = stream_at<true>(p, stream);
+    return st.n > 0 ? (st.n * p.heads + TR - 1) / TR - 1 : 0;
+  }
+  __device__ bool take(Segment<true>& g, const Stream<true>& st, int stream, int tile) {
+    g.st = st;
+    g.s = stream;
+    g.tile = tile;
+    g.at = tile_span<BN, TR, true>(p, st, tile);
+    return true;
+  }
+  __device__ bool next(Segment<true>& g) {
+    while (s < p.seqs) {
+      const Stream<true> st = stream_at<true>(p, s);
+      s += teams;
+      if (st.n > 0) return take(g, st, s - teams, 0);
+    }
+    const int lane = threadIdx.x & 31;
+    while (more && base < p.seqs) {
+      const int mine = further_of(base + lane);
+      int x = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
+      const int all = __shfl_sync(0xffffffffu, x, 31);
+      const long long at = next_more - before;  // among these 32 streams' tiles
+      if (at < all) {
+        const int l = __ffs(__ballot_sync(0xffffffffu, at < x)) - 1;
+        const int first = __shfl_sync(0xffffffffu, x - mine, l);
+        next_more += teams;
+        return take(g, stream_at<true>(p, base + l), base + l,
+                    1 + static_cast<int>(at) - first);
+      }
+      before += all;
+      base += 32;
+    }
+    return false;
+  }
+};
+
 // Place of key block kb of the pool's: its first token, and the rows of its group from
 // there. The blocks of a segment follow one another from first_block on.
 template <int BN>
@@ -574,5 +632,7 @@ inline PagedK paged_params(const PagedAttnArgs& a, int bn, int dv) {
 int launch_paged_join(const PagedK& k, int ctas, int cl, const PagedAttnArgs& a);
 int launch_paged_decode(const PagedAttnArgs& a);
 int launch_window_decode(const PagedAttnArgs& a);
+int launch_window_teams(const PagedAttnArgs& a, int team, int teams);
+int window_team_slots(int team);  // teams of 1, 2, 4 or 8 CTAs that run at a time
 
 }  // namespace vmla

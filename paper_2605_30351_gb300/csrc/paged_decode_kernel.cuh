@@ -48,7 +48,7 @@ constexpr int kBN = 16 * kWarps;              // keys of a block
 constexpr float kMoveLog2 = 8.0f;             // how far a maximum lags behind
 constexpr int kRedStride = 40;                // floats per row of a reduction tile (32 + pad)
 
-template <int DC, int DR, bool WIN>
+template <int DC, int DR, bool WIN, bool TEAM>
 struct DecodeShape {
   static constexpr int DK = DC + DR;
   static constexpr int kTileBytes = 16 * DK * 2;  // a warp's stage of 16 keys:
@@ -58,9 +58,13 @@ struct DecodeShape {
   // Q's rows, with a window the sinks' q_r behind them
   static constexpr int kQStride = (WIN ? DK + DR : DK) * 2 + 16;  // bytes; rows in different banks
   static constexpr int kQBytes = kRows * kQStride;
-  static constexpr int kRedBytes = 2 * kWarps * kRows * kRedStride * 4;
+  // the warps' results, 32 columns at a time in two buffers; in a team one, beside what the
+  // team's CTAs send
+  static constexpr int kRedBufs = TEAM ? 1 : 2;
+  static constexpr int kRedBytes = kRedBufs * kWarps * kRows * kRedStride * 4;
+  static constexpr int kTeamBytes = TEAM ? kRows * (DC * 4 + 8) : 0;
   static constexpr int kMlBytes = kWarps * kRows * 8;
-  static constexpr int kRest = 1024 + kQBytes + kRedBytes + kMlBytes + 192;
+  static constexpr int kRest = 1024 + kQBytes + kRedBytes + kMlBytes + kTeamBytes + 192;
   static constexpr int kFit = (232448 - kRest) / (kTileBytes * kWarps);
   static constexpr int kStages = kFit > 4 ? 4 : kFit;
   static constexpr int kSmemBytes = kRest + kTileBytes * kWarps * kStages;
@@ -94,19 +98,22 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes)
                : "memory");
 }
 
-template <int DC, int DR, bool WIN>
+template <int DC, int DR, bool WIN, bool TEAM>
 __global__ void __launch_bounds__(kDecodeThreads, 1)
     paged_decode_kernel(const uint8_t* c, const uint8_t* kr, const __nv_bfloat16* q_c,
                         const __nv_bfloat16* q_r, const __nv_bfloat16* q_sink, const PagedK p) {
-  using S = DecodeShape<DC, DR, WIN>;
+  using S = DecodeShape<DC, DR, WIN, TEAM>;
   constexpr int NST = S::kStages, kSteps = S::DK / 16;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sKV = align_smem_1024(smem_raw);
   uint8_t* sQ = sKV + NST * kWarps * S::kTileBytes;
   float* red = reinterpret_cast<float*>(sQ + S::kQBytes);  // [2][warps][16][kRedStride]
-  float2* warp_ml = reinterpret_cast<float2*>(red + 2 * kWarps * kRows * kRedStride);
-  long long* scratch = reinterpret_cast<long long*>(warp_ml + kWarps * kRows);  // [8]
-  Place<WIN>* ends = reinterpret_cast<Place<WIN>*>(scratch + 8);                          // [2]
+  float2* warp_ml = reinterpret_cast<float2*>(red + S::kRedBufs * kWarps * kRows * kRedStride);
+  // of a team: [its CTAs][this one's rows] (maximum, sum), then the rows
+  float2* team_ml = warp_ml + kWarps * kRows;
+  float* team_o = reinterpret_cast<float*>(team_ml + (TEAM ? kRows : 0));
+  long long* scratch = reinterpret_cast<long long*>(team_o + (TEAM ? kRows * DC : 0));  // [8]
+  Place<WIN>* ends = reinterpret_cast<Place<WIN>*>(scratch + 8);                         // [2]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   grid_dep_sync();
@@ -114,10 +121,36 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     check_q_start(p.q_start, p.seqs, p.total, p.status);
     check_streams<WIN>(p);
   }
-  if (threadIdx.x < 2) p.part_desc[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
-  find_share<kBN, kRows, WIN>(p, blockIdx.x, gridDim.x, scratch, ends);
-  Walk<kBN, kRows, WIN> walk(p, ends);
+  // What a CTA computes: a share of all tiles' blocks, or as one of a team of CTAs (a
+  // cluster), which takes whole streams in turn, its part of each of their tiles.
+  const int team = TEAM ? static_cast<int>(cluster_nctarank()) : 1;
+  const int member = TEAM ? static_cast<int>(cluster_ctarank()) : 0;
+  if constexpr (TEAM) {
+    cluster_arrive_release();  // a wait before sending: the others run, and have read
+  } else {
+    if (threadIdx.x < 2) p.part_desc[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
+    find_share<kBN, kRows, WIN>(p, blockIdx.x, gridDim.x, scratch, ends);
+  }
   Segment<WIN> g;
+  auto walk = [&]() {
+    if constexpr (TEAM) {
+      bool further = false;  // tiles that are not a stream's first
+      for (int k = threadIdx.x; k < p.seqs; k += kDecodeThreads)
+        further |= static_cast<long long>(p.q_start[k + 1] - p.q_start[k]) * p.heads > kRows;
+      return TeamWalk<kBN, kRows>(p, blockIdx.x / team, gridDim.x / team,
+                                  __syncthreads_or(further));
+    } else {
+      return Walk<kBN, kRows, WIN>(p, ends);
+    }
+  }();
+  auto next_segment = [&]() {
+    if (!walk.next(g)) return false;
+    if constexpr (TEAM) {
+      g.kb0 = static_cast<int>(static_cast<long long>(g.at.all) * member / team);
+      g.kb1 = static_cast<int>(static_cast<long long>(g.at.all) * (member + 1) / team);
+    }
+    return true;
+  };
   const int ra = lane >> 2, rb = ra + 8;  // the lane's two rows
   const int cq = 2 * (lane & 3);          // and the first of its two columns in a tile of 8
   // ldmatrix addresses: Q, keys (two tiles of 8 keys x 16 values), values transposed
@@ -132,27 +165,12 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   const int page_at = small ? 16 * warp / p.page_tokens : 0;
   const int off_at = small ? 16 * warp - page_at * p.page_tokens : 16 * warp;
   bool any = false;
-  while (walk.next(g)) {
+  while (next_segment()) {
     any = true;
     const int rows = g.st.n * p.heads, row0 = g.tile * kRows;
     const int n_rows = min(kRows, rows - row0);
     const size_t grow = static_cast<size_t>(g.st.q0) * p.heads + row0;
     const bool own_qr = WIN && p.turned && g.kb0 < g.at.sb;  // the sinks' queries are needed
-    constexpr int kPc = DC / 8, kPr = DR / 8;  // 16-byte pieces of a row
-    constexpr int kPq = WIN ? kPc + 2 * kPr : kPc + kPr;
-    for (int i = threadIdx.x; i < kRows * kPq; i += kDecodeThreads) {
-      const int r = i / kPq, pc = i - r * kPq;
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (r < n_rows) {
-        if (pc < kPc)
-          v = reinterpret_cast<const uint4*>(q_c + (grow + r) * DC)[pc];
-        else if (pc < kPc + kPr)
-          v = reinterpret_cast<const uint4*>(q_r + (grow + r) * DR)[pc - kPc];
-        else if (own_qr)
-          v = reinterpret_cast<const uint4*>(q_sink + (grow + r) * DR)[pc - kPc - kPr];
-      }
-      *reinterpret_cast<uint4*>(sQ + r * S::kQStride + pc * 16) = v;
-    }
     auto keys_of = [&](int r) {
       return r < n_rows
                  ? keys_seen<WIN>(p, g.st.len - g.st.n + p.by_heads(row0 + r), g.st)
@@ -245,8 +263,22 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       look_up(i + 1);
     };
     look_up(0);
+    // Q's rows (zeros where the tile has none) are on their way while the page is looked up
+    constexpr int kPc = DC / 8, kPr = DR / 8;  // 16-byte pieces of a row
+    constexpr int kPq = WIN ? kPc + 2 * kPr : kPc + kPr;
+    for (int i = threadIdx.x; i < kRows * kPq; i += kDecodeThreads) {
+      const int r = i / kPq, pc = i - r * kPq;
+      if (WIN && pc >= kPc + kPr && !own_qr) continue;
+      const size_t row = grow + (r < n_rows ? r : 0);
+      const __nv_bfloat16* src = pc < kPc ? q_c + row * DC + pc * 8
+                                          : (pc < kPc + kPr ? q_r + row * DR + (pc - kPc) * 8
+                                                            : q_sink + row * DR + (pc - kPc - kPr) * 8);
+      copy16(smem_u32(sQ) + r * S::kQStride + pc * 16, src, r < n_rows ? 16 : 0);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
 #pragma unroll 1
     for (int i = 0; i < NST - 1; ++i) fetch(i);
+    asm volatile("cp.async.wait_group %0;" ::"n"(NST - 1) : "memory");
     __syncthreads();
     uint32_t q[S::kQRegs ? kSteps : 1][4];
     if constexpr (S::kQRegs) {
@@ -283,9 +315,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         const uint32_t ka = ring + (i % NST) * S::kTileBytes;
         float s[2][4];  // two tiles of 8 keys
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) s[i][c] = 0.f;
+          for (int c = 0; c < 4; ++c) s[t][c] = 0.f;
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
           uint32_t b[4];
@@ -321,12 +353,12 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         } else {
           const int lim_a = min(room, keys_a - token), lim_b = min(room, keys_b - token);
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              const int key = 8 * i + cq + c;
-              if (key >= lim_a) s[i][c] = -INFINITY;
-              if (key >= lim_b) s[i][2 + c] = -INFINITY;
+              const int key = 8 * t + cq + c;
+              if (key >= lim_a) s[t][c] = -INFINITY;
+              if (key >= lim_b) s[t][2 + c] = -INFINITY;
             }
         }
         float x_a = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
@@ -394,7 +426,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       warp_ml[warp * kRows + rb] = make_float2(m_b, l_b);
     }
     __syncthreads();
-    const bool whole = g.kb0 == 0 && g.kb1 == g.at.all;
+    const bool whole = TEAM ? team == 1 : g.kb0 == 0 && g.kb1 == g.at.all;
     const int slot = 2 * blockIdx.x + (g.kb0 == 0 ? 1 : 0);
     // row r over all warps: maximum, sum
     auto total_of = [&](int r) {
@@ -417,9 +449,17 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     };
     const float f_a = factor(m_a, t_a), f_b = factor(m_b, t_b);
     const int out_r = threadIdx.x >> 4, out_c = 2 * (threadIdx.x & 15);
+    const int to_rows = kRows / team;  // rows that each of a team joins
+    uint32_t to_o = 0;
+    if constexpr (TEAM)
+      if (team > 1) {
+        cluster_wait_acquire();
+        to_o = dsmem_addr(smem_u32(team_o + ((member * to_rows + out_r % to_rows) * DC + out_c)),
+                          out_r / to_rows);
+      }
 #pragma unroll
-    for (int c = 0; c < DC / 32; ++c) {  // 32 columns at a time, two buffers
-      float* buf = red + (c & 1) * kWarps * kRows * kRedStride;
+    for (int c = 0; c < DC / 32; ++c) {  // 32 columns at a time
+      float* buf = red + (TEAM ? 0 : c & 1) * kWarps * kRows * kRedStride;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float* at = buf + (warp * kRows + ra) * kRedStride + 8 * i + cq;
@@ -440,10 +480,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         if (whole)
           *reinterpret_cast<uint32_t*>(p.o + (grow + out_r) * DC + 32 * c + out_c) =
               pack_bf16x2(sum.x, sum.y);
+        else if constexpr (TEAM)
+          dsmem_st_f32x2(to_o + 32 * c * 4, sum.x, sum.y);
         else
           *reinterpret_cast<float2*>(p.part_o + (static_cast<size_t>(slot) * kBM + out_r) * DC +
                                      32 * c + out_c) = sum;
       }
+      if constexpr (TEAM) __syncthreads();  // the buffer is the next columns'
     }
     if (!whole && threadIdx.x < n_rows) {
       float2 t = total_of(threadIdx.x);
@@ -459,22 +502,59 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         }
       }
       if (sees) t.x = fmaxf(t.x, kLowest);
-      p.part_ml[slot * kBM + threadIdx.x] = t;
+      if constexpr (TEAM) {
+        const int r = threadIdx.x;
+        dsmem_st_f32x2(dsmem_addr(smem_u32(team_ml + member * to_rows + r % to_rows), r / to_rows),
+                       t.x, t.y);
+      } else {
+        p.part_ml[slot * kBM + threadIdx.x] = t;
+      }
     }
-    if (!whole && threadIdx.x == 0)
-      p.part_desc[slot] = make_int4(static_cast<int>(grow), n_rows,
-                                    kPartHeld | (g.kb1 == g.at.all ? kPartEnds : 0), 2);
+    if constexpr (!TEAM)
+      if (!whole && threadIdx.x == 0)
+        p.part_desc[slot] = make_int4(static_cast<int>(grow), n_rows,
+                                      kPartHeld | (g.kb1 == g.at.all ? kPartEnds : 0), 2);
+    if constexpr (TEAM)
+      if (team > 1) {
+        // every CTA joins its rows, parts in their order
+        __syncwarp();
+        cluster_sync();
+        for (int i = threadIdx.x; i < to_rows * (DC / 2); i += kDecodeThreads) {
+          const int r = i / (DC / 2), col = 2 * (i - r * (DC / 2)), row = member * to_rows + r;
+          if (row >= n_rows) continue;
+          float m = -INFINITY;
+          for (int k = 0; k < team; ++k) m = fmaxf(m, team_ml[k * to_rows + r].x);
+          const float ref = m == -INFINITY ? 0.f : m;
+          float l = 0.f, x = 0.f, y = 0.f;
+          for (int k = 0; k < team; ++k) {
+            const float2 ml = team_ml[k * to_rows + r];
+            if (ml.x == -INFINITY) continue;  // the part has no key that the row sees
+            const float2 v = *reinterpret_cast<const float2*>(team_o + (k * to_rows + r) * DC + col);
+            const float w = ex2_approx(ml.x - ref);
+            l += w * ml.y;
+            x += w * v.x;
+            y += w * v.y;
+          }
+          const float f = l == 0.f ? 0.f : 1.f / l;
+          *reinterpret_cast<uint32_t*>(p.o + (grow + row) * DC + col) = pack_bf16x2(x * f, y * f);
+        }
+        cluster_arrive_release();
+      }
     __syncthreads();  // sQ, the sums and the buffers are the next segment's
   }
-  if (!any && threadIdx.x == 0)
-    p.part_desc[2 * blockIdx.x] = make_int4(0, 0, kPartEmpty, 0);
+  if constexpr (TEAM) {
+    cluster_wait_acquire();
+  } else {
+    if (!any && threadIdx.x == 0)
+      p.part_desc[2 * blockIdx.x] = make_int4(0, 0, kPartEmpty, 0);
+  }
 }
 
 template <int DC, int DR, bool WIN>
 int launch_decode(const PagedAttnArgs& a) {
-  using S = DecodeShape<DC, DR, WIN>;
+  using S = DecodeShape<DC, DR, WIN, false>;
   const PagedK k = paged_params(a, kBN, DC);
-  auto kern = paged_decode_kernel<DC, DR, WIN>;
+  auto kern = paged_decode_kernel<DC, DR, WIN, false>;
   static PerDevice known;  // one CTA per SM, asked once
   std::atomic<int>* cell = known.cell();
   if (!cell) return MLA_ERR_CUDA;
@@ -501,6 +581,99 @@ int launch_decode(const PagedAttnArgs& a) {
                             static_cast<const __nv_bfloat16*>(a.q_r),
                             static_cast<const __nv_bfloat16*>(a.q_sink), k);
   return rc != MLA_OK ? rc : launch_paged_join(k, ctas, 1, a);
+}
+
+// Clusters of `team` CTAs with one on an SM that are resident at a time; 0 and the CUDA error
+// recorded if none. Asked once for each size.
+template <int DC, int DR>
+int team_slots(int team) {
+  using S = DecodeShape<DC, DR, true, true>;
+  static_assert(S::kSmemBytes > 232448 / 2, "one CTA per SM");
+  static PerDevice known[9];
+  std::atomic<int>* cell = known[team].cell();
+  if (!cell) return 0;
+  int n = cell->load();
+  if (n == 0) {
+    auto kern = paged_decode_kernel<DC, DR, true, true>;
+    cudaError_t e =
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmemBytes);
+    if (e == cudaSuccess) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(kMaxCtas / team * team);
+      cfg.blockDim = dim3(kDecodeThreads);
+      cfg.dynamicSmemBytes = S::kSmemBytes;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = team;
+      attr[0].val.clusterDim.y = 1;
+      attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      e = cudaOccupancyMaxActiveClusters(&n, kern, &cfg);
+    }
+    if (e != cudaSuccess) {
+      (void)cudaGetLastError();
+      set_last_cuda_error(e);
+      return 0;
+    }
+    n = n < kMaxCtas / team ? n : kMaxCtas / team;
+    cell->store(n);
+  }
+  return n;
+}
+
+// The same in teams of `team` CTAs (a cluster: 1, 2, 4 or 8), up to `teams` of them.
+template <int DC, int DR>
+int launch_teams(const PagedAttnArgs& a, int team, int teams) {
+  using S = DecodeShape<DC, DR, true, true>;
+  const PagedK k = paged_params(a, kBN, DC);
+  auto kern = paged_decode_kernel<DC, DR, true, true>;
+  static PerDevice known;  // the kernel's shared memory, set once
+  std::atomic<int>* cell = known.cell();
+  if (!cell) return MLA_ERR_CUDA;
+  cudaError_t e = cudaSuccess;
+  if (cell->load() == 0) {
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmemBytes);
+    if (e == cudaSuccess) cell->store(1);
+  }
+  if (e == cudaSuccess) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(team * teams);
+    cfg.blockDim = dim3(kDecodeThreads);
+    cfg.dynamicSmemBytes = S::kSmemBytes;
+    cfg.stream = a.stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = team;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see grid_dep_sync
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    e = cudaLaunchKernelEx(&cfg, kern, static_cast<const uint8_t*>(a.c),
+                           static_cast<const uint8_t*>(a.kr),
+                           static_cast<const __nv_bfloat16*>(a.q_c),
+                           static_cast<const __nv_bfloat16*>(a.q_r),
+                           static_cast<const __nv_bfloat16*>(a.q_sink), k);
+  }
+  if (e != cudaSuccess) {
+    (void)cudaGetLastError();
+    set_last_cuda_error(e);
+    return MLA_ERR_CUDA;
+  }
+  return MLA_OK;
+}
+
+template <int DR>
+int pick_teams(const PagedAttnArgs& a, int team, int teams) {
+  switch (a.d_c) {
+    case 64: return launch_teams<64, DR>(a, team, teams);
+    case 128: return launch_teams<128, DR>(a, team, teams);
+    case 192: return launch_teams<192, DR>(a, team, teams);
+    case 256: return launch_teams<256, DR>(a, team, teams);
+    default: return MLA_ERR_UNSUPPORTED;
+  }
 }
 
 template <int DR, bool WIN>

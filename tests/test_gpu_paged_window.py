@@ -204,6 +204,33 @@ def test_long_streams_other_widths(d_c, d_r):
     run_check(Problem([7003, 100, 2500], [2, 90, 40], 3000, 333, d_c=d_c, d_r=d_r, heads=16, page=32), 4)
 
 
+@pytest.mark.parametrize("d_c,d_r", [(64, 32), (128, 64), (192, 32), (256, 64), (512, 32)])
+@pytest.mark.parametrize("page", [16, 100])
+def test_single_tokens_of_many_long_streams(d_c, d_r, page):
+    """As many key blocks as share the work among all SMs, cut tiles joined by a second
+    kernel; one stream has more rows than a tile."""
+    n = 24
+    p = Problem([4300 - 31 * s for s in range(n)], [3 if s == 5 else 1 for s in range(n)], 4000, 130,
+                gone=[page * (s % 3) for s in range(n)], heads=12, d_c=d_c, d_r=d_r, page=page, seed=d_c)
+    o = run_check(p)
+    assert torch.equal(o, p.run())
+
+
+@pytest.mark.parametrize("seqs,new,window", [(1, 40, 60), (3, 7, 300), (40, 2, 100), (150, 1, 100),
+                                             (200, 1, 20), (9, 5, 1000)])
+def test_teams(seqs, new, window):
+    """Teams of one to eight CTAs, each with whole tiles: a stream's further tiles, more tiles
+    than teams, streams that are idle."""
+    rng = np.random.default_rng(seqs)
+    counts = [new if s % 4 else int(rng.integers(0, 2 * new + 1)) for s in range(seqs)]
+    counts[-1] = max(1, counts[-1])
+    lens = [int(rng.integers(n, n + 1500)) for n in counts]
+    for turned in (True, False):
+        p = Problem(lens, counts, window, 20, heads=12, d_c=128, page=32, turned=turned, seed=window)
+        o = run_check(p, 6)
+        assert torch.equal(o, p.run())
+
+
 def test_random_calls():
     """Sizes and masks drawn at random."""
     rng = np.random.default_rng(5)
