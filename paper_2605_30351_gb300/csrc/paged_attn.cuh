@@ -68,6 +68,7 @@ struct PagedK {
   // wherever these lie
   bool compact;
   int page_log;  // log2 of page_tokens where they do, else 0
+  bool o_wide;   // o's rows start on 32-byte boundaries
 };
 
 // Partial rows lie as [4 columns][128 rows], which a warp (a lane per row) writes in
@@ -623,6 +624,7 @@ inline PagedK paged_params(const PagedAttnArgs& a, int bn, int dv) {
   k.front = static_cast<int>(front < kMostTokens ? front : kMostTokens);
   k.turned = a.q_sink != nullptr && a.sinks > 0;
   k.compact = divides;
+  k.o_wide = aligned_to(a.o, 32);
   k.page_log = 0;
   while (divides && (1 << k.page_log) < a.page_tokens) ++k.page_log;
   return k;

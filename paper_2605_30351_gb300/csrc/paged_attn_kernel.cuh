@@ -27,7 +27,7 @@
 //              tile's last blocks are computed
 //   warp 1     clears rows of a stage that hold no token of the stream (they may
 //              hold NaN, and 0 * NaN would reach O), issues the score MMAs
-//   warp 2     issues O += P V
+//   warp 2     issues O += P V; of pairs with a window it does the clearing
 //   warps 4-7  move Q from the ring to its place, then the softmax: thread i owns
 //              row i. It copies a block's scores to registers at once, so the next
 //              block's are computed while it works on the exponentials. Two threads
@@ -140,6 +140,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr int BN = S::BN, DV = S::DV, NST = S::kStages, QST = S::kQStages, NB = S::kBufs;
   constexpr int TR = kBM * CL / S::kSplit;  // rows of a CTA's, or a pair's, tile
   constexpr int MC = S::kSplit == 1 ? CL : 1;  // CTAs that share a stage's boxes
+  // With a window the rows of c that a tile does not see are cleared between the weights and
+  // the output, beside the next scores, where tiles are long (pairs: four chunks 1,100 -> 1,050
+  // us, a prompt of 28,000 tokens 780 -> 760); else before the scores, by the warp that has the
+  // code at hand (19 tokens of 3 streams 29.2 us, 30.0 so).
+  constexpr bool kLate = WIN && CL == 2 && S::kSplit == 1;
   constexpr uint16_t kPair = static_cast<uint16_t>((1u << CL) - 1u);
   static_assert(S::kSplit == 1 || CL == S::kSplit, "split tiles take a pair");
   extern __shared__ uint8_t smem_raw[];
@@ -356,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         BlockPos<BN> pos(p, first_block(g));
         // where the keys end that the tile's first and last row see; its first behind the sinks
         int first_end = 0, last_end = 0, tile_low = 0;
-        if constexpr (WIN) {
+        if constexpr (WIN && !kLate) {
           const int a = g.st.len - g.st.n;
           first_end = keys_seen<WIN>(p, a + p.by_heads(g.tile * TR), g.st);
           last_end = keys_seen<WIN>(
@@ -370,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int valid = max(0, min(pos.rows(p), held_to(p, g, token) - token));
           ok = __all_sync(0xffffffffu, mbar_wait(&kv_full[st], (sc / NST) & 1, wc));
           if (!ok) break;
-          if constexpr (WIN) {
+          if constexpr (WIN && !kLate) {
             const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
             // nothing to clear in most blocks: all rows hold tokens that some row sees
             if (valid < BN || tile_hides_some<BN>(p, g, kb, token, tile_low, last_end)) {
@@ -390,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               fence_proxy_async_smem();
               __syncwarp();
             }
-          } else if (valid < BN) {
+          } else if (!WIN && valid < BN) {
             const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
             for (int cb = 0; cb < DV / 64; ++cb)
               for (int i = valid * 8 + lane; i < BN * 8; i += 32)
@@ -470,25 +475,83 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
     } else if (warp == 2) {
       // ---------------------------------------------------------- PV issuer
-      if (lane == 0) {
+      auto output = [&](bool first) {  // of block `it`, in ring stage sc
+        const int st = sc % NST;
+        const uint32_t va = smem_u32(sKV) + st * S::kTileBytes;
+#pragma unroll
+        for (int s = 0; s < BN / 16; ++s)
+          umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + (it % NB) * BN + s * 8,
+                  sdesc(va + s * 2048, S::kCBox, 1024, kSw128), S::kIdescPV,
+                  (!first || s > 0) ? 1u : 0u);
+        if constexpr (MC == 1)
+          umma_commit(&kv_empty[st]);
+        else
+          umma_commit_mc(&kv_empty[st], kPair);
+        umma_commit(&pv_done[it % NB]);
+      };
+      if constexpr (kLate) {
+        // Before an output the warp clears the rows of c that no row of the tile sees (there
+        // are none in most blocks): what they score is masked, but they may hold NaN, and
+        // 0 * NaN would reach O. It finds them while the weights are computed. (It cannot wait
+        // for the copies alone: the stage's phase before may be a Q that it did not wait for.)
+        while (ok && walk.next(g)) {
+          sc += QST + own_qr(g);
+          const int a = g.st.len - g.st.n;
+          const int first_end = keys_seen<WIN>(p, a + p.by_heads(g.tile * TR), g.st);
+          const int last_end = keys_seen<WIN>(
+              p, a + p.by_heads(min(g.st.n * p.heads, (g.tile + 1) * TR) - 1), g.st);
+          const int tile_low = first_key(p, first_end, g.st.gone);
+          BlockPos<BN> pos(p, first_block(g));
+          for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, ++sc, next_block<BN>(p, g, kb - 1, pos)) {
+            const int token = pos.token(p);
+            const int valid = max(0, min(pos.rows(p), held_to(p, g, token) - token));
+            const bool some =
+                valid < BN || tile_hides_some<BN>(p, g, kb, token, tile_low, last_end);
+            unsigned hid[BN / 32] = {};
+            if (some)
+#pragma unroll
+              for (int q = 0; q < BN / 32; ++q) {
+                const int i = q * 32 + lane;
+                hid[q] = __ballot_sync(
+                    0xffffffffu,
+                    i >= valid || tile_hides(p, g, kb, token + i, first_end, last_end));
+              }
+            // the weights are there, so the block's copies and scores are done
+            ok = __all_sync(0xffffffffu, mbar_wait(&p_full[it % NB], phase(it), wc));
+            if (!ok) break;
+            if (some) {
+              uint8_t* kv = sKV + (sc % NST) * S::kTileBytes;
+              const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+              for (int q = 0; q < BN / 32; ++q)
+                if (hid[q])
+                  for (int cb = 0; cb < DV / 64; ++cb)
+                    for (int j = lane; j < 32 * 8; j += 32)
+                      if (hid[q] >> (j >> 3) & 1)
+                        *reinterpret_cast<uint4*>(kv + cb * S::kCBox + q * 32 * 128 + j * 16) =
+                            zero;
+              fence_proxy_async_smem();
+              __syncwarp();
+            }
+            if (lane == 0) {
+              tc_fence_after();
+              output(kb == g.kb0);
+            }
+            __syncwarp();
+          }
+        }
+        if (!ok && lane == 0) {
+          umma_commit(&mma_drain[1]);
+          mbar_wait_drain(&mma_drain[1], 0, p.status);
+        }
+      } else if (lane == 0) {
         while (ok && walk.next(g)) {
           sc += QST + own_qr(g);
           for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, ++sc) {
             ok = mbar_wait(&p_full[it % NB], phase(it), wc);
             if (!ok) break;
             tc_fence_after();
-            const int st = sc % NST;
-            const uint32_t va = smem_u32(sKV) + st * S::kTileBytes;
-#pragma unroll
-            for (int s = 0; s < BN / 16; ++s)
-              umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + (it % NB) * BN + s * 8,
-                      sdesc(va + s * 2048, S::kCBox, 1024, kSw128), S::kIdescPV,
-                      (kb > g.kb0 || s > 0) ? 1u : 0u);
-            if constexpr (MC == 1)
-              umma_commit(&kv_empty[st]);
-            else
-              umma_commit_mc(&kv_empty[st], kPair);
-            umma_commit(&pv_done[it % NB]);
+            output(kb == g.kb0);
           }
         }
         if (!ok) {
@@ -794,6 +857,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int k = 0; k < 8; ++k)
                 x[k] = pack_bf16x2(__uint_as_float(ov[16 * i + 2 * k]) * f,
                                    __uint_as_float(ov[16 * i + 2 * k + 1]) * f);
+              if (WIN && DC > 128 && p.o_wide) {
+                st_global_32(dst + c * 32 + i * 16, x);
+                continue;
+              }
               *reinterpret_cast<uint4*>(dst + c * 32 + i * 16) = make_uint4(x[0], x[1], x[2], x[3]);
               *reinterpret_cast<uint4*>(dst + c * 32 + i * 16 + 8) =
                   make_uint4(x[4], x[5], x[6], x[7]);
