@@ -122,10 +122,12 @@ __device__ __forceinline__ Stream<WIN> stream_at(const PagedK& p, int s) {
 }
 
 // Record lengths that the table cannot hold (and what else stream_held asks for, of
-// streams with new tokens); one block calls it.
+// streams with new tokens), and a q_start that does not ascend; `threads` threads of one block
+// call it, of which this is the i-th.
 template <bool WIN>
-__device__ __forceinline__ void check_streams(const PagedK& p) {
-  for (int s = threadIdx.x; s < p.seqs; s += blockDim.x) {
+__device__ __forceinline__ void check_streams(const PagedK& p, int i, int threads) {
+  check_q_start(p.q_start, p.seqs, p.total, p.status, i, threads);
+  for (int s = i; s < p.seqs; s += threads) {
     int n = 0, gone = 0;
     if constexpr (WIN) {
       n = p.q_start[s + 1] - p.q_start[s];
@@ -441,8 +443,9 @@ struct TeamWalk {
   int base, before;  // streams from base on, and the further tiles of those before
   long long next_more;
   bool more;
-  __device__ TeamWalk(const PagedK& k, int i, int n, bool further)
-      : p(k), id(i), teams(n), s(i), base(0), before(0), more(further) {
+  Stream<true> first;  // stream id, loaded while `more` is found out
+  __device__ TeamWalk(const PagedK& k, int i, int n, const Stream<true>& st, bool further)
+      : p(k), id(i), teams(n), s(i), base(0), before(0), more(further), first(st) {
     next_more = (i + n - k.seqs % n) % n;
   }
   __device__ int further_of(int stream) const {
@@ -459,7 +462,7 @@ struct TeamWalk {
   }
   __device__ bool next(Segment<true>& g) {
     while (s < p.seqs) {
-      const Stream<true> st = stream_at<true>(p, s);
+      const Stream<true> st = s == id ? first : stream_at<true>(p, s);
       s += teams;
       if (st.n > 0) return take(g, st, s - teams, 0);
     }

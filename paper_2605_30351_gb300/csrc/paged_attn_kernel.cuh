@@ -210,10 +210,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int first_row = S::kSplit == 1 ? crank * kBM : 0;  // of the pair's tile
   const int vpart = S::kSplit > 1 ? crank : 0;              // of c's columns
   const bool has_r = vpart == 0;  // the first of a split tile's CTAs adds q_r . k
-  if (blockIdx.x == 0) {
-    check_q_start(p.q_start, p.seqs, p.total, p.status);
-    check_streams<WIN>(p);
-  }
+  if (!WIN && blockIdx.x == 0) check_streams<WIN>(p, threadIdx.x, kThreads);
   if (threadIdx.x < 2) p.part_desc[2 * blockIdx.x + threadIdx.x] = make_int4(0, 0, 0, 0);
   const long long share =
       find_share<BN, TR, WIN>(p, blockIdx.x / CL, gridDim.x / CL, scratch, ends);
@@ -559,6 +556,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           mbar_wait_drain(&mma_drain[1], 0, p.status);
         }
       }
+      __syncwarp();
+    } else if (WIN && blockIdx.x == 0) {  // the warp without a role
+      check_streams<WIN>(p, lane, 32);
       __syncwarp();
     }
   } else {

@@ -27,15 +27,20 @@ __device__ __forceinline__ int stream_of(const int* q_start, int seqs, int t, in
   return lo;
 }
 
-// Record a q_start that does not ascend from 0 to total; one block calls it.
+// Record a q_start that does not ascend from 0 to total; one block calls it, or `threads` of
+// its threads, of which this is the i-th.
 __device__ __forceinline__ void check_q_start(const int* q_start, int seqs, int total,
-                                              int* status) {
-  for (int s = threadIdx.x; s <= seqs; s += blockDim.x) {
+                                              int* status, int i, int threads) {
+  for (int s = i; s <= seqs; s += threads) {
     const int v = q_start[s];
     const int next = s < seqs ? q_start[s + 1] : total;
     if (v > next || (s == 0 && v != 0) || (s == seqs && v != total))
       record_status(status, MLA_ERR_RANGE);
   }
+}
+__device__ __forceinline__ void check_q_start(const int* q_start, int seqs, int total,
+                                              int* status) {
+  check_q_start(q_start, seqs, total, status, threadIdx.x, blockDim.x);
 }
 
 }  // namespace vmla

@@ -46,7 +46,6 @@ constexpr int kDecodeThreads = 32 * kWarps;
 constexpr int kRows = 16;                     // rows of a tile
 constexpr int kBN = 16 * kWarps;              // keys of a block
 constexpr float kMoveLog2 = 8.0f;             // how far a maximum lags behind
-constexpr int kRedStride = 40;                // floats per row of a reduction tile (32 + pad)
 
 template <int DC, int DR, bool WIN, bool TEAM>
 struct DecodeShape {
@@ -58,10 +57,12 @@ struct DecodeShape {
   // Q's rows, with a window the sinks' q_r behind them
   static constexpr int kQStride = (WIN ? DK + DR : DK) * 2 + 16;  // bytes; rows in different banks
   static constexpr int kQBytes = kRows * kQStride;
-  // the warps' results, 32 columns at a time in two buffers; in a team one, beside what the
-  // team's CTAs send
-  static constexpr int kRedBufs = TEAM ? 1 : 2;
-  static constexpr int kRedBytes = kRedBufs * kWarps * kRows * kRedStride * 4;
+  // The warps' results at the end of a segment, floats per row: 32 columns at a time in two
+  // buffers, or in a team, whose calls are short, all at once in the place of the ring (one
+  // wait instead of six: one token of 38 streams 9.8 -> 9.3 us; but the decoding step of 64
+  // long streams 60.6 -> 62.3).
+  static constexpr int kRedStride = TEAM ? DC + 8 : 32 + 8;
+  static constexpr int kRedBytes = TEAM ? 0 : 2 * kWarps * kRows * kRedStride * 4;
   static constexpr int kTeamBytes = TEAM ? kRows * (DC * 4 + 8) : 0;
   static constexpr int kMlBytes = kWarps * kRows * 8;
   static constexpr int kRest = 1024 + kQBytes + kRedBytes + kMlBytes + kTeamBytes + 192;
@@ -70,6 +71,8 @@ struct DecodeShape {
   static constexpr int kSmemBytes = kRest + kTileBytes * kWarps * kStages;
   static constexpr bool kQRegs = DC <= 192;
   static_assert(kStages >= 2 && kQBytes % 16 == 0, "two stages must fit");
+  static_assert(!TEAM || kRows * kRedStride * 4 <= kTileBytes * kStages,
+                "the warps' results fit in the ring");
 };
 
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t addr) {
@@ -107,8 +110,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sKV = align_smem_1024(smem_raw);
   uint8_t* sQ = sKV + NST * kWarps * S::kTileBytes;
-  float* red = reinterpret_cast<float*>(sQ + S::kQBytes);  // [2][warps][16][kRedStride]
-  float2* warp_ml = reinterpret_cast<float2*>(red + S::kRedBufs * kWarps * kRows * kRedStride);
+  float* red = reinterpret_cast<float*>(TEAM ? sKV : sQ + S::kQBytes);  // [warps][16][kRedStride]
+  float2* warp_ml = reinterpret_cast<float2*>(sQ + S::kQBytes + S::kRedBytes);
   // of a team: [its CTAs][this one's rows] (maximum, sum), then the rows
   float2* team_ml = warp_ml + kWarps * kRows;
   float* team_o = reinterpret_cast<float*>(team_ml + (TEAM ? kRows : 0));
@@ -117,10 +120,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   grid_dep_sync();
-  if (blockIdx.x == 0) {
-    check_q_start(p.q_start, p.seqs, p.total, p.status);
-    check_streams<WIN>(p);
-  }
+  // one block looks at the metadata; of a team while its first keys are on their way
+  bool checked = blockIdx.x != 0;
+  auto check = [&]() {
+    if (!checked) check_streams<WIN>(p, threadIdx.x, kDecodeThreads);
+    checked = true;
+  };
+  if constexpr (!TEAM) check();
   // What a CTA computes: a share of all tiles' blocks, or as one of a team of CTAs (a
   // cluster), which takes whole streams in turn, its part of each of their tiles.
   const int team = TEAM ? static_cast<int>(cluster_nctarank()) : 1;
@@ -134,11 +140,12 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   Segment<WIN> g;
   auto walk = [&]() {
     if constexpr (TEAM) {
+      const int id = blockIdx.x / team;
+      const Stream<true> first = id < p.seqs ? stream_at<true>(p, id) : Stream<true>{};
       bool further = false;  // tiles that are not a stream's first
       for (int k = threadIdx.x; k < p.seqs; k += kDecodeThreads)
         further |= static_cast<long long>(p.q_start[k + 1] - p.q_start[k]) * p.heads > kRows;
-      return TeamWalk<kBN, kRows>(p, blockIdx.x / team, gridDim.x / team,
-                                  __syncthreads_or(further));
+      return TeamWalk<kBN, kRows>(p, id, gridDim.x / team, first, __syncthreads_or(further));
     } else {
       return Walk<kBN, kRows, WIN>(p, ends);
     }
@@ -278,6 +285,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     asm volatile("cp.async.commit_group;" ::: "memory");
 #pragma unroll 1
     for (int i = 0; i < NST - 1; ++i) fetch(i);
+    if constexpr (TEAM) check();
     asm volatile("cp.async.wait_group %0;" ::"n"(NST - 1) : "memory");
     __syncthreads();
     uint32_t q[S::kQRegs ? kSteps : 1][4];
@@ -457,36 +465,47 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         to_o = dsmem_addr(smem_u32(team_o + ((member * to_rows + out_r % to_rows) * DC + out_c)),
                           out_r / to_rows);
       }
-#pragma unroll
-    for (int c = 0; c < DC / 32; ++c) {  // 32 columns at a time
-      float* buf = red + (TEAM ? 0 : c & 1) * kWarps * kRows * kRedStride;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float* at = buf + (warp * kRows + ra) * kRedStride + 8 * i + cq;
-        const float(&v)[4] = o[4 * c + i];
-        *reinterpret_cast<float2*>(at) = make_float2(v[0] * f_a, v[1] * f_a);
-        *reinterpret_cast<float2*>(at + 8 * kRedStride) = make_float2(v[2] * f_b, v[3] * f_b);
-      }
-      __syncthreads();
+    // the warps' sum of the thread's row and two columns from 32 c on
+    auto put = [&](const float* buf, int c, int col) {
       float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float2 v =
-            *reinterpret_cast<const float2*>(buf + (w * kRows + out_r) * kRedStride + out_c);
+        const float2 v = *reinterpret_cast<const float2*>(
+            buf + (w * kRows + out_r) * S::kRedStride + col + out_c);
         sum.x += v.x;
         sum.y += v.y;
       }
-      if (out_r < n_rows) {
-        if (whole)
-          *reinterpret_cast<uint32_t*>(p.o + (grow + out_r) * DC + 32 * c + out_c) =
-              pack_bf16x2(sum.x, sum.y);
-        else if constexpr (TEAM)
-          dsmem_st_f32x2(to_o + 32 * c * 4, sum.x, sum.y);
-        else
-          *reinterpret_cast<float2*>(p.part_o + (static_cast<size_t>(slot) * kBM + out_r) * DC +
-                                     32 * c + out_c) = sum;
+      if (out_r >= n_rows) return;
+      if (whole)
+        *reinterpret_cast<uint32_t*>(p.o + (grow + out_r) * DC + 32 * c + out_c) =
+            pack_bf16x2(sum.x, sum.y);
+      else if constexpr (TEAM)
+        dsmem_st_f32x2(to_o + 32 * c * 4, sum.x, sum.y);
+      else
+        *reinterpret_cast<float2*>(p.part_o + (static_cast<size_t>(slot) * kBM + out_r) * DC +
+                                   32 * c + out_c) = sum;
+    };
+    auto lay = [&](float* buf, int i, int col) {  // this warp's columns 8 i .. 8 i + 7
+      float* at = buf + (warp * kRows + ra) * S::kRedStride + col + cq;
+      const float(&v)[4] = o[i];
+      *reinterpret_cast<float2*>(at) = make_float2(v[0] * f_a, v[1] * f_a);
+      *reinterpret_cast<float2*>(at + 8 * S::kRedStride) = make_float2(v[2] * f_b, v[3] * f_b);
+    };
+    if constexpr (TEAM) {  // the ring is free: every warp's loop has ended
+#pragma unroll
+      for (int i = 0; i < DC / 8; ++i) lay(red, i, 8 * i);
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < DC / 32; ++c) put(red, c, 32 * c);
+    } else {
+#pragma unroll
+      for (int c = 0; c < DC / 32; ++c) {
+        float* buf = red + (c & 1) * kWarps * kRows * S::kRedStride;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lay(buf, 4 * c + i, 8 * i);
+        __syncthreads();
+        put(buf, c, 0);
       }
-      if constexpr (TEAM) __syncthreads();  // the buffer is the next columns'
     }
     if (!whole && threadIdx.x < n_rows) {
       float2 t = total_of(threadIdx.x);
@@ -543,6 +562,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     __syncthreads();  // sQ, the sums and the buffers are the next segment's
   }
   if constexpr (TEAM) {
+    check();
     cluster_wait_acquire();
   } else {
     if (!any && threadIdx.x == 0)
