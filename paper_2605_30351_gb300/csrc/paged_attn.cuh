@@ -59,8 +59,15 @@ struct PagedK {
   Div by_heads, by_group, by_blocks, by_mask;  // by_mask: by `block`
   float scale_log2;
   int* status;
-  // a window that slides: tokens given back by stream (or none), the window, the sinks and
-  // the places of their whole pages; q_r of its own for the sinks
+};
+
+// The same with a window that slides (WIN, here and below).
+template <bool WIN>
+struct PagedP : PagedK {};
+template <>
+struct PagedP<true> : PagedK {
+  // tokens given back by stream (or none), the window, the sinks and the places of their whole
+  // pages; q_r of its own for the sinks
   const int* dropped;
   int window, sinks, front;
   bool turned;
@@ -91,7 +98,6 @@ constexpr int kPartHeld = 1, kPartEnds = 2, kPartEmpty = 4;
 // sum or value gets into the row whatever its weight.
 constexpr float kLowest = -3.402823466e38f;
 
-// WIN: the stream's window slides, here and below.
 template <bool WIN>
 struct Stream {
   int q0, n, len;
@@ -103,7 +109,7 @@ struct Stream<true> {
 };
 
 template <bool WIN>
-__device__ __forceinline__ bool stream_held(const PagedK& p, int n, int len, int gone) {
+__device__ __forceinline__ bool stream_held(const PagedP<WIN>& p, int n, int len, int gone) {
   if (len < 0 || len > static_cast<long long>(p.max_pages) * p.page_tokens) return false;
   if constexpr (WIN)  // indices below the limit, and new tokens behind the sinks' pages
     return gone >= 0 && static_cast<long long>(len) + gone < kMostTokens &&
@@ -112,7 +118,7 @@ __device__ __forceinline__ bool stream_held(const PagedK& p, int n, int len, int
 }
 
 template <bool WIN>
-__device__ __forceinline__ Stream<WIN> stream_at(const PagedK& p, int s) {
+__device__ __forceinline__ Stream<WIN> stream_at(const PagedP<WIN>& p, int s) {
   Stream<WIN> t{p.q_start[s], p.q_start[s + 1], p.lens[s]};
   if constexpr (WIN) t.gone = p.dropped ? p.dropped[s] : 0;
   const int q1 = t.n;
@@ -125,7 +131,7 @@ __device__ __forceinline__ Stream<WIN> stream_at(const PagedK& p, int s) {
 // streams with new tokens), and a q_start that does not ascend; `threads` threads of one block
 // call it, of which this is the i-th.
 template <bool WIN>
-__device__ __forceinline__ void check_streams(const PagedK& p, int i, int threads) {
+__device__ __forceinline__ void check_streams(const PagedP<WIN>& p, int i, int threads) {
   check_q_start(p.q_start, p.seqs, p.total, p.status, i, threads);
   for (int s = i; s < p.seqs; s += threads) {
     int n = 0, gone = 0;
@@ -140,7 +146,7 @@ __device__ __forceinline__ void check_streams(const PagedK& p, int i, int thread
 // Where the keys end that the token at place a (it may be negative) of a stream sees:
 // blocks of the mask count from the stream's start.
 template <bool WIN>
-__device__ __forceinline__ int keys_seen(const PagedK& p, int a, const Stream<WIN>& st) {
+__device__ __forceinline__ int keys_seen(const PagedP<WIN>& p, int a, const Stream<WIN>& st) {
   if (a < 0) return 0;
   if (p.block == 0) return st.len;
   const long long end = static_cast<long long>(p.by_mask(a + st.gone) + 1) * p.block - st.gone;
@@ -148,7 +154,7 @@ __device__ __forceinline__ int keys_seen(const PagedK& p, int a, const Stream<WI
 }
 
 // The first key behind the sinks that a token sees whose keys end there.
-__device__ __forceinline__ int first_key(const PagedK& p, int keys, int gone) {
+__device__ __forceinline__ int first_key(const PagedP<true>& p, int keys, int gone) {
   return max(gone > 0 ? p.front : p.sinks, keys - p.window);
 }
 
@@ -182,7 +188,7 @@ struct Span<true> {
 };
 
 template <int BN, int TR, bool WIN>
-__device__ __forceinline__ Span<WIN> tile_span(const PagedK& p, const Stream<WIN>& st, int tile) {
+__device__ __forceinline__ Span<WIN> tile_span(const PagedP<WIN>& p, const Stream<WIN>& st, int tile) {
   const int last = min(st.n * p.heads, (tile + 1) * TR) - 1;
   const int keys = keys_seen<WIN>(p, st.len - st.n + p.by_heads(last), st);
   if constexpr (!WIN) {
@@ -254,7 +260,7 @@ struct Cost<true> {
 };
 
 template <int BN, int TR, bool WIN>
-__device__ __forceinline__ Cost<WIN> cost_of(const PagedK& p, const Stream<WIN>& st) {
+__device__ __forceinline__ Cost<WIN> cost_of(const PagedP<WIN>& p, const Stream<WIN>& st) {
   Cost<WIN> c{};
   if (st.n == 0) return c;
   const int rows = st.n * p.heads;
@@ -308,7 +314,7 @@ struct Place {
 // 16 streams on 2,000 keys takes 13.9 us with 16 slots, 21 with 96, 115 with 1,024 and
 // 908 with 8,192. Returns the cost of a share.
 template <int BN, int TR, bool WIN>
-__device__ __forceinline__ long long find_share(const PagedK& p, int id, int groups,
+__device__ __forceinline__ long long find_share(const PagedP<WIN>& p, int id, int groups,
                                                 long long* scratch, Place<WIN>* out) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int e = warp / 3;  // which end; the other warps only wait
@@ -392,12 +398,12 @@ struct Segment {
 
 template <int BN, int TR, bool WIN>
 struct Walk {
-  const PagedK& p;
+  const PagedP<WIN>& p;
   Stream<WIN> st;
   int s, tile, off;
   Span<WIN> span;  // all < 0: not known yet
   int end_s, end_tile, end_off;
-  __device__ Walk(const PagedK& k, const Place<WIN>* ends) : p(k) {
+  __device__ Walk(const PagedP<WIN>& k, const Place<WIN>* ends) : p(k) {
     st = ends[0].st;  // the first segment needs no arithmetic: the search had it all
     s = ends[0].s;
     tile = ends[0].tile;
@@ -438,13 +444,13 @@ struct Walk {
 // team's CTAs walks them for itself; most calls have no such tiles, and `more` says so.
 template <int BN, int TR>
 struct TeamWalk {
-  const PagedK& p;
+  const PagedP<true>& p;
   int id, teams, s;
   int base, before;  // streams from base on, and the further tiles of those before
   long long next_more;
   bool more;
   Stream<true> first;  // stream id, loaded while `more` is found out
-  __device__ TeamWalk(const PagedK& k, int i, int n, const Stream<true>& st, bool further)
+  __device__ TeamWalk(const PagedP<true>& k, int i, int n, const Stream<true>& st, bool further)
       : p(k), id(i), teams(n), s(i), base(0), before(0), more(further), first(st) {
     next_more = (i + n - k.seqs % n) % n;
   }
@@ -514,7 +520,7 @@ __device__ __forceinline__ int first_block(const Segment<WIN>& g) {
 
 // From the tile's block kb to the next.
 template <int BN, bool WIN>
-__device__ __forceinline__ void next_block(const PagedK& p, const Segment<WIN>& g, int kb,
+__device__ __forceinline__ void next_block(const PagedP<WIN>& p, const Segment<WIN>& g, int kb,
                                            BlockPos<BN>& pos) {
   if (WIN && kb + 1 == g.at.sb)
     pos = BlockPos<BN>(p, g.at.wb);
@@ -524,13 +530,16 @@ __device__ __forceinline__ void next_block(const PagedK& p, const Segment<WIN>& 
 
 // Page of a tile's count of them in the stream's list.
 template <bool WIN>
-__device__ __forceinline__ int page_index(const PagedK& p, const Span<WIN>& at, int page) {
-  return WIN && page >= at.cut >> p.page_log ? page + (at.shift >> p.page_log) : page;
+__device__ __forceinline__ int page_index(const PagedP<WIN>& p, const Span<WIN>& at, int page) {
+  if constexpr (WIN)
+    return page >= at.cut >> p.page_log ? page + (at.shift >> p.page_log) : page;
+  else
+    return page;
 }
 
 // Where the tokens end that are there, as the tile counts them, in the block at `token`.
 template <bool WIN>
-__device__ __forceinline__ int held_to(const PagedK& p, const Segment<WIN>& g, int token) {
+__device__ __forceinline__ int held_to(const PagedP<WIN>& p, const Segment<WIN>& g, int token) {
   if constexpr (WIN)
     if (token < g.at.cut && g.at.cut > p.front) return min(p.front, g.st.len);
   return g.st.len - g.at.shift;
@@ -543,7 +552,7 @@ struct View {
 };
 
 // Of a row whose keys end at `keys` and begin behind the sinks at `low`.
-__device__ __forceinline__ View view_of(const PagedK& p, const Segment<true>& g, int kb, int token,
+__device__ __forceinline__ View view_of(const PagedP<true>& p, const Segment<true>& g, int kb, int token,
                                         int keys, int low) {
   View v{0, low - g.at.shift - token, keys - g.at.shift - token};
   if (kb < g.at.sb) {
@@ -556,7 +565,7 @@ __device__ __forceinline__ View view_of(const PagedK& p, const Segment<true>& g,
 
 // Whether the token u of the tile's count, in its block kb, is there as one of the sinks'
 // pages, which their own queries score.
-__device__ __forceinline__ bool among_sinks(const PagedK& p, const Segment<true>& g, int kb,
+__device__ __forceinline__ bool among_sinks(const PagedP<true>& p, const Segment<true>& g, int kb,
                                             int u) {
   return p.compact ? u < g.at.cut : kb < g.at.sb;
 }
@@ -565,7 +574,7 @@ __device__ __forceinline__ bool among_sinks(const PagedK& p, const Segment<true>
 // first_end and whose last row's at last_end: such a key may be NaN, and must not be
 // multiplied by weights of 0. (Where a window is shorter than a block of the mask, keys
 // before each block's window are hidden too.)
-__device__ __forceinline__ bool tile_hides(const PagedK& p, const Segment<true>& g, int kb, int u,
+__device__ __forceinline__ bool tile_hides(const PagedP<true>& p, const Segment<true>& g, int kb, int u,
                                            int first_end, int last_end) {
   const bool sink = among_sinks(p, g, kb, u);
   const int j = sink ? u : u + g.at.shift;
@@ -583,18 +592,19 @@ __device__ __forceinline__ bool tile_hides(const PagedK& p, const Segment<true>&
 
 // Whether it may hide one of the block's.
 template <int BN>
-__device__ __forceinline__ bool tile_hides_some(const PagedK& p, const Segment<true>& g, int kb,
+__device__ __forceinline__ bool tile_hides_some(const PagedP<true>& p, const Segment<true>& g, int kb,
                                                 int token, int tile_low, int last_end) {
   return token + BN > last_end - g.at.shift || p.block > p.window ||
          (kb < g.at.sb ? token + BN > p.sinks : token < tile_low - g.at.shift);
 }
 
 // Host side: the kernels' parameters for key blocks of bn tokens.
-inline PagedK paged_params(const PagedAttnArgs& a, int bn, int dv) {
+template <bool WIN>
+PagedP<WIN> paged_params(const PagedAttnArgs& a, int bn, int dv) {
   const bool divides = bn % a.page_tokens == 0;
   const PartLayout at(dv);
   char* ws = PartLayout::base(a.workspace);
-  PagedK k;
+  PagedP<WIN> k;
   k.q_start = a.q_start;
   k.table = a.table;
   k.lens = a.lens;
@@ -619,17 +629,19 @@ inline PagedK paged_params(const PagedAttnArgs& a, int bn, int dv) {
   k.by_mask = div_by(k.block > 0 ? k.block : 1);
   k.scale_log2 = a.scale_log2;
   k.status = a.status;
-  k.dropped = a.dropped;
-  k.window = a.window;
-  k.sinks = a.sinks;
-  const long long front =
-      (static_cast<long long>(a.sinks) + a.page_tokens - 1) / a.page_tokens * a.page_tokens;
-  k.front = static_cast<int>(front < kMostTokens ? front : kMostTokens);
-  k.turned = a.q_sink != nullptr && a.sinks > 0;
-  k.compact = divides;
-  k.o_wide = aligned_to(a.o, 32);
-  k.page_log = 0;
-  while (divides && (1 << k.page_log) < a.page_tokens) ++k.page_log;
+  if constexpr (WIN) {
+    k.dropped = a.dropped;
+    k.window = a.window;
+    k.sinks = a.sinks;
+    const long long front =
+        (static_cast<long long>(a.sinks) + a.page_tokens - 1) / a.page_tokens * a.page_tokens;
+    k.front = static_cast<int>(front < kMostTokens ? front : kMostTokens);
+    k.turned = a.q_sink != nullptr && a.sinks > 0;
+    k.compact = divides;
+    k.o_wide = aligned_to(a.o, 32);
+    k.page_log = 0;
+    while (divides && (1 << k.page_log) < a.page_tokens) ++k.page_log;
+  }
   return k;
 }
 

@@ -60,6 +60,8 @@
 // copies and join.
 #pragma once
 
+#include <type_traits>
+
 #include "internal.h"
 #include "paged_attn.cuh"
 #include "ptx_sm103.cuh"
@@ -129,13 +131,18 @@ struct PagedShape {
                 "swizzle-atom alignment");
 };
 
+// The map of the sinks' own q_r, where there may be one.
+struct NoMap {};
+template <bool WIN>
+using SinkMap = std::conditional_t<WIN, CUtensorMap, NoMap>;
+
 template <int DC, int DR, int CL, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_attn_kernel(const __grid_constant__ CUtensorMap tm_c,
                       const __grid_constant__ CUtensorMap tm_kr,
                       const __grid_constant__ CUtensorMap tm_qc,
                       const __grid_constant__ CUtensorMap tm_qr,
-                      const __grid_constant__ CUtensorMap tm_qs, const PagedK p) {
+                      const __grid_constant__ SinkMap<WIN> tm_qs, const PagedP<WIN> p) {
   using S = PagedShape<DC, DR, WIN>;
   constexpr int BN = S::BN, DV = S::DV, NST = S::kStages, QST = S::kQStages, NB = S::kBufs;
   constexpr int TR = kBM * CL / S::kSplit;  // rows of a CTA's, or a pair's, tile
@@ -193,7 +200,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     tma_prefetch_desc(&tm_kr);
     tma_prefetch_desc(&tm_qc);
     tma_prefetch_desc(&tm_qr);
-    if (WIN && p.turned) tma_prefetch_desc(&tm_qs);
+    if constexpr (WIN)
+      if (p.turned) tma_prefetch_desc(&tm_qs);
   }
   if (warp == 1) {
     tmem_alloc(tmem_slot, S::kTmemCols);
@@ -221,7 +229,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto phase = [](int block) { return static_cast<uint32_t>(block / NB) & 1u; };
   int sc = 0;  // ring stages so far, Q's included: the phases of kv_full, kv_empty
   // a segment with blocks of the sinks has a stage more in front: their own q_r
-  auto own_qr = [&](const Segment<WIN>& sg) { return WIN && p.turned && sg.kb0 < sg.at.sb ? 1 : 0; };
+  auto own_qr = [&](const Segment<WIN>& sg) {
+    if constexpr (WIN) return p.turned && sg.kb0 < sg.at.sb ? 1 : 0;
+    return 0;
+  };
 
   if (warp < 4) {
     if (warp == 0) {
@@ -275,23 +286,25 @@ __global__ void __launch_bounds__(kThreads, 1)
               tma_load_2d(st + S::kKrOff + i * 32 * S::kKrRow, &tm_qr, full, 0, r);
           }
         }
-        if (ok && own_qr(g)) {
-          ok = acquire();
-          if (ok) {
-            const int r0 = g.tile * TR + first_row;
-            const int boxes = has_r ? max(0, min(kBM / 32, (rows - r0 + 31) / 32)) : 0;
-            uint64_t* full = &kv_full[sc % NST];
-            if (lane == 0) {
-              if (boxes)
-                mbar_arrive_expect_tx(full, boxes * 32 * DR * 2);
-              else
-                mbar_arrive(full);
+        if constexpr (WIN) {
+          if (ok && own_qr(g)) {
+            ok = acquire();
+            if (ok) {
+              const int r0 = g.tile * TR + first_row;
+              const int boxes = has_r ? max(0, min(kBM / 32, (rows - r0 + 31) / 32)) : 0;
+              uint64_t* full = &kv_full[sc % NST];
+              if (lane == 0) {
+                if (boxes)
+                  mbar_arrive_expect_tx(full, boxes * 32 * DR * 2);
+                else
+                  mbar_arrive(full);
+              }
+              __syncwarp();
+              if (lane < boxes)
+                tma_load_2d(sKV + (sc % NST) * S::kTileBytes + lane * 32 * S::kKrRow, &tm_qs, full, 0,
+                            g.st.q0 * p.heads + r0 + 32 * lane);
+              ++sc;
             }
-            __syncwarp();
-            if (lane < boxes)
-              tma_load_2d(sKV + (sc % NST) * S::kTileBytes + lane * 32 * S::kKrRow, &tm_qs, full, 0,
-                          g.st.q0 * p.heads + r0 + 32 * lane);
-            ++sc;
           }
         }
         if (!ok) break;
@@ -472,20 +485,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
     } else if (warp == 2) {
       // ---------------------------------------------------------- PV issuer
-      auto output = [&](bool first) {  // of block `it`, in ring stage sc
-        const int st = sc % NST;
-        const uint32_t va = smem_u32(sKV) + st * S::kTileBytes;
-#pragma unroll
-        for (int s = 0; s < BN / 16; ++s)
-          umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + (it % NB) * BN + s * 8,
-                  sdesc(va + s * 2048, S::kCBox, 1024, kSw128), S::kIdescPV,
-                  (!first || s > 0) ? 1u : 0u);
-        if constexpr (MC == 1)
-          umma_commit(&kv_empty[st]);
-        else
-          umma_commit_mc(&kv_empty[st], kPair);
-        umma_commit(&pv_done[it % NB]);
-      };
       if constexpr (kLate) {
         // Before an output the warp clears the rows of c that no row of the tile sees (there
         // are none in most blocks): what they score is masked, but they may hold NaN, and
@@ -532,7 +531,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (lane == 0) {
               tc_fence_after();
-              output(kb == g.kb0);
+              const int st = sc % NST;
+              const uint32_t va = smem_u32(sKV) + st * S::kTileBytes;
+#pragma unroll
+              for (int s = 0; s < BN / 16; ++s)
+                umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + (it % NB) * BN + s * 8,
+                        sdesc(va + s * 2048, S::kCBox, 1024, kSw128), S::kIdescPV,
+                        (kb > g.kb0 || s > 0) ? 1u : 0u);
+              umma_commit_mc(&kv_empty[st], kPair);
+              umma_commit(&pv_done[it % NB]);
             }
             __syncwarp();
           }
@@ -548,7 +555,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             ok = mbar_wait(&p_full[it % NB], phase(it), wc);
             if (!ok) break;
             tc_fence_after();
-            output(kb == g.kb0);
+            const int st = sc % NST;
+            const uint32_t va = smem_u32(sKV) + st * S::kTileBytes;
+#pragma unroll
+            for (int s = 0; s < BN / 16; ++s)
+              umma_ts(tmem + S::kTmemO, tmem + S::kTmemP + (it % NB) * BN + s * 8,
+                      sdesc(va + s * 2048, S::kCBox, 1024, kSw128), S::kIdescPV,
+                      (kb > g.kb0 || s > 0) ? 1u : 0u);
+            if constexpr (MC == 1)
+              umma_commit(&kv_empty[st]);
+            else
+              umma_commit_mc(&kv_empty[st], kPair);
+            umma_commit(&pv_done[it % NB]);
           }
         }
         if (!ok) {
@@ -857,10 +875,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int k = 0; k < 8; ++k)
                 x[k] = pack_bf16x2(__uint_as_float(ov[16 * i + 2 * k]) * f,
                                    __uint_as_float(ov[16 * i + 2 * k + 1]) * f);
-              if (WIN && DC > 128 && p.o_wide) {
-                st_global_32(dst + c * 32 + i * 16, x);
-                continue;
-              }
+              if constexpr (WIN && DC > 128)
+                if (p.o_wide) {
+                  st_global_32(dst + c * 32 + i * 16, x);
+                  continue;
+                }
               *reinterpret_cast<uint4*>(dst + c * 32 + i * 16) = make_uint4(x[0], x[1], x[2], x[3]);
               *reinterpret_cast<uint4*>(dst + c * 32 + i * 16 + 8) =
                   make_uint4(x[4], x[5], x[6], x[7]);
@@ -899,7 +918,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 template <int DC, int DR, int CL, bool WIN>
 int launch_paged(const PagedAttnArgs& a) {
   using S = PagedShape<DC, DR, WIN>;
-  const PagedK k = paged_params(a, S::BN, S::DV);
+  const PagedP<WIN> k = paged_params<WIN>(a, S::BN, S::DV);
   CUtensorMap tm_c, tm_kr;
   const unsigned long long rows = static_cast<unsigned long long>(a.pages) * a.page_tokens;
   if (!encode_map_2d_bf16(&tm_c, a.c, DC, rows, DC * 2ull, 64, k.box_rows,
@@ -907,18 +926,22 @@ int launch_paged(const PagedAttnArgs& a) {
       !encode_map_2d_bf16(&tm_kr, a.kr, DR, rows, DR * 2ull, DR, k.box_rows,
                           DR == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
     return MLA_ERR_CUDA;
-  CUtensorMap tm_qc, tm_qr, tm_qs;  // boxes of 32 rows: short tiles fetch what they have
+  SinkMap<WIN> tm_qs{};
+  CUtensorMap tm_qc, tm_qr;  // boxes of 32 rows: short tiles fetch what they have
   const unsigned long long q_rows = static_cast<unsigned long long>(a.total) * a.heads;
   if (!encode_map_2d_bf16(&tm_qc, a.q_c, DC, q_rows, DC * 2ull, 64, 32,
                           CU_TENSOR_MAP_SWIZZLE_128B) ||
       !encode_map_2d_bf16(&tm_qr, a.q_r, DR, q_rows, DR * 2ull, DR, 32,
                           DR == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
     return MLA_ERR_CUDA;
-  if (!WIN || !k.turned)
-    tm_qs = tm_qr;
-  else if (!encode_map_2d_bf16(&tm_qs, a.q_sink, DR, q_rows, DR * 2ull, DR, 32,
-                               DR == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
-    return MLA_ERR_CUDA;
+  if constexpr (WIN) {
+    if (!k.turned)
+      tm_qs = tm_qr;
+    else if (!encode_map_2d_bf16(
+                 &tm_qs, a.q_sink, DR, q_rows, DR * 2ull, DR, 32,
+                 DR == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
+      return MLA_ERR_CUDA;
+  }
   auto kern = paged_attn_kernel<DC, DR, CL, WIN>;
   // resident CTAs of this instance (one per SM, whole clusters), asked once
   static PerDevice known;

@@ -104,7 +104,7 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes)
 template <int DC, int DR, bool WIN, bool TEAM>
 __global__ void __launch_bounds__(kDecodeThreads, 1)
     paged_decode_kernel(const uint8_t* c, const uint8_t* kr, const __nv_bfloat16* q_c,
-                        const __nv_bfloat16* q_r, const __nv_bfloat16* q_sink, const PagedK p) {
+                        const __nv_bfloat16* q_r, const __nv_bfloat16* q_sink, const PagedP<WIN> p) {
   using S = DecodeShape<DC, DR, WIN, TEAM>;
   constexpr int NST = S::kStages, kSteps = S::DK / 16;
   extern __shared__ uint8_t smem_raw[];
@@ -177,7 +177,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     const int rows = g.st.n * p.heads, row0 = g.tile * kRows;
     const int n_rows = min(kRows, rows - row0);
     const size_t grow = static_cast<size_t>(g.st.q0) * p.heads + row0;
-    const bool own_qr = WIN && p.turned && g.kb0 < g.at.sb;  // the sinks' queries are needed
+    bool own_qr = false;  // the sinks' queries are needed
+    if constexpr (WIN) own_qr = p.turned && g.kb0 < g.at.sb;
     auto keys_of = [&](int r) {
       return r < n_rows
                  ? keys_seen<WIN>(p, g.st.len - g.st.n + p.by_heads(row0 + r), g.st)
@@ -573,7 +574,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 template <int DC, int DR, bool WIN>
 int launch_decode(const PagedAttnArgs& a) {
   using S = DecodeShape<DC, DR, WIN, false>;
-  const PagedK k = paged_params(a, kBN, DC);
+  const PagedP<WIN> k = paged_params<WIN>(a, kBN, DC);
   auto kern = paged_decode_kernel<DC, DR, WIN, false>;
   static PerDevice known;  // one CTA per SM, asked once
   std::atomic<int>* cell = known.cell();
@@ -646,7 +647,7 @@ int team_slots(int team) {
 template <int DC, int DR>
 int launch_teams(const PagedAttnArgs& a, int team, int teams) {
   using S = DecodeShape<DC, DR, true, true>;
-  const PagedK k = paged_params(a, kBN, DC);
+  const PagedP<true> k = paged_params<true>(a, kBN, DC);
   auto kern = paged_decode_kernel<DC, DR, true, true>;
   static PerDevice known;  // the kernel's shared memory, set once
   std::atomic<int>* cell = known.cell();
