@@ -447,9 +447,9 @@ int mla_rope_apply(const mla_rope* rope, const void* x, const int* pos, void* y,
  * Sizes: page_tokens >= 8; d_c and d_r multiples of 8; at most 65,536 streams;
  * pages * page_tokens and max_pages * page_tokens below 2^31 - 2^16; all buffers
  * start on 16-byte boundaries.
- * A stream keeps its tokens from the first one on: lengths change at the end only, so
- * a window that slides (the ring above) has no counterpart here, and a stream holds at
- * most max_pages * page_tokens tokens.
+ * A stream holds at most max_pages * page_tokens tokens. mla_pages_resize changes its
+ * length at the end only; the pages between its first tokens and a window of its newest
+ * ones leave it by mla_pages_slide (below).
  * What costs time: attention is fastest with 8, 16, 32, 64 or 128 tokens a page (others
  * take a whole key block, 128 or at d_c = 512 64 keys, for what is left of a page), and
  * every call looks at all seqs slots, idle ones too, so a pool should have about as
@@ -586,7 +586,8 @@ int mla_paged_attention(const mla_paged_cache* cache, int layer, const void* q_c
  * never given back. The token at place p of the held ones has the index p in its stream
  * if p lies in the sinks' pages, else p + dropped. Indices stay below 2^31 - 2^16.
  * A stream keeps its numbers in every call: window may change, sinks not once tokens were
- * given back.
+ * given back. dropped has to be 0 where a stream starts (mla_paged_window_plan sees to it).
+ * mla_paged_attention sees all tokens that are held, and counts its blocks in places.
  */
 typedef struct mla_paged_window {
   int window;
@@ -600,7 +601,8 @@ typedef struct mla_paged_window {
  *     new_lens[s] = lens[s] + n_new[s], or -1 where n_new[s] = 0          int32 [seqs]
  * which mla_pages_resize takes next. A stream that holds no token starts anew: its
  * dropped becomes 0. A negative count is recorded as MLA_ERR_RANGE and counts as 0;
- * sums past 2^31 - 1 are recorded and stay there.
+ * sums past 2^31 - 1 are recorded and stay there. The arrays, lens among them, must not
+ * overlap (MLA_ERR_ARG).
  */
 int mla_paged_window_plan(const mla_paged_cache* cache, const mla_paged_window* window,
                           const int* n_new, int* q_start, int* new_lens, void* stream);
@@ -619,7 +621,7 @@ int mla_paged_window_plan(const mla_paged_cache* cache, const mla_paged_window* 
  * T and frame_width are at least 1, frame_width at most T. A token without a page has the
  * row -1 (MLA_ERR_RANGE); tokens that are no stream's (a q_start that does not ascend
  * from 0 to total, recorded too) are not written. A token at a negative place has the
- * coordinates 0. total = 0 is MLA_OK.
+ * coordinates 0. The arrays must not overlap (MLA_ERR_ARG). total = 0 is MLA_OK.
  */
 int mla_paged_window_positions(const mla_paged_cache* cache, const mla_paged_window* window,
                                const int* q_start, int total, int causal_block,

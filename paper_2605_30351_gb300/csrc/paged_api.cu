@@ -1,6 +1,7 @@
 // C ABI of the paged latent cache: argument checks and dispatch. See
 // include/videomla.h.
 #include <cmath>
+#include <utility>
 
 #include "internal.h"
 #include "ptx_sm103.cuh"
@@ -46,6 +47,16 @@ int check_window(const mla_paged_window* w, bool dropped) {
       !aligned_to(w->dropped, 4))
     return MLA_ERR_ARG;
   return MLA_OK;
+}
+
+// Whether two of the arrays (address, ints) share memory.
+bool overlap(std::initializer_list<std::pair<const int*, long long>> arrays) {
+  for (const auto& a : arrays)
+    for (const auto& b : arrays)
+      if (&a < &b && a.first && b.first && a.first < b.first + b.second &&
+          b.first < a.first + a.second)
+        return true;
+  return false;
 }
 
 // What both attention calls check, and the arguments without the window's.
@@ -241,6 +252,12 @@ int mla_paged_window_plan(const mla_paged_cache* cache, const mla_paged_window* 
   // the metadata calls look up the addresses that they use only: a lookup is a noticeable
   // part of so short a call
   if (rc == MLA_OK) rc = check_buffers(cache, false);
+  if (rc == MLA_OK && overlap({{n_new, cache->seqs},
+                               {q_start, cache->seqs + 1ll},
+                               {new_lens, cache->seqs},
+                               {cache->lens, cache->seqs},
+                               {window->dropped, cache->seqs}}))
+    rc = MLA_ERR_ARG;
   if (rc == MLA_OK)
     rc = check_resident({cache->lens, n_new, q_start, new_lens, window->dropped});
   if (rc != MLA_OK) return rc;
@@ -265,6 +282,14 @@ int mla_paged_window_positions(const mla_paged_cache* cache, const mla_paged_win
       !aligned_to(pos_sink, 4) || !aligned_to(rows, 4))
     return MLA_ERR_ARG;
   rc = check_buffers(cache, false);
+  const long long n = static_cast<long long>(total) * axes;
+  if (rc == MLA_OK && overlap({{q_start, cache->seqs + 1ll},
+                               {pos, n},
+                               {pos_sink, n},
+                               {rows, total},
+                               {cache->lens, cache->seqs},
+                               {window->dropped, cache->seqs}}))
+    rc = MLA_ERR_ARG;
   if (rc == MLA_OK)
     rc = check_resident(
         {cache->table, cache->lens, q_start, pos, pos_sink, rows, window->dropped});

@@ -624,6 +624,9 @@ class PagedWindow:
 
     def __init__(self, window, sinks=0, dropped=None):
         self.window, self.sinks, self.dropped = int(window), int(sinks), dropped
+        for v in (self.window, self.sinks):
+            if not -2 ** 31 <= v < 2 ** 31:
+                raise ValueError(f"window and sinks are 32-bit numbers, got {v}")
         self.seqs = None if dropped is None else dropped.shape[0]
         self.struct = mla_paged_window(
             window=self.window, sinks=self.sinks,

@@ -7,6 +7,9 @@ of the scores here, move a weight by less than 2^-10. So
 |o - ref| <= (2 * 2^-8 + 2^-10) * sum_j p_j |c_j|."""
 
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -438,3 +441,46 @@ def test_refusals():
         call(window=w)
     torch.cuda.synchronize()
     assert V.mla_device_status(clear=True) == V.MLA_OK
+
+
+def test_two_streams_at_once():
+    """Calls that overlap on the GPU, a workspace each."""
+    ps = [Problem([3000, 40, 700], [1, 1, 1], 2000, 20, heads=12, d_c=192, page=64, dirty=False, seed=1),
+          Problem([900, 140], [60, 70], 300, 20, heads=12, d_c=192, page=64, dirty=False, seed=2),
+          Problem([4100 - 9 * s for s in range(20)], [1] * 20, 4000, 20, heads=12, page=64, dirty=False, seed=3)]
+    streams = [torch.cuda.Stream() for _ in ps]
+    outs = [torch.full_like(p.q_c, float("nan")) for p in ps]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for p, o, s in zip(ps, outs, streams):
+            p.call(o, s)
+    torch.cuda.synchronize()
+    for p, o in zip(ps, outs):
+        p.check(o, 5)
+        assert torch.equal(o, p.run())
+
+
+FIRST = """
+import sys
+sys.path[:0] = [{root!r}, {here!r}]
+import torch
+import test_gpu_paged_window as T
+for lens, new, window in (([300], [1], 100), ([4100] * 20, [1] * 20, 4000), ([300, 90], [40, 30], 100)):
+    p = T.Problem(lens, new, window, 20, heads=12, d_c=192, page=64, dirty=False)
+    o, graph = torch.full_like(p.q_c, float("nan")), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.call(o)
+    graph.replay()
+    torch.cuda.synchronize()
+    p.check(o, 4)
+assert T.V.mla_device_status(clear=True) == T.V.MLA_OK
+print("first calls ok")
+"""
+
+
+def test_first_calls_inside_a_capture():
+    """A process whose first call of every form is captured."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    code = FIRST.format(root=os.path.dirname(here), here=here)
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "first calls ok" in r.stdout, r.stdout + r.stderr

@@ -27,16 +27,17 @@ ARGS = {
     "mla_paged_window_attention": dict(
         layer=0, q_c=FAKE, q_r=FAKE, q_r_sink=FAKE, total=4, heads=12, q_start=FAKE, head_dim=128,
         block=1, workspace=FAKE, nbytes=1 << 30, o=FAKE, stream=None),
-    "mla_paged_window_plan": dict(n_new=FAKE, q_start=FAKE, new_lens=FAKE, stream=None),
+    "mla_paged_window_plan": dict(n_new=FAKE + (1 << 16), q_start=FAKE + (2 << 16),
+                                  new_lens=FAKE + (3 << 16), stream=None),
     "mla_paged_window_positions": dict(
-        q_start=FAKE, total=4, block=1, frame=64, width=8, axes=3, pos=FAKE, pos_sink=FAKE,
-        rows=FAKE, stream=None),
+        q_start=FAKE + (1 << 16), total=4, block=1, frame=64, width=8, axes=3, pos=FAKE + (2 << 16),
+        pos_sink=FAKE + (3 << 16), rows=FAKE + (4 << 16), stream=None),
     "mla_pages_slide": dict(keep=FAKE, stream=None),
     "mla_pages_window_fork": dict(src=FAKE, dst=FAKE, n=1, stream=None),
 }
 
 
-def call(name, cache=None, window=5, sinks=1, dropped=FAKE, null=False, **kw):
+def call(name, cache=None, window=5, sinks=1, dropped=FAKE + (9 << 16), null=False, **kw):
     a = dict(ARGS[name])
     assert set(kw) <= set(a)
     a.update(kw)
@@ -77,6 +78,27 @@ def test_calls_that_write_it_need_dropped():
 ])
 def test_arguments_are_checked(name, bad):
     assert call(name, **bad) == V.MLA_ERR_ARG
+
+
+def test_arrays_that_overlap_are_refused():
+    """seqs = 3: n_new, new_lens, lens and dropped take 12 bytes, q_start 16."""
+    at = ARGS["mla_paged_window_plan"]
+    for bad in (dict(n_new=at["q_start"] + 12), dict(new_lens=at["n_new"] + 8),
+                dict(q_start=at["new_lens"] - 12), dict(new_lens=FAKE), dict(q_start=FAKE + (9 << 16) + 8),
+                dict(q_start=FAKE + 8)):
+        assert call("mla_paged_window_plan", **bad) == V.MLA_ERR_ARG, bad
+    at = ARGS["mla_paged_window_positions"]
+    for bad in (dict(pos=at["pos_sink"] + 44), dict(pos_sink=at["rows"] - 44), dict(rows=at["q_start"] + 12),
+                dict(pos=FAKE), dict(rows=FAKE + (9 << 16))):
+        assert call("mla_paged_window_positions", **bad) == V.MLA_ERR_ARG, bad
+
+
+def test_windows_past_32_bits_are_refused():
+    for bad in ((1 << 32) + 5, 1 << 31):
+        with pytest.raises(ValueError):
+            V.PagedWindow(bad)
+        with pytest.raises(ValueError):
+            V.PagedWindow(5, bad)
 
 
 def test_a_workspace_one_byte_short_is_refused():
