@@ -551,6 +551,11 @@ struct View {
   int sinks, low, valid;
 };
 
+// The lowest n bits of 32.
+__device__ __forceinline__ unsigned low_bits(int n) {
+  return n > 0 ? 0xffffffffu >> (32 - min(n, 32)) : 0u;
+}
+
 // Of a row whose keys end at `keys` and begin behind the sinks at `low`.
 __device__ __forceinline__ View view_of(const PagedP<true>& p, const Segment<true>& g, int kb, int token,
                                         int keys, int low) {

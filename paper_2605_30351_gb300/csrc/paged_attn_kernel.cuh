@@ -684,6 +684,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       float m_run = -INFINITY, l_run = 0.f;
       BlockPos<BN> pos(p, first_block(g));
       for (int kb = g.kb0; kb < g.kb1; ++kb, ++it, next_block<BN>(p, g, kb - 1, pos)) {
+        View v{0, 0, 0};
+        if constexpr (WIN) v = view_of(p, g, kb, pos.token(p), w.keys, w.low);
         if (!mbar_wait(&s_full[it % NB], phase(it), wc)) {
           ok = false;
           break;
@@ -746,16 +748,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         int valid = min(pos.rows(p), w.keys - pos.token(p));
         bool sees = true;  // WIN: the row sees one of the block's keys
         if constexpr (WIN) {
-          const View v = view_of(p, g, kb, pos.token(p), w.keys, w.low);
           valid = min(pos.rows(p), v.valid);
           sees = v.sinks > 0 || max(v.low, 0) < valid;
-          if (v.low > 0 && v.sinks < BN) {
+          // Hidden keys 32 at a time, by a bit each: most blocks have none, those at a window's
+          // ends have them in a run or two.
+          if (v.low > 0 || valid < BN) {
 #pragma unroll
-            for (int c = 0; c < BN; ++c)
-              if (c < v.low && c >= v.sinks) sv[c] = -INFINITY;
+            for (int q = 0; q < BN / 32; ++q) {
+              const int lo = v.low - 32 * q, hi = valid - 32 * q;
+              {
+                const unsigned shown =
+                    low_bits(hi) & (~low_bits(lo) | low_bits(v.sinks - 32 * q));
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (!(shown >> i & 1)) sv[32 * q + i] = -INFINITY;
+              }
+            }
           }
-        }
-        if (valid < BN) {
+        } else if (valid < BN) {
 #pragma unroll
           for (int c = 0; c < BN; ++c)
             if (c >= valid) sv[c] = -INFINITY;
