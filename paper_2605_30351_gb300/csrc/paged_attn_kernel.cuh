@@ -750,19 +750,30 @@ __global__ void __launch_bounds__(kThreads, 1)
         if constexpr (WIN) {
           valid = min(pos.rows(p), v.valid);
           sees = v.sinks > 0 || max(v.low, 0) < valid;
-          // Hidden keys 32 at a time, by a bit each: most blocks have none, those at a window's
-          // ends have them in a run or two.
-          if (v.low > 0 || valid < BN) {
+          // Most blocks hide no keys, those at a window's ends a run or two. 32 keys at a time
+          // by a bit each that is 2 - 15 % faster where windows are short (3,167 tokens, windows
+          // of 281 keys, d_c = 128: 197 -> 169 us); compared key by key, at d_c = 192 the loop
+          // over blocks that hide none is faster (four chunks 1,075 -> 1,035 us) for 1 - 4 %
+          // where windows are short.
+          if constexpr (DC == 192) {
+            if (v.low > 0 && v.sinks < BN) {
+#pragma unroll
+              for (int c = 0; c < BN; ++c)
+                if (c < v.low && c >= v.sinks) sv[c] = -INFINITY;
+            }
+            if (valid < BN) {
+#pragma unroll
+              for (int c = 0; c < BN; ++c)
+                if (c >= valid) sv[c] = -INFINITY;
+            }
+          } else if (v.low > 0 || valid < BN) {
 #pragma unroll
             for (int q = 0; q < BN / 32; ++q) {
-              const int lo = v.low - 32 * q, hi = valid - 32 * q;
-              {
-                const unsigned shown =
-                    low_bits(hi) & (~low_bits(lo) | low_bits(v.sinks - 32 * q));
+              const unsigned shown = low_bits(valid - 32 * q) &
+                                     (~low_bits(v.low - 32 * q) | low_bits(v.sinks - 32 * q));
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                  if (!(shown >> i & 1)) sv[32 * q + i] = -INFINITY;
-              }
+              for (int i = 0; i < 32; ++i)
+                if (!(shown >> i & 1)) sv[32 * q + i] = -INFINITY;
             }
           }
         } else if (valid < BN) {
