@@ -58,6 +58,28 @@
 // (3.5 TB/s): 1.2 us for a block of 64 keys in turn through score MMAs (64 keys a
 // step run at half rate), the exchange and the softmax, and 15 us of start, first
 // copies and join.
+//
+// With a sliding window (WIN; App. D.4) a row sees the sinks j < S and e - w <= j < e, e the
+// end of its block of the mask. A tile's key blocks are then two runs, the sinks' pages and
+// those from the first row's window on (tile_span), and the row masks cut both ends; hidden
+// keys may be NaN, so their rows of c are cleared before the output MMAs. The sinks may have
+// positional queries of their own (App. D.5: k is stored rotated at absolute times, and a
+// second rotation of q_r puts the sinks next to the window): a q_r tile more, in TMEM where it
+// fits, for the columns that hold sinks. What a tile costs stops growing where its window is
+// full, so the shares' cost has a knee (Cost<true>).
+// Measured on the GPU: 4 x 4,680 tokens, a sink frame of 1,560 and the newest 9,360 tokens (12
+// heads, d_c = 192, d_r = 32; 2.04 TFLOP) 1.04 ms in short runs (1,960 TFLOP/s, 1.03 of the
+// measured burst rate; tensor pipe 83 % active under ncu) and 1.14 - 1.18 ms at the power limit;
+// 9 prompts of up to 3,333 tokens, window 1,024, 4 sinks (16 heads, d_c = 128, d_r = 64) 167 -
+// 185 us: 9 blocks of 2,100 - 2,500 clocks a tile, the softmax's (1,400 - 2,000 of them), and
+// 6,500 between tiles (next segment, Q to TMEM, the last output); 28,000 tokens, window 4,096 (8
+// heads, d_c = 256) 752 us: two stages of 73 KB do not hide the copies (as without a window);
+// 5 drafted tokens of 16 streams, window 4,096 (16 heads, d_c = 512) 36.5 us.
+// Not kept: blocks of 32 keys at a window's ends (205 -> 208 us for the prompts, chunks 1,135 ->
+// 1,323); at d_c <= 128 Q in shared memory with the next tile's scores ahead of this one's
+// output (2 % faster on average, 3 % slower where windows are long); Q copied to TMEM before
+// the last block's weights (5 - 9 % slower with the votes that it needs).
+
 #pragma once
 
 #include <type_traits>
@@ -69,7 +91,7 @@
 namespace vmla {
 namespace {
 
-constexpr int kThreads = 256;  // 8 warps (the fourth has no role)
+constexpr int kThreads = 256;  // 8 warps (the fourth: with a window a look at the metadata)
 constexpr float kRescaleLog2 = 8.0f;
 
 template <int DC, int DR, bool WIN>

@@ -32,6 +32,19 @@
 // DRAM at 70 % of its peak over the kernel's start and end). The tensor-memory path
 // on the same calls: 13.3, 18.0 and 79.4 us, and with pages of 16 tokens, whose
 // copies are 2 KB boxes there, 102 us instead of 84.5.
+//
+// With a sliding window (WIN) a warp leaves out 16 keys that no row of the tile sees, and the
+// sinks' keys are scored by their own q_r (fragments loaded again where a warp passes from
+// sinks to window). 64 streams, one sink frame of 1,560 and a window of 9,360 tokens (12 heads,
+// d_c = 192): 60.8 us, 229 MB, exactly the bytes needed (ncu: 229.1 MB read), 3.8 TB/s over the
+// call and 5.8 between start and end.
+// Teams (TEAM): where a window bounds the keys of a tile, a cluster of 1 to 8 CTAs takes whole
+// tiles, each CTA a part of their blocks, and the CTAs send their rows (maximum, sum, O) to one
+// another's shared memory, where each joins its share of the 16 rows, parts in order: no share
+// search, no partial rows in the workspace, no second launch. One token on a window of 512 and
+// 4 sinks 8.7 us, by shares 10.6. What is left is latency: row starts, the page table, keys,
+// the warps' sums, the cluster's barrier, about a microsecond each.
+
 #pragma once
 
 #include "internal.h"

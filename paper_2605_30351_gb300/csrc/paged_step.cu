@@ -2,6 +2,10 @@
 // of the step's rows and the lengths to grow to, then the new tokens' coordinates and
 // rows of the pool. A stream's index of a token is its place among the held ones plus
 // what was given back (App. D.4); the sinks' coordinates are those of App. D.5.
+//
+// Both are bound by latency (a launch, then one or two dependent loads). Measured on the GPU:
+// the plan of 64 streams 1.5 us, of 65,536 4.4; positions and rows of 64 tokens 2.6 us, of
+// 30,900 2.3. A call from Python takes 6 - 7.5 us: two thirds of it the binding and the launch.
 #include "internal.h"
 #include "paged_attn.cuh"
 #include "ptx_sm103.cuh"
