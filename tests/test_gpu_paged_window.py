@@ -375,6 +375,19 @@ def test_an_unaligned_workspace():
     assert torch.equal(ref, p.run())
 
 
+@pytest.mark.parametrize("new", [[2], [60], [400]])
+@pytest.mark.parametrize("d_c", [64, 192, 256, 512])
+def test_an_output_off_32_bytes(new, d_c):
+    """o on a 16-byte boundary: rows are not stored 32 bytes at a time."""
+    p = Problem([500], new, 100, 20, heads=12, d_c=d_c, page=64, dirty=False)
+    ref = p.run()
+    o = torch.full((p.q_c.numel() + 8,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    assert o[8:].data_ptr() % 32 == 16
+    p.call(o[8:].view(p.q_c.shape))
+    torch.cuda.synchronize()
+    assert torch.equal(o[8:].view(p.q_c.shape), ref) and o[:8].isnan().all()
+
+
 def test_bad_metadata_is_recorded():
     """Lengths, indices, page numbers and row starts that cannot be: nothing is read out of
     range, the other streams' rows are right."""
