@@ -70,11 +70,11 @@
 // Measured on the GPU: 4 x 4,680 tokens, a sink frame of 1,560 and the newest 9,360 tokens (12
 // heads, d_c = 192, d_r = 32; 2.04 TFLOP) 1.04 ms in short runs (1,960 TFLOP/s, 1.03 of the
 // measured burst rate; tensor pipe 83 % active under ncu) and 1.14 - 1.18 ms at the power limit;
-// 9 prompts of up to 3,333 tokens, window 1,024, 4 sinks (16 heads, d_c = 128, d_r = 64) 167 -
-// 185 us: 9 blocks of 2,100 - 2,500 clocks a tile, the softmax's (1,400 - 2,000 of them), and
+// 9 prompts of up to 3,333 tokens, window 1,024, 4 sinks (16 heads, d_c = 128, d_r = 64) 164 -
+// 180 us: 9 blocks of 2,100 - 2,500 clocks a tile, the softmax's (1,400 - 2,000 of them), and
 // 6,500 between tiles (next segment, Q to TMEM, the last output); 28,000 tokens, window 4,096 (8
-// heads, d_c = 256) 752 us: two stages of 73 KB do not hide the copies (as without a window);
-// 5 drafted tokens of 16 streams, window 4,096 (16 heads, d_c = 512) 36.5 us.
+// heads, d_c = 256) 743 us: two stages of 73 KB do not hide the copies (as without a window);
+// 5 drafted tokens of 16 streams, window 4,096 (16 heads, d_c = 512) 33.3 us.
 // Not kept: blocks of 32 keys at a window's ends (205 -> 208 us for the prompts, chunks 1,135 ->
 // 1,323); at d_c <= 128 Q in shared memory with the next tile's scores ahead of this one's
 // output (2 % faster on average, 3 % slower where windows are long); Q copied to TMEM before

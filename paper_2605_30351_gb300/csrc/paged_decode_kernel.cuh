@@ -36,7 +36,7 @@
 // With a sliding window (WIN) a warp leaves out 16 keys that no row of the tile sees, and the
 // sinks' keys are scored by their own q_r (fragments loaded again where a warp passes from
 // sinks to window). 64 streams, one sink frame of 1,560 and a window of 9,360 tokens (12 heads,
-// d_c = 192): 60.8 us, 229 MB, exactly the bytes needed (ncu: 229.1 MB read), 3.8 TB/s over the
+// d_c = 192): 57.7 us, 229 MB, exactly the bytes needed (ncu: 229.1 MB read), 4.0 TB/s over the
 // call and 5.8 between start and end.
 // Teams (TEAM): where a window bounds the keys of a tile, a cluster of 1 to 8 CTAs takes whole
 // tiles, each CTA a part of their blocks, and the CTAs send their rows (maximum, sum, O) to one
@@ -133,13 +133,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   grid_dep_sync();
-  // one block looks at the metadata; of a team while its first keys are on their way
+  // one block looks at the metadata; with a window while its first keys are on their way
   bool checked = blockIdx.x != 0;
   auto check = [&]() {
     if (!checked) check_streams<WIN>(p, threadIdx.x, kDecodeThreads);
     checked = true;
   };
-  if constexpr (!TEAM) check();
+  if constexpr (!WIN) check();
   // What a CTA computes: a share of all tiles' blocks, or as one of a team of CTAs (a
   // cluster), which takes whole streams in turn, its part of each of their tiles.
   const int team = TEAM ? static_cast<int>(cluster_nctarank()) : 1;
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     asm volatile("cp.async.commit_group;" ::: "memory");
 #pragma unroll 1
     for (int i = 0; i < NST - 1; ++i) fetch(i);
-    if constexpr (TEAM) check();
+    if constexpr (WIN) check();
     asm volatile("cp.async.wait_group %0;" ::"n"(NST - 1) : "memory");
     __syncthreads();
     uint32_t q[S::kQRegs ? kSteps : 1][4];
@@ -575,8 +575,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       }
     __syncthreads();  // sQ, the sums and the buffers are the next segment's
   }
+  if constexpr (WIN) check();
   if constexpr (TEAM) {
-    check();
     cluster_wait_acquire();
   } else {
     if (!any && threadIdx.x == 0)
