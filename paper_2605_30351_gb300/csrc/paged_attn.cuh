@@ -241,9 +241,13 @@ constexpr int kTileCost = 4 * BN;
 // inside a tile pays for its Q and O too, as nearly all do, and one that begins another tile
 // besides pays twice. At the tile's end, spread over its keys, the slowest CTA of 5 drafted
 // tokens of 16 streams at d_c = 512 had two tiles and took 29 us, those with one 20.5; the
-// call takes 36.9 us so and 33.3 in front, 64 streams of one token 60.8 and 58.0, 66 calls
+// call takes 36.9 us so and 33.1 in front, 64 streams of one token 60.8 and 57.8, 66 calls
 // of prompts and long windows 5 % less on average. Two or three blocks for tiles of 128 rows
 // and two or four for those of 16 differ from these by 1 % on average.
+// In shares of few blocks a tile's head in front would leave CTAs without work, and whole blocks
+// to the others: only what a share is longer than a block comes in front (of tiles of 128 rows
+// twice that), the rest is spread over the keys. One token of one stream on 4,000 keys (d_c = 192)
+// 11.3 us so, 12.3 with all of it in front; 20 calls at d_c = 512 2 % less on average.
 template <int BN, int TR, bool WIN>
 constexpr int kTileHead = !WIN ? kTileCost<BN> : TR > 16 ? 4 * BN : 3 * BN;
 
@@ -387,8 +391,10 @@ __device__ __forceinline__ long long find_share(const PagedP<WIN>& p, int id, in
         const Span<WIN> span = tile_span<BN, TR, WIN>(p, st, lo);
         long long in = rem - at, all = c.before(lo + 1) - at;
         if constexpr (WIN) {
-          in = max(in - kTileHead<BN, TR, WIN>, 0ll);
-          all = max(all - kTileHead<BN, TR, WIN>, 1ll);
+          long long head = kTileHead<BN, TR, WIN>;
+          head = min(head, (TR > 16 ? 2 : 1) * max(total / active - BN, 0ll));
+          in = max(in - head, 0ll);
+          all = max(all - head, 1ll);
         }
         const int off = static_cast<int>(
             static_cast<float>(in) *
