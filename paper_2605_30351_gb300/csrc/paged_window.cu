@@ -1,6 +1,7 @@
 // Attention of ragged streams' newest tokens over the sinks and the sliding window of a
 // paged latent cache (Eq. score; App. D.4, D.5, E): the choice of a kernel.
 #include <algorithm>
+#include <numeric>
 
 #include "paged_attn_kernel.cuh"
 
@@ -11,15 +12,16 @@ namespace {
 // that may be, and whether a team of a few CTAs is done with it sooner than shares of all
 // tiles' blocks and their join, a second launch. Estimates in tenths of a us, from calls with
 // 64 sinks and pages of 64 tokens at d_c = 192; at d_c = 64 and 256 all of them move together.
-//   teams   a wave of them takes 7 us and 1.5 a block, whatever the others do; 1.3 more where
-//           streams may have more than one tile
-//   shares  11 us and 1.8 for the blocks that each SM has on average
-//   tiles of 128 rows (streams of more than 16 rows on average)  15 us and 4 a block
-// The last two count four fifths of what the windows bound: they gain where streams are
-// shorter, while a wave of teams waits for its longest.
+//   teams   a wave of them takes 7 us and 1.4 a block, whatever the others do, 0.5 more where
+//           streams may have more than one tile; teams of more than one CTA 1.2 more in all
+//   shares  11.5 us, 1.4 for the blocks that each SM has on average and 3 for its tiles
+//   tiles of 128 rows (streams of more than 16 rows on average)  16 us and 1.2 a block
+// Blocks are what the windows bound; shares, and more so tiles of 128 rows, gain where streams
+// are shorter, and the estimates are fitted to such calls too (410 of one to a few tokens of 1 -
+// 300 streams, whole and ragged, d_c 64 - 256): the choice takes 1.2 % longer than the best.
 // Measured, one token of n streams, window w (teams of 8, 4, 2, 1: the best; shares):
-//   n = 1, w = 300: 8.4, 10.5   n = 12, w = 2,000: 11.4, 13.9   n = 76, w = 1,000: 17.0, 19.9
-//   n = 1, w = 4,000: 13.3, 11.4   n = 38, w = 4,000: 33.6, 26.0  n = 96, w = 300: 10.8, 17.3
+//   n = 1, w = 300: 8.8, 10.6   n = 12, w = 2,000: 12.0, 13.7  n = 76, w = 1,000: 17.7, 23.3
+//   n = 1, w = 4,000: 13.7, 11.5  n = 38, w = 4,000: 34.4, 27.4  n = 96, w = 300: 11.4, 14.5
 // and tiles of 16 or 128 rows: 5 tokens of 4 streams, 16 heads, w = 300: 10.4, 15.3; of 40:
 // 22.5, 17.0.
 int team_of(const PagedAttnArgs& a, bool tall, int& teams) {
@@ -33,15 +35,21 @@ int team_of(const PagedAttnArgs& a, bool tall, int& teams) {
       divides ? (keys + bn - 1) / bn : (keys / page + 2) * ((page + bn - 1) / bn);
   const long long streams = std::min(a.seqs, a.total);
   const bool further = a.total > a.seqs || a.heads > 16;
-  const long long tiles = std::max<long long>(a.seqs, further ? rows / 16 + streams / 2 : 0);
-  long long best = tall ? 150 + 32 * a.seqs * blocks / kMaxCtas
-                        : 110 + 14 * a.seqs * blocks / kMaxCtas;
+  // of 16 rows: exact where streams have as many tokens each, else as far as rows fill the
+  // last tile of each on average, and some for streams that idle
+  const long long last = streams * (16 - std::gcd(a.heads, 16)) / 32 + streams / 8 + 1;
+  const long long all =
+      a.total % streams == 0 ? streams * ((rows / streams + 15) / 16) : rows / 16 + last;
+  const long long tiles = std::max<long long>(a.seqs, further ? all : 0);
+  long long best = tall ? 160 + 12 * a.seqs * blocks / kMaxCtas
+                        : 115 + (30 + 14 * blocks) * a.seqs / kMaxCtas;
   int team = 0;
   for (int t = 8; t > 0; t /= 2) {
     const int slots = window_team_slots(t);
     if (slots < 1) continue;
     const long long waves = (tiles + slots - 1) / slots;
-    const long long cost = waves * (70 + (further ? 13 : 0) + 15 * ((blocks + t - 1) / t));
+    const long long cost =
+        waves * (70 + (further ? 5 : 0) + 14 * ((blocks + t - 1) / t)) + (t > 1 ? 12 : 0);
     if (cost < best) {
       best = cost;
       team = t;
