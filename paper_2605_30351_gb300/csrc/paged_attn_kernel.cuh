@@ -176,6 +176,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr bool kLate = WIN && CL == 2 && S::kSplit == 1;
   constexpr uint16_t kPair = static_cast<uint16_t>((1u << CL) - 1u);
   static_assert(S::kSplit == 1 || CL == S::kSplit, "split tiles take a pair");
+  static_assert((2 * NST + 3 * NB + 12) * 8 + 64 + 2 * sizeof(Place<WIN>) + 8 <= S::kBarBytes,
+                "barriers, the search's sums, the share's ends and two words fit");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = align_smem_1024(smem_raw);
   uint8_t* sQ = smem;

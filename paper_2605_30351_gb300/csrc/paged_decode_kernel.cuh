@@ -86,6 +86,7 @@ struct DecodeShape {
   static_assert(kStages >= 2 && kQBytes % 16 == 0, "two stages must fit");
   static_assert(!TEAM || kRows * kRedStride * 4 <= kTileBytes * kStages,
                 "the warps' results fit in the ring");
+  static_assert(64 + 2 * sizeof(Place<WIN>) <= 192, "the search's sums and the share's ends fit");
 };
 
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t addr) {
