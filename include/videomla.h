@@ -621,7 +621,10 @@ int mla_paged_window_plan(const mla_paged_cache* cache, const mla_paged_window* 
  * T and frame_width are at least 1, frame_width at most T. A token without a page has the
  * row -1 (MLA_ERR_RANGE); tokens that are no stream's (a q_start that does not ascend
  * from 0 to total, recorded too) are not written. A token at a negative place has the
- * coordinates 0. The arrays must not overlap (MLA_ERR_ARG). total = 0 is MLA_OK.
+ * coordinates 0. A stream that gave tokens back and whose new ones lie among the sinks'
+ * pages (its list was cut to less than those) has no indices for them: rows -1, coordinates
+ * 0, MLA_ERR_RANGE. Cut such a list to 0 instead, so that it starts anew. The arrays must
+ * not overlap (MLA_ERR_ARG). total = 0 is MLA_OK.
  */
 int mla_paged_window_positions(const mla_paged_cache* cache, const mla_paged_window* window,
                                const int* q_start, int total, int causal_block,

@@ -212,11 +212,13 @@ def slide(pages, gone, keep, sinks):
         gone[s] += n * P
 
 
-def window_positions(held, gone, new, block, window, sinks, frame, width):
-    """[(t, h, w)], [(t beside the sinks, h, w)] of the newest `new` tokens."""
+def window_positions(held, gone, new, block, window, sinks, frame, width, page=1):
+    """[(t, h, w)], [(t beside the sinks, h, w)] of the newest `new` tokens. Of a stream that
+    gave tokens back they lie behind the sinks' pages, else they have no index."""
     out, beside, total = [], [], held + gone
+    refused = gone > 0 and held - new < front(sinks, page)
     for i in range(new):
-        if held - new + i < 0:
+        if refused or held - new + i < 0:
             out.append((0, 0, 0))
             beside.append((0, 0, 0))
             continue

@@ -25,6 +25,12 @@ struct PartLayout {
   }
 };
 
+// Places of the pages that hold a stream's sinks; past the largest index they are all alike.
+inline int sink_places(int sinks, int page_tokens) {
+  const long long n = (static_cast<long long>(sinks) + page_tokens - 1) / page_tokens * page_tokens;
+  return static_cast<int>(n < kMostTokens ? n : kMostTokens);
+}
+
 // What a short call pays for is the code that it runs for the first time, about 15
 // ns an instruction: divisions by the call's own numbers are prepared on the host.
 // n / d for 0 <= n < 2^31 and d >= 1: mul = floor(2^shift / d) + 1 with shift = 31 +
@@ -659,9 +665,7 @@ PagedP<WIN> paged_params(const PagedAttnArgs& a, int bn, int dv) {
     k.dropped = a.dropped;
     k.window = a.window;
     k.sinks = a.sinks;
-    const long long front =
-        (static_cast<long long>(a.sinks) + a.page_tokens - 1) / a.page_tokens * a.page_tokens;
-    k.front = static_cast<int>(front < kMostTokens ? front : kMostTokens);
+    k.front = sink_places(a.sinks, a.page_tokens);
     k.turned = a.q_sink != nullptr && a.sinks > 0;
     k.compact = divides;
     k.o_wide = aligned_to(a.o, 32);

@@ -78,7 +78,7 @@ struct PositionsK {
   int* pos;
   int* pos_sink;
   int* rows;
-  int total, seqs, pages, page_tokens, max_pages, window, sinks, block, axes;
+  int total, seqs, pages, page_tokens, max_pages, window, sinks, front, block, axes;
   int frame, width;
   Div by_page, by_mask, by_frame, by_width;
   int* status;
@@ -114,7 +114,10 @@ __global__ void __launch_bounds__(kPos) window_positions_kernel(const PositionsK
   const int len = p.lens[lo], gone = p.dropped ? p.dropped[lo] : 0;
   int g = 0, hidden = 0, row = -1;
   const long long place = static_cast<long long>(len) - (q1 - q0) + (t - q0);
-  if (len < 0 || gone < 0 || static_cast<long long>(len) + gone >= kMostTokens) {
+  if (len < 0 || gone < 0 || static_cast<long long>(len) + gone >= kMostTokens ||
+      (gone > 0 && static_cast<long long>(len) - (q1 - q0) < p.front)) {
+    // no stream, or new tokens among the sinks' pages of one that gave tokens back: attention
+    // refuses the same (stream_held)
     record_status(p.status, MLA_ERR_RANGE);
   } else if (place >= 0) {
     const int j = p.by_page(static_cast<int>(place));
@@ -173,6 +176,7 @@ int launch_paged_positions(const PagedPositionsArgs& a) {
   k.max_pages = a.max_pages;
   k.window = a.window;
   k.sinks = a.sinks;
+  k.front = sink_places(a.sinks, a.page_tokens);
   k.block = a.causal_block;
   k.axes = a.axes;
   k.frame = a.tokens_per_frame;
