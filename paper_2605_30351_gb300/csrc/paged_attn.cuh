@@ -126,10 +126,19 @@ __device__ __forceinline__ bool stream_held(const PagedP<WIN>& p, int n, int len
 template <bool WIN>
 __device__ __forceinline__ Stream<WIN> stream_at(const PagedP<WIN>& p, int s) {
   Stream<WIN> t{p.q_start[s], p.q_start[s + 1], p.lens[s]};
-  if constexpr (WIN) t.gone = p.dropped ? p.dropped[s] : 0;
   const int q1 = t.n;
   t.n = q1 - t.q0;
-  if (t.q0 < 0 || q1 < t.q0 || q1 > p.total || !stream_held<WIN>(p, t.n, t.len, t.gone)) t.n = 0;
+  // The two tests say the same without a window; but through stream_held the compiler orders
+  // the block loop at d_c = 512, d_r = 64 so that it takes 3 - 6 % longer (429 tokens of 3
+  // streams on 18,367 keys: 496 us, 466 so).
+  if constexpr (WIN) {
+    t.gone = p.dropped ? p.dropped[s] : 0;
+    if (t.q0 < 0 || q1 < t.q0 || q1 > p.total || !stream_held<WIN>(p, t.n, t.len, t.gone)) t.n = 0;
+  } else {
+    if (t.q0 < 0 || q1 < t.q0 || q1 > p.total || t.len < 0 ||
+        t.len > static_cast<long long>(p.max_pages) * p.page_tokens)
+      t.n = 0;
+  }
   return t;
 }
 
