@@ -661,7 +661,8 @@ int mla_paged_window_attention(const mla_paged_cache* cache, const mla_paged_win
  * was is free afterwards; a page that branches share stays theirs. A page number outside
  * the pool is recorded as MLA_ERR_RANGE and leaves the list; a stream whose indices would
  * pass 2^31 - 2^16 is recorded and left alone, as is one whose length its table cannot
- * hold or whose dropped is negative. dropped must not be NULL.
+ * hold or whose dropped is negative. dropped must not be NULL. keep, dropped, table, lens and
+ * refs must not overlap (MLA_ERR_ARG).
  */
 int mla_pages_slide(mla_paged_cache* cache, const mla_paged_window* window, const int* keep,
                     void* stream);

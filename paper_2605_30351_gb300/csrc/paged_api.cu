@@ -49,12 +49,16 @@ int check_window(const mla_paged_window* w, bool dropped) {
   return MLA_OK;
 }
 
+long long table_ints(const mla_paged_cache* c) {
+  return static_cast<long long>(c->seqs) * c->max_pages;
+}
+
 // Whether two of the arrays (address, ints) share memory.
 bool overlap(std::initializer_list<std::pair<const int*, long long>> arrays) {
   for (const auto& a : arrays)
     for (const auto& b : arrays)
-      if (&a < &b && a.first && b.first && a.first < b.first + b.second &&
-          b.first < a.first + a.second)
+      if (&a < &b && a.first && b.first && a.second > 0 && b.second > 0 &&
+          a.first < b.first + b.second && b.first < a.first + a.second)
         return true;
   return false;
 }
@@ -324,6 +328,12 @@ int mla_pages_slide(mla_paged_cache* cache, const mla_paged_window* window, cons
   if (!keep || !aligned_to(keep, 4)) return MLA_ERR_ARG;
   int rc = check_window(window, true);
   if (rc == MLA_OK) rc = check_buffers(cache, false);
+  if (rc == MLA_OK && overlap({{cache->table, table_ints(cache)},
+                               {cache->lens, cache->seqs},
+                               {cache->refs, cache->pages},
+                               {keep, cache->seqs},
+                               {window->dropped, cache->seqs}}))
+    rc = MLA_ERR_ARG;
   if (rc == MLA_OK)
     rc = check_resident({cache->table, cache->lens, cache->refs, keep, window->dropped});
   if (rc != MLA_OK) return rc;
