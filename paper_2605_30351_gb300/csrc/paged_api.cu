@@ -291,6 +291,7 @@ int mla_paged_window_positions(const mla_paged_cache* cache, const mla_paged_win
                                {pos, n},
                                {pos_sink, n},
                                {rows, total},
+                               {cache->table, table_ints(cache)},
                                {cache->lens, cache->seqs},
                                {window->dropped, cache->seqs}}))
     rc = MLA_ERR_ARG;

@@ -50,3 +50,9 @@ def test_slide(a, b):
     """It writes table, lens, refs and dropped, a block per stream, while others read them and
     keep."""
     refused("mla_pages_slide", a, b)
+
+
+@pytest.mark.parametrize("a", ["pos", "pos_sink", "rows"])
+def test_positions_and_the_page_table(a):
+    """Pages are looked up while other blocks write pos, pos_sink and rows."""
+    refused("mla_paged_window_positions", a, "table")
