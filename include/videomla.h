@@ -668,7 +668,8 @@ int mla_pages_slide(mla_paged_cache* cache, const mla_paged_window* window, cons
                     void* stream);
 
 /* mla_pages_fork for streams whose window slides: dropped[dst[i]] becomes dropped[src[i]]
- * too. dropped must not be NULL. */
+ * too. dropped must not be NULL; it, table, lens and refs must not overlap one another or src
+ * or dst (MLA_ERR_ARG). */
 int mla_pages_window_fork(mla_paged_cache* cache, const mla_paged_window* window,
                           const int* src, const int* dst, int n, void* stream);
 

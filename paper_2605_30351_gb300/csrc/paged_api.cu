@@ -351,6 +351,14 @@ int mla_pages_window_fork(mla_paged_cache* cache, const mla_paged_window* window
   if (rc == MLA_OK) rc = check_sizes(cache);
   if (rc == MLA_OK && n > cache->seqs) rc = MLA_ERR_ARG;
   if (rc == MLA_OK) rc = check_buffers(cache, false);
+  if (rc == MLA_OK)  // src and dst are only read: they may be anywhere else
+    for (const int* pairs : {src, dst})
+      if (overlap({{cache->table, table_ints(cache)},
+                   {cache->lens, cache->seqs},
+                   {cache->refs, cache->pages},
+                   {pairs, n},
+                   {window->dropped, cache->seqs}}))
+        rc = MLA_ERR_ARG;
   if (rc == MLA_OK)
     rc = check_resident({cache->table, cache->lens, cache->refs, src, dst, window->dropped});
   if (rc != MLA_OK || n == 0) return rc;

@@ -56,3 +56,11 @@ def test_slide(a, b):
 def test_positions_and_the_page_table(a):
     """Pages are looked up while other blocks write pos, pos_sink and rows."""
     refused("mla_paged_window_positions", a, "table")
+
+
+@pytest.mark.parametrize("a,b", [(a, b) for a in ("dropped", "src", "dst") for b in ("table", "lens", "refs")] +
+                         [("src", "dropped"), ("dst", "dropped")])
+def test_branches(a, b):
+    """They write the new stream's row of the table, its length and count, and the pages'
+    reference counts."""
+    refused("mla_pages_window_fork", a, b)
