@@ -1,9 +1,11 @@
-"""Rollouts that never end, in a pool of fixed size and one captured graph.
+"""Rollouts much longer than their window, in a pool of fixed size and one captured graph.
 
 Each rollout keeps its first frame (the sink) and a window of its newest frames; what lies
 between goes back to the pool, and positions are counted with sink and window next to each
 other (App. D.4, D.5). A step of all rollouts is one graph: lengths, pages and positions come
-from the device, so the same graph is replayed chunk after chunk.
+from the device, so the same graph is replayed chunk after chunk. Keys are rotated at absolute
+frames, so the rotary table has to hold as many as a rollout will have (128 bytes each; 1,024 of them
+by default, which a rollout would leave behind).
 
     counts to rows and lengths                      mla_paged_window_plan
     pages for them                                  mla_pages_resize
@@ -32,13 +34,14 @@ BF16, I32 = torch.bfloat16, torch.int32
 
 
 class Step:
-    """One chunk of every rollout over a paged cache with a sliding window, as a graph."""
+    """One chunk of every rollout over a paged cache with a sliding window, as a graph; rollouts
+    of up to `longest` frames."""
 
-    def __init__(self, w, rollouts, frames, page=16):
+    def __init__(self, w, rollouts, frames, longest, page=16):
         self.w, self.n = w, frames * w.tokens_per_frame
         T, S, W = w.tokens_per_frame, w.sink_frames, w.window_frames
         most = -(-S * T // page) + -(-((W - S) * T + page) // page)
-        cfg = V.make_config(w)
+        cfg = V.make_config(w.with_(rope_table_len=max(w.rope_table_len, longest)))
         self.cache = V.PagedCache.empty(1, most * rollouts, page, rollouts, most, w.d_c, w.d_r)
         self.window = V.PagedWindow((W - S) * T, S * T, torch.zeros(rollouts, dtype=I32, device="cuda"))
         self.rope = V.Rope(torch.from_numpy(V.mla_rope_table_fill(cfg)).cuda(), w.rope_pairs)
@@ -82,7 +85,7 @@ def main(chunks=12, rollouts=2, frames=2):
     w = synth.workload("tiny").with_(batch=1, sink_frames=1, window_frames=7)
     n = frames * w.tokens_per_frame
     wt = {k: v.cuda() for k, v in synth.draw_layer_weights(w, 1).items()}
-    step = Step(w, rollouts, frames)
+    step = Step(w, rollouts, frames, chunks * frames)
     rings = [V.LatentCache(V.make_config(w)) for _ in range(rollouts)]
     stage = [V.LatentCache(V.make_config(w.with_(window_frames=frames, sink_frames=0), V.MLA_FLAG_ROTATE_AT_USE))
              for _ in range(rollouts)]

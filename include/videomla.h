@@ -571,9 +571,16 @@ int mla_paged_attention(const mla_paged_cache* cache, int layer, const void* q_c
  *
  * A stream keeps its first tokens, the sinks, for good, and a window of its newest
  * ones; the pages between them are given back and the stream's page list closes up,
- * so a stream may go on for ever in a short list. All of it is the paged cache above:
+ * so a stream may be much longer than its list. All of it is the paged cache above:
  * mla_pages_resize, mla_paged_append and the other calls work on the tokens that are
  * held.
+ * A stream ends with its indices, below 2^31 - 2^16, or with its rotary table: keys are
+ * stored rotated at absolute times, so the token of index g needs table_len > g /
+ * tokens_per_frame (past it mla_paged_append and mla_rope_apply record MLA_ERR_RANGE and
+ * turn by 0, and the attention of that stream is wrong from there on). A table takes 4 d_r
+ * bytes a position, for d_r = 32 128 KB for the default 1,024 frames, 176 MB for all indices
+ * at 1,560 tokens a frame, and token by token 128 MB for every million. (The ring's
+ * mla_attention_window_forward numbers the frames it holds anew and has no such end.)
  * ------------------------------------------------------------------------ */
 
 /*
