@@ -1,4 +1,8 @@
-"""Where the streams of a sliding window end: lists cut back into the sinks' pages."""
+"""Where the streams of a sliding window end: lists cut back into the sinks' pages, the rotary
+table."""
+
+import importlib.util
+import os
 
 import numpy as np
 import pytest
@@ -10,6 +14,9 @@ from paper_2605_30351_gb300 import videomla as V
 pytestmark = pytest.mark.gpu
 
 I32, BF16 = torch.int32, torch.bfloat16
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+# weights and output are rounded to bf16 once each; scores move a weight by less than 2^-10
+REL = 2 * 2.0 ** -8 + 2.0 ** -10
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -72,3 +79,94 @@ def test_a_list_cut_back_into_the_sinks_pages(cut, new):
     V.mla_paged_window_attention(cache, win, 0, q, q[:, :, :32].contiguous(), None, q_start, 128, 1, ws, o)
     assert V.mla_device_status(clear=True) == (V.MLA_ERR_RANGE if refused else V.MLA_OK)
     assert (o[:new] == (7.0 if refused else 0.0)).all() and (o[new:] == 0).all()
+
+
+def test_a_stream_past_the_usual_table():
+    """Coordinates are absolute, so a stream goes as far as its rotary table: the 1,024
+    positions that a configuration has by default, or as many as the caller makes. Tokens 1,000 to
+    1,047 of a stream: with the longer table their keys and queries are those of the formula's
+    angles; with the short one each coordinate past its end is recorded, by the append and by the
+    rotation, and counts as 0."""
+    page, new, m = 16, 48, 16
+    cache = V.PagedCache.empty(1, 8, page, 1, 7, 64, 32)
+    win = V.PagedWindow(30, 4, i32([0]))
+    V.mla_pages_resize(cache, i32([40]))
+    win.dropped.fill_(960)
+    q_start, lens, pos, rows = ints(2), ints(1), ints(new, 1), ints(new)
+    V.mla_paged_window_plan(cache, win, i32([new]), q_start, lens)
+    V.mla_pages_resize(cache, lens)
+    V.mla_paged_window_positions(cache, win, q_start, 1, 1, 1, pos, None, rows)
+    assert pos[:, 0].tolist() == list(range(1000, 1048)) and V.mla_device_status(clear=True) == V.MLA_OK
+    g = torch.Generator(device="cuda").manual_seed(3)
+    c, kr, q = (torch.randn(new, *s, device="cuda", generator=g).to(BF16) for s in ((64,), (32,), (3, 32)))
+    freq = 10000.0 ** (-np.arange(m) / m)
+    for length in (1048, 1024, 4096):
+        rope = V.Rope(torch.from_numpy(V.mla_rope_scaled_table_fill(32, length)).cuda(), (m, 0, 0), axes=1)
+        inside = np.array([p < length for p in range(1000, 1048)])
+        y = torch.empty_like(q)
+        for call in (lambda: V.mla_paged_append(cache, 0, c, kr, q_start, pos, rope),
+                     lambda: V.mla_rope_apply(rope, q, pos, y)):
+            call()
+            assert V.mla_device_status(clear=True) == (V.MLA_OK if inside.all() else V.MLA_ERR_RANGE), length
+        angle = np.where(inside, np.arange(1000, 1048), 0)[:, None] * freq
+        cos, sin = np.cos(angle), np.sin(angle)
+        got = cache.kr[0].view(-1, 32)[rows.long()]
+        for x, z in ((kr[:, None], got[:, None]), (q, y)):
+            x, z = x.double().cpu().numpy(), z.double().cpu().numpy()
+            a, b = x[..., ::2], x[..., 1::2]
+            # one rounding to bf16; the table's (2^-24) and three of fp32 arithmetic on |a|, |b|
+            for ref, out in ((a * cos[:, None] - b * sin[:, None], z[..., ::2]),
+                             (a * sin[:, None] + b * cos[:, None], z[..., 1::2])):
+                bound = 2.0 ** -8 * np.abs(ref) + 2.0 ** -21 * (np.abs(a) + np.abs(b))
+                assert (np.abs(out - ref) <= bound).all(), length
+
+
+def test_a_stream_shifted_back_by_a_constant():
+    """Scores depend on distances only: a stream across the end of the usual table gives what
+    the same stream gives 1,000 positions earlier. A rotated key or query is off by a rounding of 2^-8
+    of its size, so a score by (2 * 2^-8 + 2^-16) sum |q_r| |k| / sqrt(128) in each of the two, sums over
+    the pairs; weights by a factor of exp of twice that; on top of the two rounding bounds."""
+    page, new, d_r = 16, 40, 32
+    rope = V.Rope(torch.from_numpy(V.mla_rope_scaled_table_fill(d_r, 2048)).cuda(), (16, 0, 0), axes=1)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    held = 100
+    c, kr = (torch.randn(held, w, device="cuda", generator=g).to(BF16) for w in (64, d_r))
+    q_c, q_r = (torch.randn(new, 4, w, device="cuda", generator=g).to(BF16) for w in (64, d_r))
+    outs, keys = [], []
+    for first in (0, 960):                            # tokens given back: whole pages
+        cache = V.PagedCache.empty(1, 8, page, 1, 8, 64, d_r)
+        win = V.PagedWindow(50, 0, i32([0]))
+        V.mla_pages_resize(cache, i32([held]))
+        win.dropped.fill_(first)
+        pos, q = ints(held, 1), torch.empty_like(q_r)
+        start = i32([0, held])
+        V.mla_paged_window_positions(cache, win, start, 1, 1, 1, pos)
+        V.mla_paged_append(cache, 0, c, kr, start, pos, rope)
+        V.mla_rope_apply(rope, q_r, pos[-new:].contiguous(), q)
+        o, ws = torch.empty_like(q_c), torch.empty(V.mla_paged_workspace_bytes(cache), dtype=torch.uint8, device="cuda")
+        V.mla_paged_window_attention(cache, win, 0, q_c, q, None, i32([0, new]), 128, 1, ws, o)
+        outs.append(o.double().cpu().numpy())
+    assert pos[-1, 0] == 1059 and V.mla_device_status(clear=True) == V.MLA_OK
+    kd, qd = kr.double().cpu().numpy(), q_r.double().cpu().numpy()
+    norm = lambda x: np.hypot(x[..., ::2], x[..., 1::2])  # noqa: E731  turned channels are within it
+    for i in range(new):
+        p = held - new + i
+        sees = range(max(0, p - 49), p + 1)
+        v = np.abs(c.double().cpu().numpy()[list(sees)])
+        worst = max((norm(qd[i]) @ norm(kd[j])).max() for j in sees)
+        shift = 2 * (2 * 2.0 ** -8 + 2.0 ** -16) * worst / 128 ** 0.5
+        bound = (np.exp(2 * shift) - 1 + 2 * REL) * v.max(0)
+        assert (np.abs(outs[0][i] - outs[1][i]) <= bound).all(), i
+
+
+def test_the_example_past_the_usual_table():
+    """1,032 frames: more than the 1,024 positions of a default table. Its layer agrees with
+    the sink ring, which numbers held frames anew for every window; both are within 1e-2 (relative
+    norm) of the float64 layer, the bound of the ring's own tests, so within 2e-2 of each other."""
+    spec = importlib.util.spec_from_file_location(
+        "sliding_rollouts", os.path.join(ROOT, "examples", "sliding_rollouts.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    worst, held, gone = m.main(chunks=172, rollouts=1, frames=6)
+    assert worst <= 2e-2
+    assert [h + g for h, g in zip(held, gone)] == [1032 * 64]
