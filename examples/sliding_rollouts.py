@@ -40,7 +40,7 @@ class Step:
     def __init__(self, w, rollouts, frames, longest, page=16):
         self.w, self.n = w, frames * w.tokens_per_frame
         T, S, W = w.tokens_per_frame, w.sink_frames, w.window_frames
-        most = -(-S * T // page) + -(-((W - S) * T + page) // page)
+        most = -(-S * T // page) + -(-(max((W - S) * T, self.n) + page) // page)
         cfg = V.make_config(w.with_(rope_table_len=max(w.rope_table_len, longest)))
         self.cache = V.PagedCache.empty(1, most * rollouts, page, rollouts, most, w.d_c, w.d_r)
         self.window = V.PagedWindow((W - S) * T, S * T, torch.zeros(rollouts, dtype=I32, device="cuda"))
@@ -58,7 +58,7 @@ class Step:
         self.q_c, self.q_r = rows(w.heads, w.d_c), rows(w.heads, w.d_r)
         self.q, self.q_sink, self.o = rows(w.heads, w.d_r), rows(w.heads, w.d_r), rows(w.heads, w.d_c)
         self.new = torch.full((rollouts,), self.n, dtype=I32, device="cuda")
-        self.keep = torch.full((rollouts,), self.window.window - self.n, dtype=I32, device="cuda")
+        self.keep = torch.full((rollouts,), max(0, self.window.window - self.n), dtype=I32, device="cuda")
         self.q_start, self.lens = ints(rollouts + 1), ints(rollouts)
         self.pos, self.pos_sink = ints(total, 3), ints(total, 3)
         self.run()                                  # loads the kernels; then back to the start

@@ -664,9 +664,10 @@ int mla_paged_window_attention(const mla_paged_cache* cache, const mla_paged_win
  * the sinks' pages and the newest keep[s] tokens leave the stream's list, which closes up:
  *     lens[s] -= n,  dropped[s] += n,  n a multiple of page_tokens.
  * What the next step's first token sees of a window w is kept with keep = w - 1 (token by
- * token; w - b with blocks of b tokens that a step fills). A page whose last stream this
- * was is free afterwards; a page that branches share stays theirs. A page number outside
- * the pool is recorded as MLA_ERR_RANGE and leaves the list; a stream whose indices would
+ * token; max(0, w - b) with blocks of b tokens that a step fills). A count below -1, as
+ * w - b of blocks longer than the window, is recorded as MLA_ERR_RANGE and leaves the stream
+ * alone. A page whose last stream this was is free afterwards; a page that branches share
+ * stays theirs. A page number outside the pool is recorded as MLA_ERR_RANGE and leaves the list; a stream whose indices would
  * pass 2^31 - 2^16 is recorded and left alone, as is one whose length its table cannot
  * hold or whose dropped is negative. dropped must not be NULL. keep, dropped, table, lens and
  * refs must not overlap (MLA_ERR_ARG).

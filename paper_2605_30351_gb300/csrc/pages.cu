@@ -295,7 +295,10 @@ __global__ void __launch_bounds__(kCopy)
   const int s = blockIdx.x;
   const int kept = keep[s], len = p.lens[s], gone = dropped[s];
   const long long cap = static_cast<long long>(p.max_pages) * p.page_tokens;
-  if (kept < 0) return;
+  if (kept < 0) {
+    if (kept < -1 && threadIdx.x == 0) record_status(p.status, MLA_ERR_RANGE);
+    return;
+  }
   if (len < 0 || len > cap || gone < 0) {
     if (threadIdx.x == 0) record_status(p.status, MLA_ERR_RANGE);
     return;

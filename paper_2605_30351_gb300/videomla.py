@@ -690,7 +690,8 @@ def mla_paged_window_attention(cache, window, layer, q_c, q_r, q_r_sink, q_start
 
 def mla_pages_slide(cache, window, keep, stream=None):
     """Give back the pages between the sinks' and the newest keep [seqs] tokens
-    (-1: leave the stream alone); the streams' page lists close up."""
+    (max(0, window - block); -1: leave the stream alone); the streams' page lists
+    close up."""
     _check("mla_pages_slide",
            load().mla_pages_slide(cache.ref, _window_ref(cache, window),
                                   _ptr(keep, torch.int32, (cache.seqs,), "keep"),

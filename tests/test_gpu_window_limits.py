@@ -1,5 +1,5 @@
 """Where the streams of a sliding window end: lists cut back into the sinks' pages, the rotary
-table."""
+table, windows shorter than a block."""
 
 import importlib.util
 import os
@@ -170,3 +170,60 @@ def test_the_example_past_the_usual_table():
     worst, held, gone = m.main(chunks=172, rollouts=1, frames=6)
     assert worst <= 2e-2
     assert [h + g for h, g in zip(held, gone)] == [1032 * 64]
+
+
+@pytest.mark.parametrize("window,block", [(20, 32), (1, 8), (31, 32), (32, 32), (50, 100)])
+def test_a_window_shorter_than_a_block(window, block):
+    """Blocks longer than the window: the next block sees no key of those before it, so
+    max(0, window - block) tokens are kept. The list stays short however long the stream gets,
+    and a block's rows see the newest keys of their own block and the sinks."""
+    page, sinks = 16, 5
+    most = -(-sinks // page) + -(-(max(0, window - block) + page + block) // page)
+    cache = V.PagedCache.empty(1, most + 1, page, 1, most, 64, 32)
+    win = V.PagedWindow(window, sinks, i32([0]))
+    keep, n = i32([max(0, window - block)]), i32([block])
+    q_start, lens = ints(2), ints(1)
+    g = torch.Generator(device="cuda").manual_seed(window)
+    ws = torch.empty(V.mla_paged_workspace_bytes(cache), dtype=torch.uint8, device="cuda")
+    rope = V.Rope(torch.from_numpy(V.mla_rope_scaled_table_fill(32, 40 * block)).cuda(), (16, 0, 0), axes=1)
+    pos = ints(block, 1)
+    for step in range(40):
+        V.mla_paged_window_plan(cache, win, n, q_start, lens)
+        V.mla_pages_resize(cache, lens)
+        V.mla_paged_window_positions(cache, win, q_start, block, 1, 1, pos)
+        assert pos[:, 0].tolist() == list(range(step * block, (step + 1) * block))
+        c, kr, q_c, q_r = (torch.randn(*s, device="cuda", generator=g).to(BF16) for s in
+                           ((block, 64), (block, 32), (block, 4, 64), (block, 4, 32)))
+        V.mla_paged_append(cache, 0, c, kr, q_start, pos, rope)
+        o = torch.full_like(q_c, float("nan"))
+        V.mla_paged_window_attention(cache, win, 0, q_c, q_r, None, q_start, 128, block, ws, o)
+        if step in (0, 1, 7, 39):
+            held, gone = int(cache.lens[0]), int(win.dropped[0])
+            a = np.arange(held)
+            ids = cache.table[0].cpu().numpy()[a // page]
+            k, r = (t[0].double().cpu().numpy()[ids, a % page] for t in (cache.c, cache.kr))
+            sees = O.window_sees(held - 1, held, gone, block, window, sinks, page)
+            for i in (0, block - 1):                  # the rows of a block see the same
+                ref, size = O.attend_window(q_c[i].double().cpu().numpy(), *2 * [q_r[i].double().cpu().numpy()],
+                                            k, r, sees, 128)
+                assert (np.abs(o[i].double().cpu().numpy() - ref) <= REL * size).all(), (step, i)
+        V.mla_pages_slide(cache, win, keep)
+    assert V.mla_device_status(clear=True) == V.MLA_OK
+    assert int(cache.lens[0] + win.dropped[0]) == 40 * block
+
+
+def test_a_negative_count_to_keep():
+    """-1 leaves a stream alone; any other negative count, as w - b of a block longer than the
+    window, is recorded too."""
+    cache = V.PagedCache.empty(1, 40, 8, 3, 12, 8, 8)
+    win = V.PagedWindow(5, 3, i32([0, 0, 0]))
+    V.mla_pages_resize(cache, i32([60, 60, 60]))
+    for bad in (-2, -12, -2 ** 31):
+        V.mla_pages_slide(cache, win, i32([-1, bad, -1]))
+        assert V.mla_device_status(clear=True) == V.MLA_ERR_RANGE, bad
+        assert cache.lens.tolist() == [60] * 3 and win.dropped.tolist() == [0] * 3
+    V.mla_pages_slide(cache, win, i32([-1, -7, 20]))
+    assert V.mla_device_status(clear=True) == V.MLA_ERR_RANGE
+    assert cache.lens.tolist() == [60, 60, 28] and win.dropped.tolist() == [0, 0, 32]
+    V.mla_pages_slide(cache, win, i32([-1, -1, -1]))
+    assert V.mla_device_status(clear=True) == V.MLA_OK
