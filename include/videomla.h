@@ -692,6 +692,18 @@ int mla_pages_window_fork(mla_paged_cache* cache, const mla_paged_window* window
  */
 int mla_selftest_bounded_wait(unsigned long long limit_ns, void* stream);
 
+/*
+ * Self-test of the forms of mla_paged_window_attention: the calls of this process take the
+ * form named here, whatever their sizes, until another is named.
+ *   form   0 = by the library's estimates of their times (as without this call), 1, 2, 4, 8 =
+ *          teams of so many CTAs, 16 = shares of tiles of 16 rows, 128 = tiles of 128 rows,
+ *          256 = tiles of 256 rows, a pair of CTAs each
+ *   taken  the form that the last call took (0: there was none), NULL: not wanted
+ * All forms give what the description says; their sums run in different orders. d_c = 512 has
+ * 128 only: others make such calls MLA_ERR_UNSUPPORTED. MLA_ERR_ARG for another form.
+ */
+int mla_selftest_window_form(int form, int* taken);
+
 /* Human-readable name of a status code. */
 const char* mla_status_string(int status);
 

@@ -188,6 +188,7 @@ struct PagedAttnArgs {
   const void* q_sink = nullptr;   // bf16 [total][heads][d_r], or none: q_r
   const int* dropped = nullptr;   // int32 [seqs], or none: zeros
   int window = 0, sinks = 0;
+  int form = 0;  // as mla_selftest_window_form; 0: chosen by sizes
 };
 
 // Rows of a step's tokens and their coordinates.
@@ -231,6 +232,7 @@ int launch_paged_window_plan(const mla_paged_cache& c, int* dropped, const int* 
                              int* q_start, int* new_lens, int* status, cudaStream_t stream);
 int launch_paged_positions(const PagedPositionsArgs& a);
 int launch_paged_window_attention(const PagedAttnArgs& a);
+int window_form(int form, int* taken);
 int launch_pages_copy(const mla_paged_cache& c, const int* src, const int* dst, int n,
                       int* status, cudaStream_t stream);
 int launch_pages_compact(const mla_paged_cache& c, int* new_table, int* new_refs, int* status,

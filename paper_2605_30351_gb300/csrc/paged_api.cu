@@ -247,6 +247,8 @@ int mla_paged_window_attention(const mla_paged_cache* cache, const mla_paged_win
   return launch_paged_window_attention(a);
 }
 
+int mla_selftest_window_form(int form, int* taken) { return window_form(form, taken); }
+
 int mla_paged_window_plan(const mla_paged_cache* cache, const mla_paged_window* window,
                           const int* n_new, int* q_start, int* new_lens, void* stream) {
   if (!n_new || !q_start || !new_lens || !aligned_to(n_new, 4) || !aligned_to(q_start, 4) ||

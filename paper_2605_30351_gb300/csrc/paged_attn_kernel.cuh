@@ -1047,14 +1047,17 @@ int launch_paged(const PagedAttnArgs& a) {
 // tile from L2 once for 256 rows. Shorter ones would leave half a pair idle (ragged
 // prompts 51 us with pairs, 60 without). Idle slots count as short streams here too: a
 // 4,680-token chunk on 32,760 keys 820 us in a pool of 4 slots, 891 of 256.
+inline bool takes_pairs(const PagedAttnArgs& a) {
+  if (a.form != 0) return a.form == 2 * kBM;
+  return static_cast<long long>(a.total) * a.heads >= 2ll * kBM * a.seqs;
+}
+
 template <int DC, int DR, bool WIN>
 int pick(const PagedAttnArgs& a) {
   if constexpr (PagedShape<DC, DR, WIN>::kSplit == 2) {
     return launch_paged<DC, DR, 2, WIN>(a);
   } else {
-    return static_cast<long long>(a.total) * a.heads >= 2ll * kBM * a.seqs
-               ? launch_paged<DC, DR, 2, WIN>(a)
-               : launch_paged<DC, DR, 1, WIN>(a);
+    return takes_pairs(a) ? launch_paged<DC, DR, 2, WIN>(a) : launch_paged<DC, DR, 1, WIN>(a);
   }
 }
 

@@ -1,6 +1,7 @@
 // Attention of ragged streams' newest tokens over the sinks and the sliding window of a
 // paged latent cache (Eq. score; App. D.4, D.5, E): the choice of a kernel.
 #include <algorithm>
+#include <atomic>
 #include <numeric>
 
 #include "paged_attn_kernel.cuh"
@@ -26,6 +27,12 @@ namespace {
 // 22.5, 17.0.
 int team_of(const PagedAttnArgs& a, bool tall, int& teams) {
   const long long rows = static_cast<long long>(a.total) * a.heads;
+  const long long most = rows / 16 + a.seqs;  // teams that may find work
+  if (a.form != 0) {
+    const int slots = a.form <= 8 ? window_team_slots(a.form) : 0;
+    teams = static_cast<int>(std::min<long long>(slots, most));
+    return slots > 0 ? a.form : 0;
+  }
   const long long page = a.page_tokens, bn = 128;
   const bool divides = bn % page == 0;
   // the window of a tile's tokens, ends in pages
@@ -53,22 +60,55 @@ int team_of(const PagedAttnArgs& a, bool tall, int& teams) {
     if (cost < best) {
       best = cost;
       team = t;
-      teams = static_cast<int>(std::min<long long>(slots, rows / 16 + a.seqs));
+      teams = static_cast<int>(std::min<long long>(slots, most));
     }
   }
   return team;
 }
 
+// mla_selftest_window_form: what is asked for, and what the last call took
+std::atomic<int> asked_form{0}, taken_form{0};
+
 }  // namespace
 
-int launch_paged_window_attention(const PagedAttnArgs& a) {
-  const bool tall = static_cast<long long>(a.total) * a.heads > 16ll * a.seqs;
-  if (a.d_c <= 256) {
+int window_form(int form, int* taken) {
+  switch (form) {
+    case 0:
+    case 1:
+    case 2:
+    case 4:
+    case 8:
+    case 16:
+    case kBM:
+    case 2 * kBM: break;
+    default: return MLA_ERR_ARG;
+  }
+  asked_form = form;
+  if (taken) *taken = taken_form;
+  return MLA_OK;
+}
+
+int launch_paged_window_attention(const PagedAttnArgs& call) {
+  PagedAttnArgs a = call;
+  a.form = asked_form;
+  const bool short_forms = a.d_c <= 256;  // d_c = 512 has tiles of 128 rows only
+  if (a.form != 0 && !short_forms && a.form != kBM) return MLA_ERR_UNSUPPORTED;
+  const bool tall = a.form != 0 ? a.form >= kBM
+                                : static_cast<long long>(a.total) * a.heads > 16ll * a.seqs;
+  if (short_forms) {
     int teams = 0;
     const int team = team_of(a, tall, teams);
-    if (team > 0) return launch_window_teams(a, team, teams);
-    if (!tall) return launch_window_decode(a);
+    if (team > 0) {
+      taken_form = team;
+      return launch_window_teams(a, team, teams);
+    }
+    if (a.form != 0 && a.form <= 8) return MLA_ERR_UNSUPPORTED;
+    if (!tall) {
+      taken_form = 16;
+      return launch_window_decode(a);
+    }
   }
+  taken_form = short_forms && takes_pairs(a) ? 2 * kBM : kBM;
   return a.d_r == 32 ? pick_dc<32, true>(a) : pick_dc<64, true>(a);
 }
 

@@ -47,7 +47,8 @@ EXPORTS = ("mla_rope_table_bytes", "mla_rope_table_fill", "mla_config_check",
            "mla_pages_compact", "mla_paged_append", "mla_paged_workspace_bytes",
            "mla_paged_attention", "mla_paged_window_plan", "mla_paged_window_positions",
            "mla_paged_window_attention", "mla_pages_slide", "mla_pages_window_fork",
-           "mla_selftest_bounded_wait", "mla_status_string", "mla_last_cuda_error", "mla_device_status",
+           "mla_selftest_bounded_wait", "mla_selftest_window_form", "mla_status_string",
+           "mla_last_cuda_error", "mla_device_status",
            "mla_debug_rescale_count", "mla_version")
 
 
@@ -138,6 +139,7 @@ def load():
     lib.mla_dense_attention_forward.argtypes = [P(mla_config), VP, VP, VP, I, I, I, VP, VP]
     lib.mla_decompress_window.argtypes = [P(mla_cache), VP, VP, VP, VP, VP]
     lib.mla_selftest_bounded_wait.argtypes = [ctypes.c_ulonglong, VP]
+    lib.mla_selftest_window_form.argtypes = [I, P(ctypes.c_int)]
     lib.mla_window_workspace_bytes.argtypes = [P(mla_config), I]
     lib.mla_window_workspace_bytes.restype = ctypes.c_ulonglong
     lib.mla_attention_window_forward.argtypes = [P(mla_cache), VP, VP, VP, I, VP, VP,
@@ -175,7 +177,7 @@ def load():
                  "mla_version", "mla_absorb_weights", "mla_query_prologue",
                  "mla_query_prologue_noalloc", "mla_output_projection",
                  "mla_dense_attention_forward", "mla_attention_window_forward",
-                 "mla_decompress_window", "mla_selftest_bounded_wait",
+                 "mla_decompress_window", "mla_selftest_bounded_wait", "mla_selftest_window_form",
                  "mla_debug_rescale_count"):
         getattr(lib, name).restype = I
     _lib = lib
@@ -709,6 +711,15 @@ def mla_selftest_bounded_wait(limit_ns, stream=None):
     """Make one bounded device wait run out (nothing arrives on its barrier)."""
     _check("mla_selftest_bounded_wait",
            load().mla_selftest_bounded_wait(int(limit_ns), _stream_ptr(stream)))
+
+
+def mla_selftest_window_form(form=0):
+    """Make mla_paged_window_attention take one of its forms (0: as it chooses);
+    returns the form that the last call took."""
+    taken = ctypes.c_int(0)
+    _check("mla_selftest_window_form",
+           load().mla_selftest_window_form(int(form), ctypes.byref(taken)))
+    return taken.value
 
 
 def mla_device_status(clear=True):
