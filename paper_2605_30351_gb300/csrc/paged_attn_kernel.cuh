@@ -774,23 +774,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         if constexpr (WIN) {
           valid = min(pos.rows(p), v.valid);
           sees = v.sinks > 0 || max(v.low, 0) < valid;
-          // Most blocks hide no keys, those at a window's ends a run or two. 32 keys at a time
-          // by a bit each that is 2 - 15 % faster where windows are short (3,167 tokens, windows
-          // of 281 keys, d_c = 128: 197 -> 169 us); compared key by key, at d_c = 192 the loop
-          // over blocks that hide none is faster (four chunks 1,075 -> 1,035 us) for 1 - 4 %
-          // where windows are short.
-          if constexpr (DC == 192) {
-            if (v.low > 0 && v.sinks < BN) {
-#pragma unroll
-              for (int c = 0; c < BN; ++c)
-                if (c < v.low && c >= v.sinks) sv[c] = -INFINITY;
-            }
-            if (valid < BN) {
-#pragma unroll
-              for (int c = 0; c < BN; ++c)
-                if (c >= valid) sv[c] = -INFINITY;
-            }
-          } else if (v.low > 0 || valid < BN) {
+          // Most blocks hide no keys, those at a window's ends a run or two: 32 keys at a time by a
+          // bit each. Compared key by key, short windows (281 and 1,024 keys) take longer: 3 - 5 % at
+          // d_c = 64 and 128, 1 - 3 at 192, 2 - 4 at 256, up to 1 at 512. Long ones (four chunks on
+          // 10,920 keys) take 0.7 and 0.5 % less at 64 and 128, 1.6 more at 256, the same at 512, and
+          // less at 192: 3.3 % with d_r = 32 (1,037 for 1,072 us), 1.7 with 64. A vote of the warp
+          // before the branch, or a branch for each 32 keys, changes neither at 192.
+          if (v.low > 0 || valid < BN) {
 #pragma unroll
             for (int q = 0; q < BN / 32; ++q) {
               const unsigned shown = low_bits(valid - 32 * q) &
