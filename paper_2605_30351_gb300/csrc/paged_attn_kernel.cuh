@@ -7,8 +7,11 @@
 //     P = exp2(S * log2(e)/sqrt(d_h) - m)   running maximum and sum in fp32, the sum
 //                                      over unrounded weights; P is rounded to
 //                                      bf16 (the type of c, as the MMA takes both
-//                                      operands of one type): the results' errors are
-//                                      1.0 to 1.3 times those of fp32 weights
+//                                      operands of one type). That rounding is as large
+//                                      as the output's and independent of it: the
+//                                      results' errors are up to sqrt(2) times those of
+//                                      fp32 weights, where many keys weigh alike
+//                                      (measured 1.0 - 1.25; simulated 1.09 - 1.42)
 //     O += P . c                       N = d_c, c read again from the same tile
 //
 // Work is split evenly whatever the streams look like: all (row tile, key block)
