@@ -161,7 +161,7 @@ struct NoMap {};
 template <bool WIN>
 using SinkMap = std::conditional_t<WIN, CUtensorMap, NoMap>;
 
-template <int DC, int DR, int CL, bool WIN>
+template <int DC, int DR, int CL, bool WIN, bool KEYS>
 __global__ void __launch_bounds__(kThreads, 1)
     paged_attn_kernel(const __grid_constant__ CUtensorMap tm_c,
                       const __grid_constant__ CUtensorMap tm_kr,
@@ -778,12 +778,19 @@ __global__ void __launch_bounds__(kThreads, 1)
           valid = min(pos.rows(p), v.valid);
           sees = v.sinks > 0 || max(v.low, 0) < valid;
           // Most blocks hide no keys, those at a window's ends a run or two: 32 keys at a time by a
-          // bit each. Compared key by key, short windows (281 and 1,024 keys) take longer: 3 - 5 % at
-          // d_c = 64 and 128, 1 - 3 at 192, 2 - 4 at 256, up to 1 at 512. Long ones (four chunks on
-          // 10,920 keys) take 0.7 and 0.5 % less at 64 and 128, 1.6 more at 256, the same at 512, and
-          // less at 192: 3.3 % with d_r = 32 (1,037 for 1,072 us), 1.7 with 64. A vote of the warp
-          // before the branch, or a branch for each 32 keys, changes neither at 192.
-          if (v.low > 0 || valid < BN) {
+          // bit each, or (KEYS, see keyed) key by key.
+          if constexpr (KEYS) {
+            if (v.low > 0 && v.sinks < BN) {
+#pragma unroll
+              for (int c = 0; c < BN; ++c)
+                if (c < v.low && c >= v.sinks) sv[c] = -INFINITY;
+            }
+            if (valid < BN) {
+#pragma unroll
+              for (int c = 0; c < BN; ++c)
+                if (c >= valid) sv[c] = -INFINITY;
+            }
+          } else if (v.low > 0 || valid < BN) {
 #pragma unroll
             for (int q = 0; q < BN / 32; ++q) {
               const unsigned shown = low_bits(valid - 32 * q) &
@@ -953,7 +960,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if constexpr (CL > 1) cluster_sync();
 }
 
-template <int DC, int DR, int CL, bool WIN>
+template <int DC, int DR, int CL, bool WIN, bool KEYS = false>
 int launch_paged(const PagedAttnArgs& a) {
   using S = PagedShape<DC, DR, WIN>;
   const PagedP<WIN> k = paged_params<WIN>(a, S::BN, S::DV);
@@ -980,7 +987,7 @@ int launch_paged(const PagedAttnArgs& a) {
                  DR == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
       return MLA_ERR_CUDA;
   }
-  auto kern = paged_attn_kernel<DC, DR, CL, WIN>;
+  auto kern = paged_attn_kernel<DC, DR, CL, WIN, KEYS>;
   // resident CTAs of this instance (one per SM, whole clusters), asked once
   static PerDevice known;
   std::atomic<int>* cell = known.cell();
@@ -1045,12 +1052,29 @@ inline bool takes_pairs(const PagedAttnArgs& a) {
   return static_cast<long long>(a.total) * a.heads >= 2ll * kBM * a.seqs;
 }
 
+// How a window's hidden keys leave a row's scores. Rows whose mask gives them a window each (token
+// by token) take a bit a key; rows of a block of the mask agree on what they see, so a warp has
+// one end of the window in a block at most and compares key by key. Pairs, windows of 500 / 2,000 /
+// 8,000 / 30,000 keys, us by bits and by keys:
+//   d_c     2 x 3,000 tokens, token by token                1 x 4,680 tokens, one block
+//    64  50 / 82 / 215 / 703, 53 / 84 / 222 / 728      96 / 141 / 207 / 587,  88 / 134 / 206 / 600
+//   128  57 / 101 / 272 / 887, 60 / 105 / 276 / 902   115 / 163 / 256 / 738, 102 / 152 / 255 / 741
+//   192  63 / 106 / 275 / 889, 64 / 106 / 271 / 863   120 / 171 / 259 / 743, 115 / 166 / 249 / 726
+//   256  83 / 164 / 478 / 1628, 84 / 166 / 489 / 1676 146 / 214 / 444 / 1340, 144 / 212 / 450 / 1375
+// (128 with d_r = 64, the others with 32). Beyond d_c = 192 keys give no more than they cost (at
+// 512 3 % less to 2 % more). Both in one kernel, by a branch, is 1 - 3 % slower token by token
+// at 64 and 128.
+inline bool keyed(const PagedAttnArgs& a) { return a.causal_block != 1; }
+
 template <int DC, int DR, bool WIN>
 int pick(const PagedAttnArgs& a) {
   if constexpr (PagedShape<DC, DR, WIN>::kSplit == 2) {
     return launch_paged<DC, DR, 2, WIN>(a);
   } else {
-    return takes_pairs(a) ? launch_paged<DC, DR, 2, WIN>(a) : launch_paged<DC, DR, 1, WIN>(a);
+    if (!takes_pairs(a)) return launch_paged<DC, DR, 1, WIN>(a);
+    if constexpr (WIN && DC <= 192)
+      if (keyed(a)) return launch_paged<DC, DR, 2, WIN, true>(a);
+    return launch_paged<DC, DR, 2, WIN>(a);
   }
 }
 

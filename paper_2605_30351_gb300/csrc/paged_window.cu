@@ -12,14 +12,20 @@ namespace {
 // A window bounds what a tile of 16 rows needs, so the host knows how many key blocks of 128
 // that may be, and whether a team of a few CTAs is done with it sooner than shares of all
 // tiles' blocks and their join, a second launch. Estimates in tenths of a us, from calls with
-// 64 sinks and pages of 64 tokens at d_c = 192; at d_c = 64 and 256 all of them move together.
+// 64 sinks and pages of 64 tokens at d_c = 192, used at every width; the clusters that run at a
+// time are asked of d_c = 192's instance, which has one CTA an SM (d_c = 64's could have two).
 //   teams   a wave of them takes 7 us and 1.4 a block, whatever the others do, 0.5 more where
 //           streams may have more than one tile; teams of more than one CTA 1.2 more in all
 //   shares  11.5 us, 1.4 for the blocks that each SM has on average and 3 for its tiles
 //   tiles of 128 rows (streams of more than 16 rows on average)  16 us and 1.2 a block
 // Blocks are what the windows bound; shares, and more so tiles of 128 rows, gain where streams
-// are shorter, and the estimates are fitted to such calls too (410 of one to a few tokens of 1 -
-// 300 streams, whole and ragged, d_c 64 - 256): the choice takes 1.2 % longer than the best.
+// are shorter, and the estimates are fitted to such calls too. Of 400 other calls, drawn (1 - 17
+// tokens of 1 - 300 streams, whole and ragged, 50 for each d_c and d_r), every form was timed: the
+// choice takes longer than the best by 1.3 and 1.7 % on average at d_c = 64 with d_r = 32 and 64,
+// 2.6 and 2.2 at 128, 3.2 and 2.6 at 192, 2.4 and 5.2 at 256, at most by 46; always shares 28 %,
+// always tiles of 128 rows 27, always teams of one CTA 66. Farthest off: a token or two of some 200
+// streams. Every slot of the pool counts as a stream with work, as the host does not know which
+// are idle.
 // Measured, one token of n streams, window w (teams of 8, 4, 2, 1: the best; shares):
 //   n = 1, w = 300: 8.8, 10.6   n = 12, w = 2,000: 12.0, 13.7  n = 76, w = 1,000: 17.7, 23.3
 //   n = 1, w = 4,000: 13.7, 11.5  n = 38, w = 4,000: 34.4, 27.4  n = 96, w = 300: 11.4, 14.5

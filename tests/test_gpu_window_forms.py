@@ -80,6 +80,15 @@ def test_blocks(form, d_c):
                 run(form, T.Problem([333, 200, 150, 1], [3, 1, 2, 1], window, 30, block, gone=gone, d_c=d_c), 6)
 
 
+@pytest.mark.parametrize("d_c,d_r", WIDTHS)
+def test_blocks_in_pairs(d_c, d_r):
+    """Tiles of 256 rows mask hidden keys in two ways, token by token and by blocks of the mask."""
+    for block, window, page in ((0, 40, 16), (7, 100, 64), (64, 300, 100), (100, 20, 32), (1, 130, 24)):
+        for sinks in (0, 70):
+            run(PAIRS, T.Problem([600, 200, 150, 1], [300, 200, 64, 1], window, sinks, block, heads=12, d_c=d_c,
+                                 d_r=d_r, page=page, turned=block != 7, gone=[page * 2, 0, 0, 0]), 6)
+
+
 @pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("page", [8, 24, 32, 48, 96, 120, 128, 200, 256])
 def test_page_sizes(form, page):
