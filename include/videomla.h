@@ -622,7 +622,10 @@ int mla_paged_window_plan(const mla_paged_cache* cache, const mla_paged_window* 
  *     pos_sink[i]  the same with t counted as App. D.5 does, sinks and window held next to
  *                  each other: t - floor(k / T), k = max(0, e - window - sinks) the tokens
  *                  between the sinks and the first one that the window holds, e the end of
- *                  what token i sees (see mla_paged_window_attention). NULL: not wanted
+ *                  what token i sees (see mla_paged_window_attention). NULL: not wanted.
+ *                  Below 0 for tokens that many before their window, in blocks longer than
+ *                  window + sinks: no rotary table has that (MLA_ERR_RANGE when rotating), so
+ *                  with such blocks the sinks have no queries of their own
  *     rows[i]      its row of the pool, page * page_tokens + place in the page. NULL: not
  *                  wanted
  * T and frame_width are at least 1, frame_width at most T. A token without a page has the

@@ -227,3 +227,24 @@ def test_a_negative_count_to_keep():
     assert cache.lens.tolist() == [60, 60, 28] and win.dropped.tolist() == [0, 0, 32]
     V.mla_pages_slide(cache, win, i32([-1, -1, -1]))
     assert V.mla_device_status(clear=True) == V.MLA_OK
+
+
+def test_coordinates_beside_the_sinks_in_long_blocks():
+    """In blocks of at most window + sinks tokens no coordinate beside the sinks is negative; in
+    longer ones it is for tokens far before their window, and the rotation records it."""
+    page, window, sinks = 16, 20, 12
+    rope = V.Rope(torch.from_numpy(V.mla_rope_scaled_table_fill(32, 512)).cuda(), (16, 0, 0), axes=1)
+    for block in (7, 32, 33, 100, 0):
+        cache = V.PagedCache.empty(1, 30, page, 1, 30, 8, 8)
+        V.mla_pages_resize(cache, i32([300]))
+        win, pos, beside = V.PagedWindow(window, sinks, i32([0])), ints(300, 1), ints(300, 1)
+        V.mla_paged_window_positions(cache, win, i32([0, 300]), block, 1, 1, pos, beside)
+        assert V.mla_device_status(clear=True) == V.MLA_OK
+        want, apart = O.window_positions(300, 0, 300, block, window, sinks, 1, 1, page)
+        assert pos[:, 0].tolist() == [v[0] for v in want]
+        assert beside[:, 0].tolist() == [v[0] for v in apart]
+        low = int(beside.min())
+        assert (low < 0) == (block in (33, 100, 0)), (block, low)
+        x = torch.randn(300, 1, 32, device="cuda").to(BF16)
+        V.mla_rope_apply(rope, x, beside, torch.empty_like(x))
+        assert V.mla_device_status(clear=True) == (V.MLA_ERR_RANGE if low < 0 else V.MLA_OK)
