@@ -98,6 +98,29 @@ def test_page_sizes(form, page):
                                 heads=5, d_c=d_c, turned=turned), 5)
 
 
+@pytest.mark.parametrize("form", FORMS)
+def test_odd_page_sizes(form):
+    """Pages of any size from 8 tokens on, odd ones and longer than several blocks of keys."""
+    for page in (9, 13, 50, 127, 129, 300):
+        front = O.front(70, page)
+        for turned in (True, False):
+            run(form, T.Problem([front + 450, 3, 700], [40, 2, 1], 150, 70, gone=[page * 2, 0, 0], page=page, heads=5,
+                                d_c=128, turned=turned), 5)
+            if form == TILES:
+                run(form, T.Problem([front + 450, 3, 700], [40, 2, 1], 150, 70, gone=[page * 2, 0, 0], page=page,
+                                    heads=5, d_c=512, turned=turned), 5)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_as_many_slots_as_there_may_be(form):
+    """65,536 slots, six of them with work."""
+    seqs = 65536
+    lens, new = [0] * seqs, [0] * seqs
+    for s, (k, n) in zip((0, 1, 777, 40000, 65534, 65535), ((300, 1), (40, 30), (90, 2), (5, 5), (400, 1), (33, 4))):
+        lens[s], new[s] = k, n
+    run(form, T.Problem(lens, new, 64, 10, heads=3, d_c=128), 4)
+
+
 @pytest.mark.parametrize("page", [8, 24, 48, 64, 100, 200])
 def test_page_sizes_of_the_widest(page):
     for new in (1, 5, 40):
