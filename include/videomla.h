@@ -666,6 +666,7 @@ int mla_paged_window_attention(const mla_paged_cache* cache, const mla_paged_win
  * of each stream to keep (-1 = leave the stream alone). The whole pages that lie between
  * the sinks' pages and the newest keep[s] tokens leave the stream's list, which closes up:
  *     lens[s] -= n,  dropped[s] += n,  n a multiple of page_tokens.
+ * (0 counts as 1: a stream that held no token would start anew.)
  * What the next step's first token sees of a window w is kept with keep = w - 1 (token by
  * token; max(0, w - b) with blocks of b tokens that a step fills). A count below -1, as
  * w - b of blocks longer than the window, is recorded as MLA_ERR_RANGE and leaves the stream

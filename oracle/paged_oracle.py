@@ -197,13 +197,15 @@ def attend_window(q_c, q_r, q_sink, c, kr, places, head_dim):
 
 
 def slide(pages, gone, keep, sinks):
-    """Pages (above) and gone [seqs] after the pages between sinks and window went."""
+    """Pages (above) and gone [seqs] after the pages between sinks and window went; the last
+    page stays, as a stream that holds no token is one that ended."""
     P, first = pages.P, front(sinks, pages.P) // pages.P
     for s, k in enumerate(keep):
         if k < 0:
             continue
         row = [int(v) for v in pages.table[s]]
-        n = max(0, (int(pages.lens[s]) - int(k)) // P - first) if pages.lens[s] > k else 0
+        k = max(int(k), 1)
+        n = max(0, (int(pages.lens[s]) - k) // P - first) if pages.lens[s] > k else 0
         for v in row[first:first + n]:
             pages.refs[v] -= 1
         row = row[:first] + row[first + n:] + [-1] * n if n else row

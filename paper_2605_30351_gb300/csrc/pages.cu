@@ -303,7 +303,8 @@ __global__ void __launch_bounds__(kCopy)
     if (threadIdx.x == 0) record_status(p.status, MLA_ERR_RANGE);
     return;
   }
-  const int n = (len > kept ? len - kept : 0) / p.page_tokens - front;
+  // a stream that holds no token starts anew (window_plan_kernel): its last page stays
+  const int most = max(kept, 1), n = (len > most ? len - most : 0) / p.page_tokens - front;
   if (n <= 0) return;
   if (static_cast<long long>(gone) + len >= kMostTokens) {
     if (threadIdx.x == 0) record_status(p.status, MLA_ERR_RANGE);

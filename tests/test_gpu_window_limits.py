@@ -248,3 +248,27 @@ def test_coordinates_beside_the_sinks_in_long_blocks():
         x = torch.randn(300, 1, 32, device="cuda").to(BF16)
         V.mla_rope_apply(rope, x, beside, torch.empty_like(x))
         assert V.mla_device_status(clear=True) == (V.MLA_ERR_RANGE if low < 0 else V.MLA_OK)
+
+
+@pytest.mark.parametrize("window,block,page", [(16, 16, 16), (20, 32, 8), (1, 8, 8), (30, 48, 24)])
+def test_a_stream_without_sinks_keeps_its_count(window, block, page):
+    """A window of no more than the next block keeps nothing of what is held. Without sinks and with
+    whole pages all of it could go; but a stream that holds no token starts anew, at index 0, so a slide
+    leaves the last page. A stream that ended does start anew."""
+    cache = V.PagedCache.empty(1, 24, page, 2, 12, 8, 8)
+    win = V.PagedWindow(window, 0, i32([0, 0]))
+    n, keep = i32([block, block]), i32([max(0, window - block)] * 2)
+    q_start, lens, pos = ints(3), ints(2), ints(2 * block, 1)
+    first = [0, 0]
+    for step in range(30):
+        V.mla_paged_window_plan(cache, win, n, q_start, lens)
+        V.mla_pages_resize(cache, lens)
+        V.mla_paged_window_positions(cache, win, q_start, block, 1, 1, pos)
+        assert pos[:, 0].tolist() == [f + i for f in first for i in range(block)], step
+        V.mla_pages_slide(cache, win, keep)
+        assert all(0 < k <= page for k in cache.lens.tolist())
+        first = [f + block for f in first]
+        if step == 11:
+            V.mla_pages_resize(cache, i32([-1, 0]))
+            first[1] = 0
+    assert V.mla_device_status(clear=True) == V.MLA_OK
