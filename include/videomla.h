@@ -669,9 +669,9 @@ int mla_paged_window_attention(const mla_paged_cache* cache, const mla_paged_win
  * (0 counts as 1: a stream that held no token would start anew.)
  * What the next step's first token sees of a window w is kept with keep = w - 1 (token by
  * token; max(0, w - b) with blocks of b tokens that a step fills); where mla_pages_resize may
- * cut up to r of the newest tokens off again (rejected drafts), with r more. A count below -1,
- * as w - b of blocks longer than the window, is recorded as MLA_ERR_RANGE and leaves the
- * stream alone. A page whose last stream this was is free afterwards; a page that branches
+ * cut up to r of the newest tokens off again (rejected drafts), with r more, r + 1 at least.
+ * A count below -1, as w - b of blocks longer than the window, is recorded as MLA_ERR_RANGE
+ * and leaves the stream alone. A page whose last stream this was is free afterwards; a page that branches
  * share stays theirs. A page number outside the pool is recorded as MLA_ERR_RANGE and leaves
  * the list; a stream whose indices would pass 2^31 - 2^16 is recorded and left alone, as is
  * one whose length its table cannot hold or whose dropped is negative. dropped must not be
